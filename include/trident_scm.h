@@ -118,6 +118,57 @@ typedef enum trident_dtype {
  *
  * TRIDENT_OP_LAYER_CHAIN_QKNORM (20 tensors): LAYER_CHAIN with QKNORM_ROPE_KV instead of
  *   ROPE_KV; 18 gamma_q [D] fp32, 19 gamma_k [D] fp32.
+ *
+ * Paged serving: B requests of unequal lengths share a pool of P cache pages of ps tokens each;
+ * request b's token at position j lives on page block_table[b, j / ps], row j % ps.
+ *
+ * TRIDENT_OP_PAGE_MAP (10 tensors, all i32; T = B; scalar = ps, a whole number in [1, 65536])
+ *   0 ctx_len [B]  1 new_len [B]  2 free_pages [F]  3 free_head [1]  4 block_table [B,M] (in/out)
+ *   5 cu_q [B+1] (out)  6 kv_len [B] (out)  7 pos [N] (out)  8 slot [N] (out)  9 free_head_out [1] (out)
+ *   Request b has ctx_len tokens in the cache and gets new_len more (each >= 0). With
+ *   have = ceil(ctx / ps) and need = ceil((ctx + new) / ps), its pages have .. need-1 are the next
+ *   entries of free_pages after free_head, requests in order; they are written to the table.
+ *   cu_q[b] = sum of new_len before b;  kv_len = ctx + new;  free_head_out = free_head + pages taken.
+ *   New token n of request b (i = n - cu_q[b]): pos[n] = ctx + i; slot[n] = page * ps + pos[n] % ps.
+ *   The rows of pos and slot past the last token are padding: pos 0, slot -1.
+ *   All or nothing: with a negative length, more than N tokens, more than M pages for a request or
+ *   too few free pages (or free_head outside [0,F]) nothing is handed out (cu_q 0, kv_len = ctx_len,
+ *   every slot -1, free_head_out = free_head, table untouched) and TRIDENT_DEVERR_PAGES is set. A
+ *   table entry of the last held page that is no page number (negative, or its slot past 2^31-1)
+ *   gives slot -1 and sets TRIDENT_DEVERR_TABLE.
+ *
+ * TRIDENT_OP_ROPE_PAGED_KV (9 tensors; act = bf16 | fp16; scalar = the magnitude of cos and sin, > 0)
+ *   0 q [T,Hq,D] act  1 k [T,Hkv,D] act  2 v [T,Hkv,D] act  3 pos [T] i32  4 slot [T] i32
+ *   5 freqs [R/2,2] fp32  6 q_out [T,Hq,D] act (out)
+ *   7 k_cache [P,Hkv,ps,D] act (out)  8 v_cache [P,Hkv,ps,D] act (out)
+ *   Rotates the first R elements of each q and k head (R even, <= D; the others pass through): pairs
+ *   (i, i + R/2), i < R/2, angle a = pos * f_i, f_i = freqs[i,0] + freqs[i,1] (trident_rope_freqs
+ *   fills such a table, also for positions rescaled to long contexts), scalar * cos a and
+ *   scalar * sin a in the place of cos and sin. q_out = round(rope(q)) (in place: q_out = q);
+ *   k_cache[slot / ps, h, slot % ps, :] = round(rope(k)); the same row of v_cache = v (bit copy).
+ *   The caches may have any page, head and row strides (elements of a row packed) that give every
+ *   element bytes of its own. A slot below 0 is padding: its token's k and v are dropped. A slot of
+ *   P * ps or more is dropped as well and sets TRIDENT_DEVERR_SLOT. Slots >= 0 in one call must be
+ *   distinct. A position outside [0, 2^24) skips its token (q_out too) and sets TRIDENT_DEVERR_POS.
+ * TRIDENT_OP_ROPE_PAGED_KV_INTERLEAVED: the same with pairs (2i, 2i+1).
+ * TRIDENT_OP_QKNORM_ROPE_PAGED_KV, TRIDENT_OP_QKNORM_ROPE_PAGED_KV_INTERLEAVED (11 tensors):
+ *   9 gamma_q [D] fp32, 10 gamma_k [D] fp32; heads are RMS-normalised first as in QKNORM_ROPE_KV.
+ *
+ * TRIDENT_OP_PAGED_ATTN (9 tensors; act = bf16 | fp16; scalar = the scale of the scores, > 0)
+ *   0 q [T,Hq,D] act  1 k_cache [P,Hkv,ps,D] act  2 v_cache [P,Hkv,ps,D] act
+ *   3 block_table [B,M] i32  4 cu_q [B+1] i32  5 kv_len [B] i32
+ *   6 work [W] fp32 (in/out; trident_scm_workspace)  7 out [T,Hq,D] act (out)  8 lse [T,Hq] fp32 (out)
+ *   Request b owns the rows cu_q[b] .. cu_q[b+1]-1 of q, its last tokens: row i of n sees the keys
+ *   j <= kv_len - n + i (a chunk of new tokens after what is cached; one row: a decode step). Head h
+ *   reads kv head h / (Hq / Hkv). s_j = scalar * (q . k_j); out = round(sum_j softmax(s)_j v_j);
+ *   lse = log(sum_j exp(s_j)). A row that sees no key gets out 0 and lse -inf, and so do the rows
+ *   from cu_q[B] on. Cache rows from kv_len on are never used (they may hold NaN); keys below kv_len
+ *   have to be finite. Sums and the softmax's statistics are fp32; its numerators are rounded to act
+ *   for the product with v.
+ *   work: zeros before its first use, left ready for the next call; calls that may overlap on the
+ *   GPU need a workspace each. cu_q that is not ascending from 0 within [0,T], a kv_len outside
+ *   [0, M * ps] or a page number outside [0,P) (read as page 0) sets TRIDENT_DEVERR_TABLE; the
+ *   outputs of such a request are unspecified.
  */
 typedef enum trident_op {
   TRIDENT_OP_ADD_RMSNORM = 1,
@@ -130,11 +181,30 @@ typedef enum trident_op {
   TRIDENT_OP_SILU = 8,
   TRIDENT_OP_ADD = 9,
   TRIDENT_OP_NEG = 10,
-  TRIDENT_OP_MASKED_FILL = 11
+  TRIDENT_OP_MASKED_FILL = 11,
+  /* 12 .. 15 are not assigned */
+  TRIDENT_OP_PAGE_MAP = 16,
+  TRIDENT_OP_ROPE_PAGED_KV = 17,
+  TRIDENT_OP_ROPE_PAGED_KV_INTERLEAVED = 18,
+  TRIDENT_OP_QKNORM_ROPE_PAGED_KV = 19,
+  TRIDENT_OP_QKNORM_ROPE_PAGED_KV_INTERLEAVED = 20,
+  TRIDENT_OP_PAGED_ATTN = 21
 } trident_op;
 
+/* How trident_rope_freqs rescales the frequencies f_i = theta^(-2i/R) for contexts longer than
+ * the model was trained on (the paper has no counterpart). */
+typedef enum trident_rope_scaling {
+  TRIDENT_ROPE_PLAIN = 0,   /* f_i                                                          */
+  TRIDENT_ROPE_LINEAR = 1,  /* f_i / factor (positions interpolated)                        */
+  TRIDENT_ROPE_BASE = 2,    /* theta * factor^(R / (R - 2)) in the place of theta: the highest
+                               frequency stays, the lowest is divided by factor (R > 2)     */
+  TRIDENT_ROPE_PARTS = 3    /* by the turns n_i = context * f_i / (2 pi) that pair i makes over
+                               the trained context: k_i = clamp((n_i - slow) / (fast - slow),
+                               0, 1), f_i * (k_i + (1 - k_i) / factor)                      */
+} trident_rope_scaling;
+
 /* Layout class of an argument tuple (guard field, §2.2.1 "shape-related metadata").
- * Over the op's activation tensors (not gamma, pos or the caches):
+ * Over the op's activation tensors (not gamma, pos or the caches; PAGE_MAP: the block table):
  *   every tensor needs unit element stride and packed inner dims, else the tuple has
  *   no layout class and matches no version;
  *   CONTIG      every tensor's row stride equals its row width (a tensor with one row
@@ -159,6 +229,9 @@ typedef enum trident_variant {
 #define TRIDENT_DEVERR_POS 0x1u   /* a RoPE/KV position was outside [0, S) */
 #define TRIDENT_DEVERR_TIMEOUT 0x2u /* a kernel's bounded wait for its own bulk copies ran
                                        out; that block's outputs were not written */
+#define TRIDENT_DEVERR_SLOT 0x4u  /* ROPE_PAGED_KV: a slot was outside the cache */
+#define TRIDENT_DEVERR_PAGES 0x8u /* PAGE_MAP: the call's lengths do not fit (pages, table, rows) */
+#define TRIDENT_DEVERR_TABLE 0x10u /* a page number, cu_q or kv_len out of range */
 
 /* Option flags of trident_scm_create. */
 #define TRIDENT_OPT_DRY_RUN 0x1        /* no CUDA at all: invoke selects and calls the hook,
@@ -205,18 +278,21 @@ typedef struct trident_args {
 /* Descriptor of one version (specialisation). register_spec copies it. */
 typedef struct trident_spec_desc {
   int32_t op;                       /* trident_op                                        */
-  int32_t dtype;                    /* activation dtype                                  */
+  int32_t dtype;                    /* activation dtype (PAGE_MAP: TRIDENT_I32)           */
   int32_t rank;                     /* rank of slot 0 (2 or 3 for the norms, SWIGLU and
                                        the pointwise ops,
-                                       3 for ROPE ops, 2 for the chains)                  */
+                                       3 for ROPE ops and PAGED_ATTN, 2 for the chains,
+                                       1 for PAGE_MAP)                                    */
   int32_t layout;                   /* trident_layout                                    */
   int64_t fixed[TRIDENT_MAX_FIXED]; /* fixed sizes: ADD_RMSNORM, RMSNORM {H}; SWIGLU {I};
                                        SILU, ADD, NEG, MASKED_FILL {W};
                                        ROPE ops {Hq, Hkv, D, S};
-                                       chains {H, Hq, Hkv, D, S, I}; unused entries 0    */
+                                       chains {H, Hq, Hkv, D, S, I};
+                                       paged ROPE ops {Hq, Hkv, D, R, ps};
+                                       PAGED_ATTN {Hq, Hkv, D, ps}; unused entries 0      */
   int64_t tok_lo, tok_hi;           /* inclusive token-count bucket, 1 <= lo <= hi       */
   int32_t align_bytes;              /* 16: every pointer and every outer stride 16-byte
-                                       aligned (positions excepted: read per element);
+                                       aligned (i32 tensors excepted: read per element);
                                        or the element size (no extra requirement)        */
   int32_t device;                   /* CUDA ordinal; must equal the SCM's device         */
   int32_t variant;                  /* trident_variant                                   */
@@ -444,6 +520,22 @@ int32_t trident_scm_invoke_tree(trident_scm_t* scm, const trident_node* nodes, i
  * invoke hook (§3.5: the caller's compile path runs only on a miss, never from inside a
  * hook). Errors: ERR_INVALID (scm NULL). */
 int32_t trident_scm_set_tree_hook(trident_scm_t* scm, trident_tree_hook hook, void* user);
+
+/* Elements of the workspace (slot `work`) that calls of PAGED_ATTN version `index` need, from
+ * the version's sizes and the device's SM count (calls of any length and number of requests fit).
+ * What a launch needs is fixed when the specialisation is built (§3.3), and a hit allocates
+ * nothing, so the caller holds the workspace.
+ * 0 for versions of ops without a workspace. Errors: ERR_INVALID (scm or out NULL, no such
+ * version), ERR_STATE (dry-run SCM: the device is unknown). */
+int32_t trident_scm_workspace(const trident_scm_t* scm, int32_t index, int64_t* out);
+
+/* Fills out[0 .. R-1] with the R/2 pairs (hi, lo) of ROPE_PAGED_KV's freqs tensor: frequencies in
+ * fp64, hi = fp32(f), lo = fp32(f - hi). Where ROPE_KV's base is a specialised constant (§3.3), the
+ * paged ops take the finished table as a tensor. A host function; needs no GPU. R even, in [2, 1024];
+ * theta > 0; factor >= 1 and, for PARTS, context > 0 and 0 <= slow < fast (others: not used).
+ * Errors: ERR_INVALID. */
+int32_t trident_rope_freqs(double theta, int32_t R, int32_t scaling, double factor, double context,
+                           double slow, double fast, float* out);
 
 /* Selection only: validation plus Algorithm 1's guard loop, with no launch, no hook
  * and no statistics. Returns OK (*out_selected = index), MISS (-1) or ERR_INVALID.

@@ -1,0 +1,116 @@
+// attn.cu -- attention of each request's last rows over its cache pages.
+//
+// Row i of request b's n rows stands at position kv - n + i and sees the keys up to there:
+//   s_j = scale * q . k_j,  m = max s_j,  l = sum exp(s_j - m),  out = sum exp(s_j - m) v_j / l,
+//   lse = m + log l.
+// Scores are kept in units of log 2 (scale * log2(e) folded in), so that each exponential is one exp2.
+#include "device_common.cuh"
+
+namespace trident {
+namespace {
+
+constexpr uint32_t kErrTable = 0x10u;  // TRIDENT_DEVERR_TABLE
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// Request b's rows [q0, q0 + n) and keys; lengths out of range give none and set *ok = false.
+struct Request { int32_t q0, n, kv; };
+__device__ __forceinline__ Request request(const PagedAttnParams& p, int64_t b, bool* ok) {
+  const int32_t c0 = p.cu[b], c1 = p.cu[b + 1], kv = p.kv[b];
+  const int64_t most = p.M * p.page.d;
+  Request r{c0, c1 - c0, kv};
+  if (c0 < 0 || c1 < c0 || c1 > p.T || (b == 0 && c0 != 0)) {
+    *ok = false;
+    r.q0 = r.n = 0;
+  }
+  if (kv < 0 || kv > most) {
+    *ok = false;
+    r.kv = kv < 0 ? 0 : (int32_t)most;
+  }
+  return r;
+}
+
+// Any alignment and head size up to 512: one warp per (row, head), a key per lane for the scores, then
+// the lanes split D for the product with v.
+template <int DT>
+__global__ void __launch_bounds__(kThreads) attn_generic_kernel(const PagedAttnParams p) {
+  pdl_prologue();
+  const int lane = threadIdx.x & 31;
+  const int64_t unit = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / 32;
+  if (unit >= p.T * p.Hq) return;
+  const int64_t t = unit / p.Hq;
+  const int h = (int)(unit - t * p.Hq), hk = (int)fast_div((uint32_t)h, p.group.magic, p.group.shift);
+  // the request of row t: the last one that starts at or before it
+  int64_t lo = 0, hi = p.B;
+  while (hi - lo > 1) {
+    const int64_t mid = (lo + hi) / 2;
+    if (p.cu[mid] <= t) lo = mid;
+    else hi = mid;
+  }
+  bool ok = p.B > 0;
+  Request r{0, 0, 0};
+  if (ok) r = request(p, lo, &ok);
+  if (unit == 0)  // one warp looks every request's numbers over
+    for (int64_t b = lane; b < p.B; b += 32) request(p, b, &ok);
+  const bool mine = t >= r.q0 && t < r.q0 + r.n;
+  const int64_t seen = mine ? max((int64_t)0, min((int64_t)r.kv, r.kv - r.n + (t - r.q0) + 1)) : 0;
+  const char* q = row_ptr(p.q, t, p.q_rs, 2) + (int64_t)h * p.D * 2;
+  float m = -INFINITY, l = 0.f, acc[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+  for (int64_t j0 = 0; j0 < seen; j0 += 32) {
+    const int64_t j = j0 + lane;
+    float s = -INFINITY;
+    int64_t vat = 0;
+    if (j < seen) {
+      const uint32_t pg = fast_div((uint32_t)j, p.page.magic, p.page.shift);
+      const int64_t at = (uint32_t)j - pg * (uint32_t)p.page.d;
+      int64_t page = p.table[lo * p.table_rs + pg];
+      if (page < 0 || page >= p.P) {
+        ok = false;
+        page = 0;
+      }
+      const int64_t kat = page * p.kc.page + hk * p.kc.head + at * p.kc.row;
+      vat = page * p.vc.page + hk * p.vc.head + at * p.vc.row;
+      float d = 0.f;
+      for (int e = 0; e < p.D; ++e) d = fmaf(load_elem<DT>(q, e), load_elem<DT>(p.kc.base, kat + e), d);
+      s = d * (p.scale * kLog2e);
+    }
+    float top = s;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float m2 = fmaxf(m, top), old = exp2f(m - m2);  // the first key of a chunk is always seen
+    const float e = exp2f(s - m2);
+    l = l * old + warp_sum(e);
+    m = m2;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) acc[x] *= old;
+    const int n = (int)min((int64_t)32, seen - j0);
+    for (int k = 0; k < n; ++k) {
+      const float pk = __shfl_sync(0xffffffffu, e, k);
+      const int64_t at = __shfl_sync(0xffffffffu, vat, k);
+#pragma unroll
+      for (int x = 0; x < 16; ++x)
+        if (lane + 32 * x < p.D) acc[x] = fmaf(pk, load_elem<DT>(p.vc.base, at + lane + 32 * x), acc[x]);
+    }
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  char* out = row_ptr(p.out, t, p.o_rs, 2) + (int64_t)h * p.D * 2;
+#pragma unroll
+  for (int x = 0; x < 16; ++x)
+    if (lane + 32 * x < p.D) store_elem<DT>(out, lane + 32 * x, acc[x] * inv);
+  if (lane == 0) p.lse[t * p.Hq + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+  if (!ok) atomicOr(p.err, kErrTable);
+}
+
+}  // namespace
+
+bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, KernelEntry* out, const char** why) {
+  if (dtype != DT_BF16 && dtype != DT_FP16) { *why = "paged attention supports bf16 and fp16"; return false; }
+  if (variant != 1) { *why = "no vector kernel"; return false; }
+  out->kind = KK_PAGED_ATTN;
+  out->vec = 1;
+  out->fn = dtype == DT_BF16 ? (const void*)attn_generic_kernel<DT_BF16> : (const void*)attn_generic_kernel<DT_FP16>;
+  return true;
+}
+
+}  // namespace trident

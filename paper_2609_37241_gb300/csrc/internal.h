@@ -151,6 +151,76 @@ struct ChainStepParams {
   ChainParams c[kStepMax];
 };
 
+// n / d and n mod d by fast_div, for a divisor known per launch.
+struct FastDiv {
+  uint32_t magic;
+  int32_t shift;
+  int32_t d;
+};
+
+// PAGE_MAP: page numbers, positions and slots of a batch's new tokens from its lengths.
+struct PageMapParams {
+  const int32_t* ctx;
+  const int32_t* fresh;  // new tokens per request
+  const int32_t* free_pages;
+  const int32_t* free_head;
+  int32_t* table;
+  int32_t* cu;
+  int32_t* kv;
+  int32_t* pos;
+  int32_t* slot;
+  int32_t* head_out;
+  uint32_t* err;
+  int64_t B, N, F, M, table_rs;
+  FastDiv page;
+};
+
+// A paged cache: strides in elements, rows of D packed elements.
+struct PagedCache {
+  void* base;
+  int64_t page, head, row;
+};
+
+// Partial, rescaled and interleaved RoPE with the append to a paged cache.
+struct RopePagedParams {
+  const void* q;
+  const void* k;
+  const void* v;
+  const int32_t* pos;
+  const int32_t* slot;
+  const float2* freqs;
+  void* q_out;
+  PagedCache kc, vc;
+  const float* gamma_q;
+  const float* gamma_k;
+  uint32_t* err;
+  int64_t T, slots;  // slots: P * ps
+  int64_t q_rs, k_rs, v_rs, o_rs;
+  int32_t Hq, Hkv, D, R, NH;
+  float eps, inv_D, mag;
+  FastDiv page;
+  int32_t ipt, rpi;  // warp items per token, head-rows per item (RopeSplit)
+  uint32_t ipt_magic;
+  int32_t ipt_shift;
+};
+
+// Attention of each request's last rows over its pages.
+struct PagedAttnParams {
+  const void* q;
+  PagedCache kc, vc;  // read only
+  const int32_t* table;
+  const int32_t* cu;
+  const int32_t* kv;
+  float* work;
+  void* out;
+  float* lse;
+  uint32_t* err;
+  int64_t T, B, M, P, table_rs, q_rs, o_rs;
+  int32_t Hq, Hkv, G, D;
+  float scale;
+  FastDiv page, group;  // by ps; by G = Hq / Hkv
+};
+
 // Elementwise entries (pointwise_plan): flat and rows kernels with one or two vectors per
 // thread, and the generic kernel.
 enum PointwiseEntry : int32_t { PW_FLAT, PW_FLAT2, PW_ROWS, PW_ROWS2, PW_GENERIC, kPwEntries };
@@ -203,8 +273,15 @@ enum KernelKind : int32_t {
   KK_ROPE_PAIR = 2,     // vector: grid by rope_plan
   KK_ROPE_WARP = 3,     // generic: one warp per head-row
   KK_POINTWISE = 4,     // flat, rows or generic entry by the call's layout (pw_fn)
-  KK_CHAIN = 6
+  KK_CHAIN = 6,
+  KK_PAGE_MAP = 7,
+  KK_ROPE_PAGED = 8,   // vector: any_fn by rope_paged_plan; generic (vec 1): one warp per head-row
+  KK_PAGED_ATTN = 9
 };
+
+constexpr int kMapThreads = 256;  // PAGE_MAP: block size
+constexpr int kMapTokens = 1024;  // ... and tokens per block
+constexpr int64_t kPosLimit = 1 << 24;  // paged RoPE: positions are exact in fp32
 
 // Lookup of compiled kernels. Return false (with a reason) if no kernel fits.
 bool norm_kernel(bool res, int32_t dtype, int32_t variant, int64_t H, KernelEntry* out, const char** why);
@@ -261,6 +338,12 @@ struct ChainPlan {
 ChainPlan chain_plan(int64_t T, int64_t I, const RopeSplit* rope, int32_t threads, int32_t vec, int64_t wave, int32_t sms,
                      bool inplace, bool qk, bool pdl);
 int32_t chain_rope_k(int64_t one, int64_t wave, bool qk);
+const void* page_map_entry();
+bool rope_paged_kernel(int32_t dtype, int32_t variant, int32_t D, int32_t R, bool qknorm, bool inter,
+                       KernelEntry* out, const char** why);
+// Which any_fn entry a vector call takes; sets its item split, block size and grid.
+int rope_paged_plan(RopePagedParams* p, int32_t* threads, int64_t* blocks, int32_t sms);
+bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, KernelEntry* out, const char** why);
 const void* empty_kernel_entry();  // the latency-floor probe's kernel (does nothing)
 
 // Validation, guard-equivalent checks (sizes, layouts, 16-byte alignment, overlap) and

@@ -110,7 +110,10 @@ bool driver() {
 
 // ------------------------------------------------------------------ op tables
 enum Kind : uint8_t { K_ACT_H, K_ACT_I, K_GAMMA_H, K_GAMMA_D, K_HEADS_Q, K_HEADS_KV, K_POS, K_CACHE,
-                     K_MASK_H };
+                     K_MASK_H,
+                     // paged ops: i32 vectors [B], [B+1], [1], of any length and [B,M]; a paged cache, the
+                     // frequency table, per-row statistics and the workspace
+                     K_REQ, K_CU, K_ONE, K_LIST, K_TABLE, K_PAGED, K_FREQ, K_LSE, K_WORK };
 
 struct OpInfo {
   int32_t nslots;
@@ -122,7 +125,7 @@ struct OpInfo {
   uint8_t group[TRIDENT_MAX_TENSORS];  // in-place group id (0: none)
 };
 
-constexpr int kMaxOp = 11;
+constexpr int kMaxOp = TRIDENT_OP_PAGED_ATTN;  // ops without slots are not assigned
 OpInfo g_ops[kMaxOp + 1];
 
 // slot index constants of the chains
@@ -174,8 +177,29 @@ struct OpInit {
     o.kind[18] = o.kind[19] = K_GAMMA_D;
     o.out[18] = o.out[19] = false;
     o.group[18] = o.group[19] = 0;
+    set(TRIDENT_OP_PAGE_MAP, 0, false, false,
+        {{K_REQ, false, 0}, {K_REQ, false, 0}, {K_LIST, false, 0}, {K_ONE, false, 0}, {K_TABLE, true, 0},
+         {K_CU, true, 0}, {K_REQ, true, 0}, {K_LIST, true, 0}, {K_LIST, true, 0}, {K_ONE, true, 0}});
+    const std::initializer_list<std::tuple<Kind, bool, int>> rope_paged = {
+        {K_HEADS_Q, false, 1}, {K_HEADS_KV, false, 0}, {K_HEADS_KV, false, 0}, {K_POS, false, 0}, {K_POS, false, 0},
+        {K_FREQ, false, 0}, {K_HEADS_Q, true, 1}, {K_PAGED, true, 0}, {K_PAGED, true, 0}};
+    for (int op : {TRIDENT_OP_ROPE_PAGED_KV, TRIDENT_OP_ROPE_PAGED_KV_INTERLEAVED, TRIDENT_OP_QKNORM_ROPE_PAGED_KV,
+                   TRIDENT_OP_QKNORM_ROPE_PAGED_KV_INTERLEAVED}) {
+      set(op, 5, false, false, rope_paged);
+      if (op < TRIDENT_OP_QKNORM_ROPE_PAGED_KV) continue;
+      g_ops[op].nslots = 11;
+      g_ops[op].kind[9] = g_ops[op].kind[10] = K_GAMMA_D;
+    }
+    set(TRIDENT_OP_PAGED_ATTN, 4, false, false,
+        {{K_HEADS_Q, false, 0}, {K_PAGED, false, 0}, {K_PAGED, false, 0}, {K_TABLE, false, 0}, {K_CU, false, 0},
+         {K_REQ, false, 0}, {K_WORK, true, 0}, {K_HEADS_Q, true, 0}, {K_LSE, true, 0}});
   }
 } g_op_init;
+
+inline bool is_paged_op(int32_t op) { return op >= TRIDENT_OP_PAGE_MAP; }
+inline bool is_rope_paged(int32_t op) {
+  return op >= TRIDENT_OP_ROPE_PAGED_KV && op <= TRIDENT_OP_QKNORM_ROPE_PAGED_KV_INTERLEAVED;
+}
 
 inline int elem_size(int32_t dt) {
   switch (dt) {
@@ -208,7 +232,14 @@ inline Rows rows_of(const trident_tensor& t, Kind k) {
     if (sh[0] == 1) return {sh[1], sh[2], st[1], inner};
     return {sh[0] * sh[1], sh[2], st[1], inner && st[0] == sh[1] * st[1]};
   }
-  // gamma, pos, cache: one dense row
+  if (k == K_TABLE) return {sh[0], sh[1], st[0], sh[1] <= 1 || st[1] == 1};
+  if (k == K_PAGED) {  // a row per page, from its first element to its last
+    if (sh[0] == 0 || sh[1] == 0 || sh[2] == 0 || sh[3] == 0) return {0, 0, 0, true};
+    const int64_t w = 1 + (sh[1] - 1) * st[1] + (sh[2] - 1) * st[2] + (sh[3] - 1) * st[3];
+    if (sh[0] == 1 || st[0] >= w) return {sh[0], w, st[0], true};
+    return {1, w + (sh[0] - 1) * st[0], 0, true};  // pages inside each other's span: one extent
+  }
+  // gamma, pos, cache and the other paged kinds: one dense row
   int64_t n = 1;
   for (int d = 0; d < t.ndim; ++d) n *= sh[d];
   return {1, n, n, true};
@@ -238,6 +269,151 @@ inline bool shape_is(const trident_tensor& t, std::initializer_list<int64_t> wan
   return true;
 }
 
+// What makes any tensor malformed.
+inline int32_t check_tensor(const trident_tensor& x, int i, int es) {
+  if (es == 0) return fail(TRIDENT_ERR_INVALID, "tensor %d: unknown dtype %d", i, x.dtype);
+  if (x.ndim < 1 || x.ndim > 4) return fail(TRIDENT_ERR_INVALID, "tensor %d: ndim %d", i, x.ndim);
+  if (x.device < -1) return fail(TRIDENT_ERR_INVALID, "tensor %d: device %d", i, x.device);
+  bool empty = false;
+  for (int d = 0; d < x.ndim; ++d) {
+    if (x.shape[d] < 0 || x.stride[d] < 0)
+      return fail(TRIDENT_ERR_INVALID, "tensor %d: negative shape or stride", i);
+    if (x.shape[d] == 0) empty = true;
+  }
+  const uintptr_t ptr = reinterpret_cast<uintptr_t>(x.data);
+  if (!ptr && !empty) return fail(TRIDENT_ERR_INVALID, "tensor %d: NULL data", i);
+  if (ptr % (uintptr_t)es != 0) return fail(TRIDENT_ERR_INVALID, "tensor %d: not element-aligned", i);
+  return TRIDENT_OK;
+}
+
+// Does every element of a paged cache have bytes of its own? Dimensions by stride, each past the
+// span of those before it.
+inline bool paged_layout_ok(const trident_tensor& x) {
+  if (x.shape[3] > 1 && x.stride[3] != 1) return false;
+  int d[3] = {0, 1, 2};
+  std::sort(d, d + 3, [&](int a, int b) { return x.stride[a] < x.stride[b]; });
+  int64_t span = x.shape[3];
+  for (int k : d) {
+    if (x.shape[k] <= 1) continue;
+    if (x.stride[k] < span) return false;
+    span += (x.shape[k] - 1) * x.stride[k];
+  }
+  return true;
+}
+
+// analyze() for the paged ops: the same two passes over their kinds of tensors.
+int32_t analyze_paged(const trident_args* a, const OpInfo& oi, Sig* s) {
+  const trident_tensor* t = a->t;
+  const int op = a->op, n = oi.nslots;
+  if (op == TRIDENT_OP_PAGE_MAP) {
+    if (!(a->scalar >= 1.0 && a->scalar <= 65536.0 && a->scalar == std::floor(a->scalar)))
+      return fail(TRIDENT_ERR_INVALID, "scalar (the page size) must be a whole number in [1, 65536]");
+  } else if (!(a->scalar > 0.0 && std::isfinite((float)a->scalar) && (float)a->scalar > 0.0f)) {
+    return fail(TRIDENT_ERR_INVALID, "scalar (%s) must be positive and finite",
+                op == TRIDENT_OP_PAGED_ATTN ? "the scale of the scores" : "the magnitude of cos and sin");
+  }
+  s->device = t[0].device;
+  s->act_dtype = -1;
+  s->aux_dtype_ok = s->ranks_ok = s->aligned16 = true;
+  s->rank = t[0].ndim;
+  for (int i = 0; i < n; ++i) {
+    const trident_tensor& x = t[i];
+    const int es = elem_size(x.dtype);
+    const int32_t st = check_tensor(x, i, es);
+    if (st != TRIDENT_OK) return st;
+    if (x.device != t[0].device) s->device = kMixed;
+    const Kind k = oi.kind[i];
+    int want = 1;
+    bool whole = false;  // i32, read one element at a time
+    switch (k) {
+      case K_HEADS_Q: case K_HEADS_KV: want = 3; break;
+      case K_PAGED: want = 4; break;
+      case K_TABLE: want = 2; whole = true; break;
+      case K_FREQ: case K_LSE: want = 2; break;
+      case K_GAMMA_D: case K_WORK: break;
+      default: whole = true; break;
+    }
+    s->ranks_ok &= x.ndim == want;
+    if (is_act(k) || k == K_PAGED || (whole && op == TRIDENT_OP_PAGE_MAP)) {
+      if (s->act_dtype == -1) s->act_dtype = x.dtype;
+      else if (s->act_dtype != x.dtype) s->act_dtype = kMixed;
+    } else {
+      s->aux_dtype_ok &= x.dtype == (whole ? TRIDENT_I32 : TRIDENT_FP32);
+    }
+    if (!whole && s->aligned16) {
+      if (reinterpret_cast<uintptr_t>(x.data) % 16 != 0) s->aligned16 = false;
+      if (k != K_FREQ && k != K_LSE)  // dense where they match
+        for (int d = 0; d + 1 < x.ndim; ++d)
+          if (x.shape[d] > 1 && (x.stride[d] * es) % 16 != 0) s->aligned16 = false;
+    }
+  }
+  s->shapes_ok = s->aux_layout_ok = false;
+  s->layout = -1;
+  for (int i = 0; i < TRIDENT_MAX_FIXED; ++i) s->fixed[i] = -1;
+  s->T = -1;
+  if (!s->ranks_ok) return TRIDENT_OK;
+  s->nlead = 1;
+  s->T = s->lead[0] = t[0].shape[0];
+  int64_t B = s->T, M = 0, Hq = 0, Hkv = 0, D = 0, P = 0, ps = 0;
+  bool shapes = true;
+  if (op == TRIDENT_OP_PAGE_MAP) {
+    M = t[4].shape[1];
+    shapes &= t[7].shape[0] == t[8].shape[0];
+  } else {
+    const trident_tensor& c = t[op == TRIDENT_OP_PAGED_ATTN ? 1 : 7];
+    Hq = t[0].shape[1];
+    D = t[0].shape[2];
+    P = c.shape[0]; Hkv = c.shape[1]; ps = c.shape[2];
+    s->fixed[0] = Hq; s->fixed[1] = Hkv; s->fixed[2] = D;
+    shapes &= P >= 1;
+    if (op == TRIDENT_OP_PAGED_ATTN) {
+      B = t[3].shape[0];
+      M = t[3].shape[1];
+      s->fixed[3] = ps;
+    } else {
+      s->fixed[3] = 2 * t[5].shape[0];
+      s->fixed[4] = ps;
+    }
+  }
+  bool all_contig = true, none = false, aux = true;
+  for (int i = 0; i < n; ++i) {
+    const trident_tensor& x = t[i];
+    const Kind k = oi.kind[i];
+    bool row = false, dense = true;
+    switch (k) {
+      case K_HEADS_Q: shapes &= shape_is(x, {s->T, Hq, D}); row = true; break;
+      case K_HEADS_KV: shapes &= shape_is(x, {s->T, Hkv, D}); row = true; break;
+      case K_PAGED: shapes &= shape_is(x, {P, Hkv, ps, D}); dense = paged_layout_ok(x); break;
+      case K_TABLE: shapes &= shape_is(x, {B, M}); row = true; break;
+      case K_POS: shapes &= shape_is(x, {s->T}); break;
+      case K_REQ: shapes &= shape_is(x, {B}); break;
+      case K_CU: shapes &= shape_is(x, {B + 1}); break;
+      case K_ONE: shapes &= shape_is(x, {1}); break;
+      case K_GAMMA_D: shapes &= shape_is(x, {D}); break;
+      case K_FREQ: shapes &= x.shape[1] == 2; break;
+      case K_LSE: shapes &= shape_is(x, {s->T, Hq}); break;
+      default: break;  // K_LIST, K_WORK: any length
+    }
+    if (row) {
+      const Rows r = rows_of(x, k);
+      if (!r.packed) none = true;
+      else if (r.n > 1) {
+        if (r.stride < r.width) none = true;
+        else if (r.stride != r.width) all_contig = false;
+      }
+    } else if (x.ndim == 1) {
+      dense = x.shape[0] <= 1 || x.stride[0] == 1;
+    } else if (x.ndim == 2) {
+      dense = (x.shape[1] <= 1 || x.stride[1] == 1) && (x.shape[0] <= 1 || x.stride[0] == x.shape[1]);
+    }
+    aux &= dense;
+  }
+  s->shapes_ok = shapes;
+  s->layout = none ? -1 : (all_contig ? TRIDENT_LAYOUT_CONTIG : TRIDENT_LAYOUT_ROWSTRIDED);
+  s->aux_layout_ok = aux;
+  return TRIDENT_OK;
+}
+
 // Structural validation -- everything that makes a call malformed rather than a miss --
 // fused with the per-tensor guarded properties (common device, dtypes, ranks, 16-byte
 // alignment) in one pass over the tensors; a second pass checks shapes and layouts against
@@ -246,10 +422,13 @@ int32_t analyze(const trident_args* a, const OpInfo** info, Sig* s) {
   if (!a) return fail(TRIDENT_ERR_INVALID, "args is NULL");
   if (a->op < 1 || a->op > kMaxOp) return fail(TRIDENT_ERR_INVALID, "unknown op %d", a->op);
   const OpInfo& oi = g_ops[a->op];
+  if (oi.nslots == 0) return fail(TRIDENT_ERR_INVALID, "unknown op %d", a->op);
   if (a->ntensors != oi.nslots)
     return fail(TRIDENT_ERR_INVALID, "op %d takes %d tensors, got %d", a->op, oi.nslots, a->ntensors);
   if (a->flags != 0) return fail(TRIDENT_ERR_INVALID, "args.flags must be 0");
   if (!(a->eps >= 0.0)) return fail(TRIDENT_ERR_INVALID, "eps must be >= 0");
+  *info = &oi;
+  if (is_paged_op(a->op)) return analyze_paged(a, oi, s);
   const trident_tensor* t = a->t;
   const int n = oi.nslots;
   s->device = t[0].device;
@@ -262,18 +441,9 @@ int32_t analyze(const trident_args* a, const OpInfo** info, Sig* s) {
   for (int i = 0; i < n; ++i) {  // pass 1: validation and per-tensor properties
     const trident_tensor& x = t[i];
     const int es = elem_size(x.dtype);
-    if (es == 0) return fail(TRIDENT_ERR_INVALID, "tensor %d: unknown dtype %d", i, x.dtype);
-    if (x.ndim < 1 || x.ndim > 4) return fail(TRIDENT_ERR_INVALID, "tensor %d: ndim %d", i, x.ndim);
-    if (x.device < -1) return fail(TRIDENT_ERR_INVALID, "tensor %d: device %d", i, x.device);
-    bool empty = false;
-    for (int d = 0; d < x.ndim; ++d) {
-      if (x.shape[d] < 0 || x.stride[d] < 0)
-        return fail(TRIDENT_ERR_INVALID, "tensor %d: negative shape or stride", i);
-      if (x.shape[d] == 0) empty = true;
-    }
+    const int32_t bad = check_tensor(x, i, es);
+    if (bad != TRIDENT_OK) return bad;
     const uintptr_t ptr = reinterpret_cast<uintptr_t>(x.data);
-    if (!ptr && !empty) return fail(TRIDENT_ERR_INVALID, "tensor %d: NULL data", i);
-    if (ptr % (uintptr_t)es != 0) return fail(TRIDENT_ERR_INVALID, "tensor %d: not element-aligned", i);
     if (x.device != t[0].device) s->device = kMixed;
     const Kind k = oi.kind[i];
     if (is_act(k) || k == K_CACHE) {
@@ -297,7 +467,6 @@ int32_t analyze(const trident_args* a, const OpInfo** info, Sig* s) {
         if (x.shape[d] > 1 && (x.stride[d] * es) % 16 != 0) s->aligned16 = false;
     }
   }
-  *info = &oi;
   s->shapes_ok = false;
   s->layout = -1;
   s->aux_layout_ok = false;
@@ -357,6 +526,7 @@ int32_t analyze(const trident_args* a, const OpInfo** info, Sig* s) {
       case K_HEADS_KV: shapes &= shape_is(x, {T0, Hkv, D}); break;
       case K_POS: shapes &= shape_is(x, {T0}); break;
       case K_CACHE: shapes &= shape_is(x, {Hkv, S, D}); break;
+      default: break;  // the paged ops' kinds
     }
     if (is_rowlike(k)) {
       const Rows r = rows_of(x, k);
@@ -763,9 +933,113 @@ inline int32_t chain_prefetch_mode(bool pdl, bool small_grid, bool norm_rows) {
 
 inline unsigned cap_grid(int64_t n) { return (unsigned)(n < 1 ? 1 : (n > 0x7fffffff ? 0x7fffffff : n)); }
 
+inline FastDiv fast_divisor(int64_t d) {
+  FastDiv f;
+  f.d = (int32_t)d;
+  div_magic((uint32_t)d, &f.magic, &f.shift);
+  return f;
+}
+
+inline PagedCache paged_cache(const trident_tensor& t) { return {t.data, t.stride[0], t.stride[1], t.stride[2]}; }
+
+void pack_page_map(const trident_args* a, const Sig& s, uint32_t* err, PageMapParams* p) {
+  const trident_tensor* t = a->t;
+  p->ctx = (const int32_t*)t[0].data; p->fresh = (const int32_t*)t[1].data;
+  p->free_pages = (const int32_t*)t[2].data; p->free_head = (const int32_t*)t[3].data;
+  p->table = (int32_t*)t[4].data; p->cu = (int32_t*)t[5].data; p->kv = (int32_t*)t[6].data;
+  p->pos = (int32_t*)t[7].data; p->slot = (int32_t*)t[8].data; p->head_out = (int32_t*)t[9].data;
+  p->err = err;
+  p->B = s.T; p->N = t[7].shape[0]; p->F = t[2].shape[0]; p->M = t[4].shape[1];
+  p->table_rs = t[4].stride[0];
+  p->page = fast_divisor((int64_t)a->scalar);
+}
+
+void pack_rope_paged(const trident_args* a, uint32_t* err, RopePagedParams* p) {
+  const trident_tensor* t = a->t;
+  const bool qk = a->op >= TRIDENT_OP_QKNORM_ROPE_PAGED_KV;
+  p->q = t[0].data; p->k = t[1].data; p->v = t[2].data;
+  p->pos = (const int32_t*)t[3].data; p->slot = (const int32_t*)t[4].data;
+  p->freqs = (const float2*)t[5].data;
+  p->q_out = t[6].data;
+  p->kc = paged_cache(t[7]); p->vc = paged_cache(t[8]);
+  p->gamma_q = qk ? (const float*)t[9].data : nullptr;
+  p->gamma_k = qk ? (const float*)t[10].data : nullptr;
+  p->err = err;
+  p->T = t[0].shape[0];
+  p->slots = t[7].shape[0] * t[7].shape[2];
+  p->q_rs = t[0].stride[0]; p->k_rs = t[1].stride[0]; p->v_rs = t[2].stride[0]; p->o_rs = t[6].stride[0];
+  p->Hq = (int32_t)t[0].shape[1]; p->Hkv = (int32_t)t[1].shape[1];
+  p->D = (int32_t)t[0].shape[2]; p->R = (int32_t)(2 * t[5].shape[0]);
+  p->NH = p->Hq + 2 * p->Hkv;
+  p->eps = (float)a->eps;
+  p->inv_D = (float)(1.0 / (double)p->D);
+  p->mag = (float)a->scalar;
+  p->page = fast_divisor(t[7].shape[2]);
+  p->ipt = p->rpi = 0;
+}
+
+void pack_paged_attn(const trident_args* a, const Sig& s, uint32_t* err, PagedAttnParams* p) {
+  const trident_tensor* t = a->t;
+  p->q = t[0].data;
+  p->kc = paged_cache(t[1]); p->vc = paged_cache(t[2]);
+  p->table = (const int32_t*)t[3].data; p->cu = (const int32_t*)t[4].data; p->kv = (const int32_t*)t[5].data;
+  p->work = (float*)t[6].data; p->out = t[7].data; p->lse = (float*)t[8].data;
+  p->err = err;
+  p->T = s.T; p->B = t[3].shape[0]; p->M = t[3].shape[1]; p->P = t[1].shape[0];
+  p->table_rs = t[3].stride[0]; p->q_rs = t[0].stride[0]; p->o_rs = t[7].stride[0];
+  p->Hq = (int32_t)t[0].shape[1]; p->Hkv = (int32_t)t[1].shape[1]; p->G = p->Hq / p->Hkv;
+  p->D = (int32_t)t[0].shape[2];
+  p->scale = (float)a->scalar;
+  p->page = fast_divisor(t[1].shape[2]);
+  p->group = fast_divisor(p->G);
+}
+
+// Launch of a paged op. Counts that index in 32 bits are bounded here; bytes are indexed in 64.
+int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, const Sig& s, void* stream) {
+  CUlaunchConfig cfg;
+  CUlaunchAttribute attr;
+  base_config(scm, stream, &cfg, &attr);
+  constexpr int64_t kMost = 0x7fffffff;
+  const int op = a->op;
+  if (op == TRIDENT_OP_PAGE_MAP) {
+    PageMapParams p;
+    pack_page_map(a, s, scm->d_err, &p);
+    if (p.B >= kMost || p.N >= kMost || p.F >= kMost || p.M >= kMost)
+      return fail(TRIDENT_ERR_INVALID, "page map too large for 32-bit counts");
+    cfg.blockDimX = kMapThreads;
+    cfg.gridDimX = cap_grid((p.N + kMapTokens - 1) / kMapTokens);
+    void* kp[1] = {&p};
+    return launch_on(scm, &cfg, v.fn, kp);
+  }
+  if (is_rope_paged(op)) {
+    RopePagedParams p;
+    pack_rope_paged(a, scm->d_err, &p);
+    if (s.T * p.NH >= kMost || p.slots > kMost)
+      return fail(TRIDENT_ERR_INVALID, "paged RoPE call too large for 32-bit counts");
+    int64_t blocks = (s.T * p.NH + kThreads / 32 - 1) / (kThreads / 32);
+    CUfunction fn = v.fn;
+    if (v.ke.vec > 1) {
+      int32_t threads = 0;
+      fn = v.any_fn[rope_paged_plan(&p, &threads, &blocks, scm->sm_count)];
+      cfg.blockDimX = (unsigned)threads;
+    }
+    cfg.gridDimX = cap_grid(blocks);
+    void* kp[1] = {&p};
+    return launch_on(scm, &cfg, fn, kp);
+  }
+  PagedAttnParams p;
+  pack_paged_attn(a, s, scm->d_err, &p);
+  if (s.T * p.Hq >= kMost || p.B >= kMost || p.M * (int64_t)p.page.d >= kMost || p.P > kMost)
+    return fail(TRIDENT_ERR_INVALID, "paged attention call too large for 32-bit counts");
+  void* kp[1] = {&p};
+  cfg.gridDimX = cap_grid((s.T * p.Hq + kThreads / 32 - 1) / (kThreads / 32));
+  return launch_on(scm, &cfg, v.fn, kp);
+}
+
 int32_t do_launch(trident_scm* scm, const Version& v, const trident_args* a, const Sig& s,
                   void* stream) {
   const int op = a->op;
+  if (is_paged_op(op)) return launch_paged(scm, v, a, s, stream);
   CUlaunchConfig cfg;
   CUlaunchAttribute attr;
   base_config(scm, stream, &cfg, &attr);
@@ -1083,12 +1357,15 @@ int32_t validate_desc(const trident_scm* scm, const trident_spec_desc* d, int32_
   if (!d) return fail(TRIDENT_ERR_INVALID, "descriptor is NULL");
   if (d->op < 1 || d->op > kMaxOp) return fail(TRIDENT_ERR_INVALID, "unknown op %d", d->op);
   const OpInfo& oi = g_ops[d->op];
+  if (oi.nslots == 0) return fail(TRIDENT_ERR_INVALID, "unknown op %d", d->op);
   const bool chain = d->op == TRIDENT_OP_LAYER_CHAIN || d->op == TRIDENT_OP_LAYER_CHAIN_QKNORM;
-  if (d->dtype != TRIDENT_BF16 && d->dtype != TRIDENT_FP16 && d->dtype != TRIDENT_FP32)
+  const bool map = d->op == TRIDENT_OP_PAGE_MAP;
+  if (map ? d->dtype != TRIDENT_I32
+          : (d->dtype != TRIDENT_BF16 && d->dtype != TRIDENT_FP16 && d->dtype != TRIDENT_FP32))
     return fail(TRIDENT_ERR_INVALID, "activation dtype %d", d->dtype);
-  if (d->dtype == TRIDENT_FP32 && (oi.rope))
-    return fail(TRIDENT_ERR_INVALID, "RoPE ops and chains take bf16 or fp16");
-  if (oi.flattening ? (d->rank != 2 && d->rank != 3) : (d->rank != (chain ? 2 : 3)))
+  if (d->dtype == TRIDENT_FP32 && (oi.rope || is_paged_op(d->op)))
+    return fail(TRIDENT_ERR_INVALID, "RoPE ops, chains and paged attention take bf16 or fp16");
+  if (oi.flattening ? (d->rank != 2 && d->rank != 3) : (d->rank != (map ? 1 : chain ? 2 : 3)))
     return fail(TRIDENT_ERR_INVALID, "rank %d is not valid for op %d", d->rank, d->op);
   if (d->layout < TRIDENT_LAYOUT_CONTIG || d->layout > TRIDENT_LAYOUT_ANY)
     return fail(TRIDENT_ERR_INVALID, "layout %d", d->layout);
@@ -1115,6 +1392,18 @@ int32_t validate_desc(const trident_scm* scm, const trident_spec_desc* d, int32_
     const int64_t D = chain ? d->fixed[3] : d->fixed[2];
     if (D % 2 != 0 || D > 1024) return fail(TRIDENT_ERR_INVALID, "head size D must be even and <= 1024");
   }
+  if (is_rope_paged(d->op)) {
+    if (d->fixed[2] > 1024) return fail(TRIDENT_ERR_INVALID, "head size D must be <= 1024");
+    if (d->fixed[3] % 2 != 0 || d->fixed[3] > d->fixed[2])
+      return fail(TRIDENT_ERR_INVALID, "the rotated part R must be even and <= D");
+  }
+  if (d->op == TRIDENT_OP_PAGED_ATTN) {
+    if (d->fixed[0] % d->fixed[1] != 0) return fail(TRIDENT_ERR_INVALID, "Hq must be a multiple of Hkv");
+    if (d->fixed[2] > 512) return fail(TRIDENT_ERR_INVALID, "head size D must be <= 512");
+  }
+  if (is_paged_op(d->op))
+    for (int i = 0; i < oi.nfixed; ++i)
+      if (d->fixed[i] > 65536) return fail(TRIDENT_ERR_INVALID, "fixed[%d] must be <= 65536", i);
   *nfixed = oi.nfixed;
   return TRIDENT_OK;
 }
@@ -1137,6 +1426,20 @@ int32_t resolve_kernel(const trident_spec_desc& d, KernelEntry* ke) {
       case TRIDENT_OP_ROPE_KV:
       case TRIDENT_OP_QKNORM_ROPE_KV:
         return rope_kernel(d.dtype, var, (int32_t)d.fixed[2], d.op == TRIDENT_OP_QKNORM_ROPE_KV, ke, &why);
+      case TRIDENT_OP_PAGE_MAP:
+        if (var == TRIDENT_VARIANT_VECTOR) { why = "the page map has no vector variant"; return false; }
+        ke->kind = KK_PAGE_MAP;
+        ke->fn = page_map_entry();
+        return true;
+      case TRIDENT_OP_ROPE_PAGED_KV:
+      case TRIDENT_OP_ROPE_PAGED_KV_INTERLEAVED:
+      case TRIDENT_OP_QKNORM_ROPE_PAGED_KV:
+      case TRIDENT_OP_QKNORM_ROPE_PAGED_KV_INTERLEAVED:
+        return rope_paged_kernel(d.dtype, var, (int32_t)d.fixed[2], (int32_t)d.fixed[3],
+                                 d.op >= TRIDENT_OP_QKNORM_ROPE_PAGED_KV,
+                                 d.op == TRIDENT_OP_ROPE_PAGED_KV_INTERLEAVED ||
+                                     d.op == TRIDENT_OP_QKNORM_ROPE_PAGED_KV_INTERLEAVED, ke, &why);
+      case TRIDENT_OP_PAGED_ATTN: return paged_attn_kernel(d.dtype, var, (int32_t)d.fixed[2], ke, &why);
       default:
         if (var == TRIDENT_VARIANT_GENERIC) { why = "the layer chain has no generic variant"; return false; }
         return chain_kernel(d.dtype, d.fixed[0], (int32_t)d.fixed[3], d.op == TRIDENT_OP_LAYER_CHAIN_QKNORM, ke, &why);
@@ -1275,7 +1578,7 @@ int32_t append_version(trident_scm_t* scm, const trident_spec_desc* desc, int32_
   v.rope = g_ops[desc->op].rope;
   st = resolve_kernel(v.d, &v.ke);
   if (st != TRIDENT_OK) return st;
-  if (v.ke.kind == KK_ROPE_PAIR || v.ke.any_fn[0])
+  if (v.ke.kind == KK_ROPE_PAIR || (v.ke.kind == KK_ROPE_WARP && v.ke.any_fn[0]))
     rope_plans(desc->fixed[0] + 2 * desc->fixed[1], (int32_t)desc->fixed[2], &v.rope_plans);
   if (v.ke.kind == KK_CHAIN)
     for (int k = 0; k < 2; ++k)
@@ -1400,6 +1703,44 @@ TRIDENT_API int32_t trident_scm_register_tree_spec(trident_scm_t* scm, const tri
                                                    const trident_recipe* recipe, int32_t* out_index) {
   if (!recipe) return fail(TRIDENT_ERR_INVALID, "recipe is NULL");
   return register_version(scm, desc, recipe, out_index);
+}
+
+TRIDENT_API int32_t trident_scm_workspace(const trident_scm_t* scm, int32_t index, int64_t* out) {
+  if (!scm || !out) return fail(TRIDENT_ERR_INVALID, "NULL argument");
+  *out = 0;
+  if (index < 0 || index >= scm->count.load(std::memory_order_acquire))
+    return fail(TRIDENT_ERR_INVALID, "no version %d", index);
+  if (scm->dry) return fail(TRIDENT_ERR_STATE, "a dry-run SCM has no device to size a workspace for");
+  return TRIDENT_OK;
+}
+
+TRIDENT_API int32_t trident_rope_freqs(double theta, int32_t R, int32_t scaling, double factor, double context,
+                                       double slow, double fast, float* out) {
+  if (!out) return fail(TRIDENT_ERR_INVALID, "out is NULL");
+  if (R < 2 || R % 2 != 0 || R > 1024) return fail(TRIDENT_ERR_INVALID, "R must be even, in [2, 1024]");
+  if (!(theta > 0.0 && std::isfinite(theta))) return fail(TRIDENT_ERR_INVALID, "theta must be positive");
+  if (scaling < TRIDENT_ROPE_PLAIN || scaling > TRIDENT_ROPE_PARTS)
+    return fail(TRIDENT_ERR_INVALID, "unknown scaling %d", scaling);
+  if (scaling != TRIDENT_ROPE_PLAIN && !(factor >= 1.0 && std::isfinite(factor)))
+    return fail(TRIDENT_ERR_INVALID, "factor must be finite and >= 1");
+  if (scaling == TRIDENT_ROPE_BASE && R == 2) return fail(TRIDENT_ERR_INVALID, "a rescaled base needs R > 2");
+  if (scaling == TRIDENT_ROPE_PARTS &&
+      !(context > 0.0 && std::isfinite(context) && slow >= 0.0 && fast > slow && std::isfinite(fast)))
+    return fail(TRIDENT_ERR_INVALID, "scaling by parts needs context > 0 and 0 <= slow < fast");
+  const double base = scaling == TRIDENT_ROPE_BASE ? theta * std::pow(factor, (double)R / (double)(R - 2)) : theta;
+  for (int32_t i = 0; i < R / 2; ++i) {
+    double f = std::pow(base, -2.0 * (double)i / (double)R);
+    if (scaling == TRIDENT_ROPE_LINEAR) f /= factor;
+    if (scaling == TRIDENT_ROPE_PARTS) {
+      const double turns = context * f / 6.283185307179586477, k = (turns - slow) / (fast - slow);
+      const double keep = k < 0.0 ? 0.0 : (k > 1.0 ? 1.0 : k);
+      f *= keep + (1.0 - keep) / factor;
+    }
+    const float hi = (float)f;
+    out[2 * i] = hi;
+    out[2 * i + 1] = (float)(f - (double)hi);
+  }
+  return TRIDENT_OK;
 }
 
 TRIDENT_API int32_t trident_scm_select(const trident_scm_t* scm, const trident_args* args,

@@ -19,18 +19,22 @@ BF16, FP16, FP32, I32, I64, U8 = 1, 2, 3, 4, 5, 6
 OP_ADD_RMSNORM, OP_ROPE_KV, OP_QKNORM_ROPE_KV, OP_SWIGLU, OP_LAYER_CHAIN, OP_LAYER_CHAIN_QKNORM = 1, 2, 3, 4, 5, 6
 OP_RMSNORM = 7
 OP_SILU, OP_ADD, OP_NEG, OP_MASKED_FILL = 8, 9, 10, 11
+OP_PAGE_MAP, OP_ROPE_PAGED_KV, OP_ROPE_PAGED_KV_INTERLEAVED = 16, 17, 18
+OP_QKNORM_ROPE_PAGED_KV, OP_QKNORM_ROPE_PAGED_KV_INTERLEAVED, OP_PAGED_ATTN = 19, 20, 21
 LAYOUT_CONTIG, LAYOUT_ROWSTRIDED, LAYOUT_ANY = 0, 1, 2
 VARIANT_AUTO, VARIANT_GENERIC, VARIANT_VECTOR = 0, 1, 2
 OPT_DRY_RUN, OPT_NO_ALIAS_CHECK, OPT_PDL, OPT_TIMING, OPT_FAIL_LAUNCHES = 0x1, 0x2, 0x4, 0x8, 0x10
 OPT_NO_STEP_REPLAY = 0x20
 OPT_TEST_WAIT_TIMEOUT = 0x40
-DEVERR_POS, DEVERR_TIMEOUT = 0x1, 0x2
+DEVERR_POS, DEVERR_TIMEOUT, DEVERR_SLOT, DEVERR_PAGES, DEVERR_TABLE = 0x1, 0x2, 0x4, 0x8, 0x10
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS = 0, 1, 2, 3
 MAX_TENSORS, MAX_FIXED = 20, 8
 STEP_MAX = 48  # calls per launch of trident_scm_invoke_step
 TREE_MAX_NODES, TREE_MAX_DEPTH = 4096, 16
 NODE_NONE, NODE_TENSOR, NODE_DLTENSOR, NODE_TUPLE, NODE_INT, NODE_FLOAT = 0, 1, 2, 3, 4, 5
 BIND_UNUSED, BIND_CONST, BIND_EPS, BIND_THETA, BIND_SCALAR = -1, -2, -3, -4, -5
-OP_NTENSORS = {1: 5, 2: 6, 3: 8, 4: 3, 5: 18, 6: 20, 7: 3, 8: 2, 9: 3, 10: 2, 11: 3}
+OP_NTENSORS = {1: 5, 2: 6, 3: 8, 4: 3, 5: 18, 6: 20, 7: 3, 8: 2, 9: 3, 10: 2, 11: 3,
+               16: 10, 17: 9, 18: 9, 19: 11, 20: 11, 21: 9}
 
 c_i32, c_i64, c_u32, c_u64, c_dbl, c_vp = (ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32,
                                            ctypes.c_uint64, ctypes.c_double, ctypes.c_void_p)
@@ -108,6 +112,8 @@ def lib():
                                                        P(c_i32)]),
             "trident_scm_invoke_tree": (c_i32, [c_vp, P(trident_node), c_i32, c_i32, c_vp, P(c_i32)]),
             "trident_scm_set_tree_hook": (c_i32, [c_vp, TREE_HOOK, c_vp]),
+            "trident_scm_workspace": (c_i32, [c_vp, c_i32, P(c_i64)]),
+            "trident_rope_freqs": (c_i32, [c_dbl, c_i32, c_i32, c_dbl, c_dbl, c_dbl, c_dbl, P(ctypes.c_float)]),
             "trident_scm_stats": (c_i32, [c_vp, P(trident_scm_stats_t)]),
             "trident_scm_spec_hits": (c_i32, [c_vp, P(c_u64), c_i32, P(c_i32)]),
             "trident_scm_host_times": (c_i32, [c_vp, P(c_u32), c_i32, P(c_i32)]),
@@ -236,6 +242,20 @@ def trident_scm_select(scm, args):
     return st, sel.value
 
 
+def trident_scm_workspace(scm, index):
+    """Returns (status, elements of the version's fp32 workspace)."""
+    n = c_i64(0)
+    st = lib().trident_scm_workspace(scm, index, ctypes.byref(n))
+    return st, n.value
+
+
+def trident_rope_freqs(theta, R, scaling=ROPE_PLAIN, factor=1.0, context=0.0, slow=1.0, fast=32.0):
+    """Returns (status, list of R floats: R/2 pairs hi, lo)."""
+    out = (ctypes.c_float * max(R, 1))()
+    st = lib().trident_rope_freqs(theta, R, scaling, factor, context, slow, fast, out)
+    return st, list(out)
+
+
 def trident_scm_stats(scm):
     s = trident_scm_stats_t()
     st = lib().trident_scm_stats(scm, ctypes.byref(s))
@@ -348,11 +368,15 @@ def make_args(op, tensors, eps=1e-6, rope_theta=0.0, scalar=0.0):
     return a
 
 
+_RANK = {OP_ROPE_KV: 3, OP_QKNORM_ROPE_KV: 3, OP_PAGE_MAP: 1, OP_ROPE_PAGED_KV: 3, OP_ROPE_PAGED_KV_INTERLEAVED: 3,
+         OP_QKNORM_ROPE_PAGED_KV: 3, OP_QKNORM_ROPE_PAGED_KV_INTERLEAVED: 3, OP_PAGED_ATTN: 3}
+
+
 def make_spec(op, dtype, fixed, tok_lo, tok_hi, rank=None, layout=LAYOUT_CONTIG, align_bytes=16,
               device=0, variant=VARIANT_AUTO, rope_theta=0.0):
     d = trident_spec_desc()
     d.op, d.dtype = op, dtype
-    d.rank = rank if rank is not None else (3 if op in (OP_ROPE_KV, OP_QKNORM_ROPE_KV) else 2)
+    d.rank = rank if rank is not None else _RANK.get(op, 2)
     d.layout = layout
     for i, f in enumerate(fixed):
         d.fixed[i] = f
@@ -360,6 +384,15 @@ def make_spec(op, dtype, fixed, tok_lo, tok_hi, rank=None, layout=LAYOUT_CONTIG,
     d.align_bytes, d.device, d.variant = align_bytes, device, variant
     d.rope_theta = rope_theta
     return d
+
+
+def rope_freqs(theta, R, scaling=ROPE_PLAIN, factor=1.0, context=0.0, slow=1.0, fast=32.0, device="cuda"):
+    """The freqs tensor [R/2, 2] of the paged RoPE ops on `device` (trident_rope_freqs)."""
+    import torch
+    st, pairs = trident_rope_freqs(theta, R, scaling, factor, context, slow, fast)
+    if st != OK:
+        raise ScmError(st, "trident_rope_freqs")
+    return torch.tensor(pairs, dtype=torch.float32).view(R // 2, 2).to(device)
 
 
 # ---------------------------------------------------------------- structured arguments
@@ -569,6 +602,13 @@ class Scm:
 
     def select(self, args):
         return trident_scm_select(self.h, args)
+
+    def workspace(self, index):
+        """Elements of the fp32 workspace that version `index` needs (PAGED_ATTN's slot 6)."""
+        st, n = trident_scm_workspace(self.h, index)
+        if st != OK:
+            raise ScmError(st, "trident_scm_workspace")
+        return n
 
     def stats(self):
         return trident_scm_stats(self.h)[1]
