@@ -1,33 +1,9 @@
-// attn.cu -- attention of each request's last rows over its cache pages.
-//
-// Row i of request b's n rows stands at position kv - n + i and sees the keys up to there:
-//   s_j = scale * q . k_j,  m = max s_j,  l = sum exp(s_j - m),  out = sum exp(s_j - m) v_j / l,
-//   lse = m + log l.
-// Scores are kept in units of log 2 (scale * log2(e) folded in), so that each exponential is one exp2.
-#include "device_common.cuh"
+// attn.cu -- attention of each request's last rows over its cache pages, any alignment (the formulas
+// are in attn_common.cuh), and the choice of the kernels.
+#include "attn_common.cuh"
 
 namespace trident {
 namespace {
-
-constexpr uint32_t kErrTable = 0x10u;  // TRIDENT_DEVERR_TABLE
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-// Request b's rows [q0, q0 + n) and keys; lengths out of range give none and set *ok = false.
-struct Request { int32_t q0, n, kv; };
-__device__ __forceinline__ Request request(const PagedAttnParams& p, int64_t b, bool* ok) {
-  const int32_t c0 = p.cu[b], c1 = p.cu[b + 1], kv = p.kv[b];
-  const int64_t most = p.M * p.page.d;
-  Request r{c0, c1 - c0, kv};
-  if (c0 < 0 || c1 < c0 || c1 > p.T || (b == 0 && c0 != 0)) {
-    *ok = false;
-    r.q0 = r.n = 0;
-  }
-  if (kv < 0 || kv > most) {
-    *ok = false;
-    r.kv = kv < 0 ? 0 : (int32_t)most;
-  }
-  return r;
-}
 
 // Any alignment and head size up to 512: one warp per (row, head), a key per lane for the scores, then
 // the lanes split D for the product with v.
@@ -48,9 +24,9 @@ __global__ void __launch_bounds__(kThreads) attn_generic_kernel(const PagedAttnP
   }
   bool ok = p.B > 0;
   Request r{0, 0, 0};
-  if (ok) r = request(p, lo, &ok);
+  if (ok) r = attn_request(p, lo, &ok);
   if (unit == 0)  // one warp looks every request's numbers over
-    for (int64_t b = lane; b < p.B; b += 32) request(p, b, &ok);
+    for (int64_t b = lane; b < p.B; b += 32) attn_request(p, b, &ok);
   const bool mine = t >= r.q0 && t < r.q0 + r.n;
   const int64_t seen = mine ? max((int64_t)0, min((int64_t)r.kv, r.kv - r.n + (t - r.q0) + 1)) : 0;
   const char* q = row_ptr(p.q, t, p.q_rs, 2) + (int64_t)h * p.D * 2;
@@ -104,10 +80,23 @@ __global__ void __launch_bounds__(kThreads) attn_generic_kernel(const PagedAttnP
 
 }  // namespace
 
+int64_t attn_work_floats(const AttnEntry& e, int32_t sms) {
+  const int64_t blocks = (int64_t)sms * e.per_sm;
+  return e.fn ? attn_counters(blocks) + 2 * blocks * e.slot_floats : 0;
+}
+
 bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, KernelEntry* out, const char** why) {
   if (dtype != DT_BF16 && dtype != DT_FP16) { *why = "paged attention supports bf16 and fp16"; return false; }
-  if (variant != 1) { *why = "no vector kernel"; return false; }
   out->kind = KK_PAGED_ATTN;
+  if (variant != 1) {
+    if (!attn_rows_entry(dtype, D, &out->attn_rows)) {
+      *why = "vector paged attention supports D in {64, 128, 256}";
+      return false;
+    }
+    out->vec = 8;
+    out->fn = out->attn_rows.fn;
+    return true;
+  }
   out->vec = 1;
   out->fn = dtype == DT_BF16 ? (const void*)attn_generic_kernel<DT_BF16> : (const void*)attn_generic_kernel<DT_FP16>;
   return true;

@@ -1,0 +1,180 @@
+// attn_common.cuh -- what the paged attention kernels share: a request's rows and keys, the split of a
+// call's work over the blocks, and the joining of partial results.
+//
+// Row i of request b's n rows stands at position kv - n + i and sees the keys up to there:
+//   s_j = scale * q . k_j,  m = max s_j,  l = sum exp(s_j - m),  out = sum exp(s_j - m) v_j / l,
+//   lse = m + log l.
+// Scores are kept in units of log 2 (scale * log2(e) folded in), so that each exponential is one exp2.
+//
+// Split. A unit is one tile of a (request, kv head)'s rows (row r: token r / G, head r mod G of the
+// group); its keys come in tiles. The units' key tiles, one after the other over the whole call, are cut
+// into equal runs, one per block: a ragged batch, one long request and a long prompt then all load the
+// blocks evenly, from lengths that only the device knows. A unit that a cut goes through is joined from
+// its fragments' (m, l, unnormalised out) in the workspace by the block that finishes last -- in
+// fragment order, so that the result does not depend on which one that is; above kFanIn fragments in two
+// levels, since one block reading hundreds would take longer than the attention itself.
+#pragma once
+#include "device_common.cuh"
+
+namespace trident {
+
+constexpr uint32_t kErrTable = 0x10u;  // TRIDENT_DEVERR_TABLE
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// Request b's rows [q0, q0 + n) and keys; lengths out of range give none and set *ok = false.
+struct Request { int32_t q0, n, kv; };
+__device__ __forceinline__ Request attn_request(const PagedAttnParams& p, int64_t b, bool* ok) {
+  const int32_t c0 = p.cu[b], c1 = p.cu[b + 1], kv = p.kv[b];
+  const int64_t most = p.M * p.page.d;
+  Request r{c0, c1 - c0, kv};
+  if (c0 < 0 || c1 < c0 || c1 > p.T || (b == 0 && c0 != 0)) {
+    *ok = false;
+    r.q0 = r.n = 0;
+  }
+  if (kv < 0 || kv > most) {
+    *ok = false;
+    r.kv = kv < 0 ? 0 : (int32_t)most;
+  }
+  return r;
+}
+
+
+// Workspace: counters (zero between calls), then two slots of rows * (D + 2) floats per block: slot 2c
+// for the unit that a block's run starts within, 2c + 1 for the one that it ends within.
+constexpr int kFanIn = 16;
+__host__ __device__ constexpr int64_t attn_counters(int64_t blocks) { return (4 * blocks + 31) / 32 * 32; }
+__host__ __device__ constexpr int64_t attn_slot_floats(int rows, int D) { return (int64_t)rows * (D + 2); }
+
+template <int DT> struct ActType;
+template <> struct ActType<DT_BF16> {
+  static __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+    uint32_t w;
+    memcpy(&w, &b, 4);
+    return w;
+  }
+};
+template <> struct ActType<DT_FP16> {
+  static __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    __half2 b = __floats2half2_rn(lo, hi);
+    uint32_t w;
+    memcpy(&w, &b, 4);
+    return w;
+  }
+};
+
+__device__ __forceinline__ float fast_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Rows past the last request: out 0, lse -inf.
+template <int NT>
+__device__ __forceinline__ void attn_fill_tail(const PagedAttnParams& p) {
+  const int32_t last = p.B > 0 ? p.cu[p.B] : 0;
+  const int64_t t0 = last < 0 ? 0 : last;
+  for (int64_t t = t0 + blockIdx.x; t < p.T; t += gridDim.x) {
+    char* out = row_ptr(p.out, t, p.o_rs, 2);
+    for (int64_t e = threadIdx.x; e < (int64_t)p.Hq * p.D / 8; e += NT) st16(out + e * 16, make_uint4(0, 0, 0, 0));
+    for (int h = threadIdx.x; h < p.Hq; h += NT) p.lse[t * p.Hq + h] = -INFINITY;
+  }
+}
+
+// One block's share of the call. Cost of a request in key tiles: Hkv * row tiles * key tiles, at least
+// one tile per unit so that a unit without keys is written too.
+struct AttnShare {
+  int64_t per, lo, hi;  // tiles per block; this block's run [lo, hi)
+};
+
+template <int NT, int ROWS, int KEYS>
+struct AttnSplit {
+  struct Smem {
+    long long warp[NT / 32];
+    long long pre[NT + 1];  // tiles before each request of the current chunk, from the call's start
+    int32_t q0[NT], n[NT], kv[NT];
+    int flag;
+  };
+
+  static __device__ __forceinline__ int64_t row_tiles(const PagedAttnParams& p, int32_t n) {
+    return ((int64_t)n * p.G + ROWS - 1) / ROWS;
+  }
+  static __device__ __forceinline__ int64_t key_tiles(int32_t kv) { return kv > KEYS ? (kv + KEYS - 1) / KEYS : 1; }
+  // Does this kernel take the request? Rows outside (few, many] are the other kernel's.
+  static __device__ __forceinline__ bool takes(const PagedAttnParams& p, int32_t n) {
+    const int64_t rows = (int64_t)n * p.G;
+    return n > 0 && rows > p.rows_above && rows <= p.rows_upto;
+  }
+  static __device__ __forceinline__ int64_t cost(const PagedAttnParams& p, const Request& r) {
+    return takes(p, r.n) ? (int64_t)p.Hkv * row_tiles(p, r.n) * key_tiles(r.kv) : 0;
+  }
+
+  static __device__ __forceinline__ AttnShare share(const PagedAttnParams& p, Smem& s) {
+    bool ok = true;
+    long long sum = 0;
+    for (int64_t b = threadIdx.x; b < p.B; b += NT) sum += cost(p, attn_request(p, b, &ok));
+    if (!ok && blockIdx.x == 0) atomicOr(p.err, kErrTable);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if ((threadIdx.x & 31) == 0) s.warp[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    sum = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) sum += s.warp[w];
+    const int64_t even = (sum + gridDim.x - 1) / gridDim.x;
+    AttnShare a;
+    a.per = even > p.min_tiles ? even : p.min_tiles;
+    a.lo = min((int64_t)sum, (int64_t)blockIdx.x * a.per);
+    a.hi = min((int64_t)sum, a.lo + a.per);
+    return a;
+  }
+
+  // Fills the chunk of NT requests from b0 on; run: the tiles before it. Returns those after it.
+  static __device__ __forceinline__ int64_t chunk(const PagedAttnParams& p, Smem& s, int64_t b0, int64_t run) {
+    const int64_t b = b0 + threadIdx.x;
+    bool ok = true;
+    Request r{0, 0, 0};
+    if (b < p.B) r = attn_request(p, b, &ok);
+    const long long own = cost(p, r);
+    long long v = own;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long u = __shfl_up_sync(0xffffffffu, v, o);
+      if ((int)(threadIdx.x & 31) >= o) v += u;
+    }
+    __syncthreads();  // the chunk before has been read
+    if ((threadIdx.x & 31) == 31) s.warp[threadIdx.x >> 5] = v;
+    s.q0[threadIdx.x] = r.q0;
+    s.n[threadIdx.x] = r.n;
+    s.kv[threadIdx.x] = r.kv;
+    __syncthreads();
+    long long before = run, all = run;
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) {
+      if (w < (int)(threadIdx.x >> 5)) before += s.warp[w];
+      all += s.warp[w];
+    }
+    s.pre[threadIdx.x + 1] = before + v;
+    if (threadIdx.x == 0) s.pre[0] = run;
+    __syncthreads();
+    return all;
+  }
+
+  // The request of the chunk that holds tile x (pre[0] <= x < pre[NT]).
+  static __device__ __forceinline__ int find(const Smem& s, int64_t x) {
+    int r = 0;
+#pragma unroll
+    for (int step = NT / 2; step > 0; step >>= 1)
+      if (s.pre[r + step] <= x) r += step;
+    return r;
+  }
+};
+
+// A fragment's place: unit tiles [u0, u1) of the call, cut into runs of `per` tiles.
+struct AttnCuts {
+  int64_t first, last;  // blocks that hold a part of the unit
+  __device__ __forceinline__ bool whole() const { return first == last; }
+  __device__ __forceinline__ int64_t slot(int64_t block) const { return block == first ? 2 * block + 1 : 2 * block; }
+};
+
+}  // namespace trident

@@ -219,6 +219,8 @@ struct PagedAttnParams {
   int32_t Hq, Hkv, G, D;
   float scale;
   FastDiv page, group;  // by ps; by G = Hq / Hkv
+  int64_t rows_above, rows_upto;  // this launch takes the requests of rows_above < n * G <= rows_upto
+  int64_t min_tiles;              // a block's run of key tiles is at least this long
 };
 
 // Elementwise entries (pointwise_plan): flat and rows kernels with one or two vectors per
@@ -235,6 +237,13 @@ int pointwise_plan(PointwiseParams* p, int32_t op, int32_t eb, int64_t* blocks, 
 constexpr int kNormBlockVecs = 2048;  // norm_block_kernel, norm_bulk_kernel: vectors of a row at most
 enum NormEntry : int32_t { NM_VEC, NM_EDGE, NM_EDGE_MANY, NM_GENERIC, NM_LARGE, NM_FEW, NM_MID,
                            NM_EDGE_FLAT, kNormEntries };
+
+// An attention kernel with its launch shape: per_sm blocks on every SM, each with two workspace slots.
+struct AttnEntry {
+  const void* fn = nullptr;
+  int32_t threads = 0, smem = 0, per_sm = 0;
+  int64_t slot_floats = 0;
+};
 
 // Kernel entry (host stub address) plus its launch shape rule.
 struct KernelEntry {
@@ -263,6 +272,7 @@ struct KernelEntry {
   int32_t threads = 0;   // chain: block size
   const void* nm_fn[kNormEntries] = {};  // norms, by NormEntry (NULL: none for this H)
   int32_t nm_threads[kNormEntries] = {};
+  AttnEntry attn_rows;   // paged attention: requests of few rows
   int32_t rows = 1;      // norms: rows per block of the NM_VEC entry
   int32_t edge_rows = 1;  // ... and of the NM_EDGE_MANY entry,
   int64_t edge_many = 0;  // which calls of at least this many rows take (on 152 SMs)
@@ -343,6 +353,8 @@ bool rope_paged_kernel(int32_t dtype, int32_t variant, int32_t D, int32_t R, boo
                        KernelEntry* out, const char** why);
 // Which any_fn entry a vector call takes; sets its item split, block size and grid.
 int rope_paged_plan(RopePagedParams* p, int32_t* threads, int64_t* blocks, int32_t sms);
+bool attn_rows_entry(int32_t dtype, int32_t D, AttnEntry* e);
+int64_t attn_work_floats(const AttnEntry& e, int32_t sms);
 bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, KernelEntry* out, const char** why);
 const void* empty_kernel_entry();  // the latency-floor probe's kernel (does nothing)
 

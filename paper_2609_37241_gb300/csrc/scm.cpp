@@ -1032,7 +1032,18 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
   if (s.T * p.Hq >= kMost || p.B >= kMost || p.M * (int64_t)p.page.d >= kMost || p.P > kMost)
     return fail(TRIDENT_ERR_INVALID, "paged attention call too large for 32-bit counts");
   void* kp[1] = {&p};
-  cfg.gridDimX = cap_grid((s.T * p.Hq + kThreads / 32 - 1) / (kThreads / 32));
+  if (v.ke.vec == 1) {
+    cfg.gridDimX = cap_grid((s.T * p.Hq + kThreads / 32 - 1) / (kThreads / 32));
+    return launch_on(scm, &cfg, v.fn, kp);
+  }
+  if (a->t[6].shape[0] < attn_work_floats(v.ke.attn_rows, scm->sm_count))
+    return fail(TRIDENT_ERR_INVALID, "the workspace is smaller than trident_scm_workspace says");
+  p.rows_above = 0;
+  p.rows_upto = INT64_MAX;
+  p.min_tiles = 4;
+  cfg.blockDimX = (unsigned)v.ke.attn_rows.threads;
+  cfg.gridDimX = (unsigned)(scm->sm_count * v.ke.attn_rows.per_sm);
+  cfg.sharedMemBytes = (unsigned)v.ke.attn_rows.smem;
   return launch_on(scm, &cfg, v.fn, kp);
 }
 
@@ -1598,6 +1609,9 @@ int32_t append_version(trident_scm_t* scm, const trident_spec_desc* desc, int32_
           cudaFuncSetAttribute(v.ke.nm_fn[NM_LARGE], cudaFuncAttributeMaxDynamicSharedMemorySize,
                                2 * kNormBlockVecs * 16) != cudaSuccess)
         return fail(TRIDENT_ERR_CUDA, "cannot set the norm kernel's shared-memory size");
+      if (v.ke.attn_rows.fn && cudaFuncSetAttribute(v.ke.attn_rows.fn, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                    v.ke.attn_rows.smem) != cudaSuccess)
+        return fail(TRIDENT_ERR_CUDA, "cannot set the attention kernel's shared-memory size");
       auto resolve = [&](const void* entry, CUfunction* out_fn) {
         cudaFunction_t e = nullptr;
         if (entry && (cudaGetFuncBySymbol(&e, entry) != cudaSuccess || !e)) return false;
@@ -1711,6 +1725,7 @@ TRIDENT_API int32_t trident_scm_workspace(const trident_scm_t* scm, int32_t inde
   if (index < 0 || index >= scm->count.load(std::memory_order_acquire))
     return fail(TRIDENT_ERR_INVALID, "no version %d", index);
   if (scm->dry) return fail(TRIDENT_ERR_STATE, "a dry-run SCM has no device to size a workspace for");
+  *out = attn_work_floats(scm->versions[index].ke.attn_rows, scm->sm_count);
   return TRIDENT_OK;
 }
 
