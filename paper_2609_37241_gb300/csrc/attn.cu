@@ -80,6 +80,16 @@ __global__ void __launch_bounds__(kThreads) attn_generic_kernel(const PagedAttnP
 
 }  // namespace
 
+// The lengths are on the device, so the choice goes by what T and B leave possible. Pages that do not
+// divide a tile's keys (or are no multiple of them), or hold fewer than the eight rows of a swizzle atom,
+// and groups of more than a tile's rows stay with the kernel of few rows. Where T - B extra rows cannot
+// make a request of more than kTileRows (every request with a row at least), so does the call.
+AttnPlan attn_plan(const AttnEntry& tile, int64_t T, int64_t B, int64_t G, int64_t ps) {
+  const bool fits = tile.fn && G <= 128 && ps % 8 == 0 && (tile.keys % ps == 0 || ps % tile.keys == 0);
+  if (!fits || T * G <= kTileRows || (T - B + 1) * G <= kTileRows) return {true, false};
+  return {B > 1, true};
+}
+
 int64_t attn_work_floats(const AttnEntry& e, int32_t sms) {
   const int64_t blocks = (int64_t)sms * e.per_sm;
   return e.fn ? attn_counters(blocks) + 2 * blocks * e.slot_floats : 0;
@@ -93,6 +103,7 @@ bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, KernelEntry* o
       *why = "vector paged attention supports D in {64, 128, 256}";
       return false;
     }
+    attn_tile_entry(dtype, D, &out->attn_tile);
     out->vec = 8;
     out->fn = out->attn_rows.fn;
     return true;

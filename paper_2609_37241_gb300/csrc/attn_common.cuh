@@ -81,32 +81,29 @@ __device__ __forceinline__ void attn_fill_tail(const PagedAttnParams& p) {
   }
 }
 
-// One block's share of the call. Cost of a request in key tiles: Hkv * row tiles * key tiles, at least
-// one tile per unit so that a unit without keys is written too.
+// Does this launch take the request? Rows outside (above, upto] are the other kernel's.
+__device__ __forceinline__ bool attn_takes(const PagedAttnParams& p, int32_t n) {
+  const int64_t rows = (int64_t)n * p.G;
+  return n > 0 && rows > p.rows_above && rows <= p.rows_upto;
+}
+
+// One block's share of the call: tiles per block and this block's run [lo, hi).
 struct AttnShare {
-  int64_t per, lo, hi;  // tiles per block; this block's run [lo, hi)
+  int64_t per, lo, hi;
 };
 
-template <int NT, int ROWS, int KEYS>
+// Cost::of(p, r): the key tiles of all of request r's units, at least one per unit so that a unit
+// without keys is written too. NT: threads of the block.
+template <int NT, class Cost>
 struct AttnSplit {
   struct Smem {
-    long long warp[NT / 32];
+    long long warp[(NT + 31) / 32];
     long long pre[NT + 1];  // tiles before each request of the current chunk, from the call's start
     int32_t q0[NT], n[NT], kv[NT];
-    int flag;
   };
 
-  static __device__ __forceinline__ int64_t row_tiles(const PagedAttnParams& p, int32_t n) {
-    return ((int64_t)n * p.G + ROWS - 1) / ROWS;
-  }
-  static __device__ __forceinline__ int64_t key_tiles(int32_t kv) { return kv > KEYS ? (kv + KEYS - 1) / KEYS : 1; }
-  // Does this kernel take the request? Rows outside (few, many] are the other kernel's.
-  static __device__ __forceinline__ bool takes(const PagedAttnParams& p, int32_t n) {
-    const int64_t rows = (int64_t)n * p.G;
-    return n > 0 && rows > p.rows_above && rows <= p.rows_upto;
-  }
   static __device__ __forceinline__ int64_t cost(const PagedAttnParams& p, const Request& r) {
-    return takes(p, r.n) ? (int64_t)p.Hkv * row_tiles(p, r.n) * key_tiles(r.kv) : 0;
+    return attn_takes(p, r.n) ? Cost::of(p, r) : 0;
   }
 
   static __device__ __forceinline__ AttnShare share(const PagedAttnParams& p, Smem& s) {
@@ -160,12 +157,14 @@ struct AttnSplit {
     return all;
   }
 
-  // The request of the chunk that holds tile x (pre[0] <= x < pre[NT]).
+  // The last request of the chunk with pre[r] <= x (pre[0] <= x < the chunk's end): it holds tile x.
   static __device__ __forceinline__ int find(const Smem& s, int64_t x) {
-    int r = 0;
-#pragma unroll
-    for (int step = NT / 2; step > 0; step >>= 1)
-      if (s.pre[r + step] <= x) r += step;
+    int r = 0, end = NT;
+    while (end - r > 1) {
+      const int mid = (r + end) / 2;
+      if (s.pre[mid] <= x) r = mid;
+      else end = mid;
+    }
     return r;
   }
 };
@@ -176,5 +175,27 @@ struct AttnCuts {
   __device__ __forceinline__ bool whole() const { return first == last; }
   __device__ __forceinline__ int64_t slot(int64_t block) const { return block == first ? 2 * block + 1 : 2 * block; }
 };
+
+// Counts a finished part; true in every thread of the NT that call it (named barrier BAR) for the block
+// that completes `total` of them, which also puts the counter back to zero. What the parts' blocks
+// wrote before is visible to it. flag: a shared word.
+template <int BAR, int NT>
+__device__ __forceinline__ void attn_sync() {
+  asm volatile("bar.sync %0, %1;" :: "n"(BAR), "n"(NT) : "memory");
+}
+template <int BAR, int NT>
+__device__ __forceinline__ bool attn_completes(volatile int* flag, bool leader, uint32_t* counter, uint32_t total) {
+  __threadfence();
+  attn_sync<BAR, NT>();
+  if (leader) {
+    const bool last = atomicAdd(counter, 1u) + 1 == total;
+    if (last) *counter = 0u;
+    *flag = last;
+  }
+  attn_sync<BAR, NT>();
+  const bool last = *flag != 0;
+  if (last) __threadfence();
+  return last;
+}
 
 }  // namespace trident

@@ -65,10 +65,24 @@ struct Unit {
   int32_t q0, n, kv, h, r0, rows, limit;  // rows: of the 16 that exist; limit: keys that the last one sees
 };
 
+// Every row tile counted with all of the request's keys: exact for decode steps, a little unequal where a
+// long chunk comes this way.
+struct RowsCost {
+  static __device__ __forceinline__ int64_t row_tiles(const PagedAttnParams& p, int32_t n) {
+    return ((int64_t)n * p.G + kRowsTile - 1) / kRowsTile;
+  }
+  static __device__ __forceinline__ int64_t key_tiles(int32_t kv) {
+    return kv > kRowsKeys ? ((int64_t)kv + kRowsKeys - 1) / kRowsKeys : 1;
+  }
+  static __device__ __forceinline__ int64_t of(const PagedAttnParams& p, const Request& r) {
+    return (int64_t)p.Hkv * row_tiles(p, r.n) * key_tiles(r.kv);
+  }
+};
+
 template <int DT, int D>
 struct RowsKernel {
   using G = RowsGeom<D>;
-  using Split = AttnSplit<kRowsThreads, kRowsTile, kRowsKeys>;
+  using Split = AttnSplit<kRowsThreads, RowsCost>;
   struct Smem {
     alignas(128) char ring[G::RING];
     typename Split::Smem split;
@@ -342,22 +356,6 @@ struct RowsKernel {
     }
   }
 
-  // Counts a finished part; true in every thread of the block that completes `total` of them, which also
-  // puts the counter back to zero. What the parts' blocks wrote before is visible to it.
-  static __device__ __forceinline__ bool completes(Smem& s, uint32_t* counter, uint32_t total) {
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      const uint32_t before = atomicAdd(counter, 1u);
-      s.last = before + 1 == total;
-      if (s.last) *counter = 0u;
-    }
-    __syncthreads();
-    const bool last = s.last != 0;
-    if (last) __threadfence();
-    return last;
-  }
-
   static __device__ __forceinline__ void run(const PagedAttnParams& p, Smem& s) {
     const AttnShare a = Split::share(p, s.split);
     attn_fill_tail<kRowsThreads>(p);
@@ -375,7 +373,7 @@ struct RowsKernel {
         u.q0 = s.split.q0[rq];
         u.n = s.split.n[rq];
         u.kv = s.split.kv[rq];
-        const int64_t nt = Split::key_tiles(u.kv), nm = Split::row_tiles(p, u.n);
+        const int64_t nt = RowsCost::key_tiles(u.kv), nm = RowsCost::row_tiles(p, u.n);
         const int64_t rel = x - s.split.pre[rq], unit = rel / nt, t0 = rel - unit * nt;
         const int64_t t1 = min(nt, t0 + a.hi - x);
         u.h = (int32_t)(unit / nm);
@@ -396,9 +394,10 @@ struct RowsKernel {
           const int64_t g0 = cut.first + (int64_t)gr * kFanIn;
           const int size = min(kFanIn, n - gr * kFanIn);
           auto slot = [&](int64_t block) { return slots + cut.slot(block) * SLOT; };
-          if (completes(s, counters + cut.slot(g0), size)) {
+          if (attn_completes<0, kRowsThreads>(&s.last, threadIdx.x == 0, counters + cut.slot(g0), size)) {
             join_slots(p, s, u, size, [&](int i) { return slot(g0 + i); }, groups > 1 ? slot(g0) : nullptr);
-            if (groups > 1 && completes(s, counters + 2 * gridDim.x + cut.slot(cut.first), groups))
+            if (groups > 1 && attn_completes<0, kRowsThreads>(&s.last, threadIdx.x == 0,
+                                                            counters + 2 * gridDim.x + cut.slot(cut.first), groups))
               join_slots(p, s, u, groups, [&](int i) { return slot(cut.first + (int64_t)i * kFanIn); }, nullptr);
           }
         }

@@ -1,0 +1,714 @@
+// attn_tile.cu -- paged attention for requests of many rows: chunks of a prompt.
+//
+// Bound: the tensor cores. A unit is NT tiles of 128 rows (tokens x the G heads of a group, so that all of
+// them share the keys' loads) against tiles of KEYS keys; per block NT softmax warpgroups, one warp that
+// issues tcgen05.mma and one that loads:
+//   load     k and v tiles by TMA, a box per page, into a ring of KEYS x D slots in the 128-byte swizzle;
+//            a unit's last v tile gets zeros in the rows past the last key up to the next 16 (a pool's
+//            unused rows may hold NaN, and 0 * NaN would reach the sums)
+//   mma      S_x = Q_x K^T into TMEM, then for each tile O_x += P_x V with P_x from TMEM; the tiles take
+//            turns, so that one tile's products run while the other tile's softmax does
+//   softmax  a thread per row, so no exchange between lanes: 128 scores from TMEM, running maximum and
+//            sum, numerators rounded to the activation type back into the columns of S_x
+// The running maximum moves only when a score passes it by 2^kLazy; then the row's accumulator in TMEM is
+// rescaled by its own thread, which may touch it because S_x of the next tile is issued after P_x V.
+// TMEM columns: NT x KEYS of S (P in their first half) and NT x D of O.
+//
+// Every wait is bounded (params.polls polls, kBulkWaitPolls by default): a wait that runs out sets
+// TRIDENT_DEVERR_TIMEOUT and a flag that ends the block's other waits; the warps then let their copies
+// and products in flight finish (bounded again), free the TMEM and return without further writes.
+#include <cuda.h>
+
+#include "attn_common.cuh"
+
+namespace trident {
+namespace {
+
+constexpr float kLazy = 8.f;
+constexpr int kFrags = 32;  // fragments listed at a time
+
+// ---------------------------------------------------------------- barriers, TMA, tcgen05
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mb_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mb_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ void mb_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mb_try(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{ .reg .pred q; mbarrier.try_wait.parity.shared::cta.b64 q, [%1], %2; selp.u32 %0, 1, 0, q; }"
+               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  return done != 0;
+}
+// Bounded wait; false when it ran out or another wait of the block did.
+__device__ __forceinline__ bool mb_wait(uint32_t bar, uint32_t parity, uint32_t polls, volatile int* abort) {
+  for (uint32_t i = 0; i < polls; ++i) {
+    if (mb_try(bar, parity)) return true;
+    if ((i & 15) == 15 && *abort) return false;
+  }
+  *abort = 1;
+  return false;
+}
+// Bounded wait on the way out, whatever the flag says.
+__device__ __forceinline__ void mb_drain(uint32_t bar, uint32_t parity) {
+  for (uint32_t i = 0; i < kBulkWaitPolls; ++i)
+    if (mb_try(bar, parity)) return;
+}
+__device__ __forceinline__ void tma_4d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+               " [%0], [%1, {%2, %3, %4, %5}], [%6];"
+               :: "r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }"
+               :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
+               :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+// Shared-memory operand descriptor, 128-byte swizzle (layout code 2, bits 61-63; version 1, bits 46-48):
+// start, leading and stride byte offsets in units of 16.
+__device__ __forceinline__ uint64_t desc128(uint32_t at, uint32_t leading, uint32_t stride) {
+  return (uint64_t)((at >> 4) & 0x3fff) | ((uint64_t)(leading >> 4) << 16) | ((uint64_t)(stride >> 4) << 32) |
+         (1ull << 46) | (2ull << 61);
+}
+// Instruction descriptor of kind::f16: fp32 accumulators, A and B of the activation type, both K-major
+// unless b_mn, M x N.
+template <int DT>
+__host__ __device__ constexpr uint32_t idesc_of(int M, int N, bool b_mn) {
+  return (1u << 4) | ((DT == DT_BF16 ? 1u : 0u) << 7) | ((DT == DT_BF16 ? 1u : 0u) << 10) | ((b_mn ? 1u : 0u) << 16) |
+         ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+#define TC_R8(r, k) "=r"(r[k]), "=r"(r[k + 1]), "=r"(r[k + 2]), "=r"(r[k + 3]), "=r"(r[k + 4]), "=r"(r[k + 5]), "=r"(r[k + 6]), "=r"(r[k + 7])
+#define TC_I8(r, k) "r"(r[k]), "r"(r[k + 1]), "r"(r[k + 2]), "r"(r[k + 3]), "r"(r[k + 4]), "r"(r[k + 5]), "r"(r[k + 6]), "r"(r[k + 7])
+// 32 columns of the warp's 32 lanes: lane i, register k = column k.
+__device__ __forceinline__ void tc_ld32(uint32_t at, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+               "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+               : TC_R8(r, 0), TC_R8(r, 8), TC_R8(r, 16), TC_R8(r, 24) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tc_st32(uint32_t at, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+               "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+               :: TC_I8(r, 0), TC_I8(r, 8), TC_I8(r, 16), TC_I8(r, 24), "r"(at) : "memory");
+}
+
+// ---------------------------------------------------------------- units
+// sum of floor((a i + b) / m) for i < n; a, b >= 0 (the Euclid-like reduction of lattice-point counts).
+__device__ __forceinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
+  int64_t total = 0;
+  while (n > 0) {
+    total += n * (n - 1) / 2 * (a / m) + n * (b / m);
+    a %= m;
+    b %= m;
+    const int64_t y = a * n + b;  // the last term's numerator is y - a
+    if (y < m) break;
+    n = y / m;
+    b = y % m;
+    const int64_t t = m;
+    m = a;
+    a = t;
+  }
+  return total;
+}
+
+// Row tile k of a request: tokens [k R, (k + 1) R) of its n, R = ROWS / G whole tokens. It sees
+// kv - n + min(n, (k + 1) R) keys (its last token's).
+template <int ROWS, int KEYS>
+struct TileCost {
+  static __device__ __forceinline__ int32_t tokens(const PagedAttnParams& p) { return ROWS / p.G; }
+  static __device__ __forceinline__ int32_t sees(const PagedAttnParams& p, const Request& r, int32_t k) {
+    const int64_t i = min((int64_t)r.n, (int64_t)(k + 1) * tokens(p));
+    return (int32_t)max((int64_t)0, min((int64_t)r.kv, (int64_t)r.kv - r.n + i));
+  }
+  static __device__ __forceinline__ int32_t key_tiles(int32_t keys) { return keys > KEYS ? (keys + KEYS - 1) / KEYS : 1; }
+  static __device__ __forceinline__ int32_t row_tiles(const PagedAttnParams& p, const Request& r) {
+    const int32_t R = tokens(p);
+    return (int32_t)(((int64_t)r.n + R - 1) / R);
+  }
+  // Key tiles of the first k row tiles of one kv head.
+  static __device__ __forceinline__ int64_t before(const PagedAttnParams& p, const Request& r, int32_t k) {
+    const int64_t c = (int64_t)r.kv - r.n, R = tokens(p);
+    int64_t full = k;  // row tiles that end at a whole R
+    int64_t total = 0;
+    if (k == row_tiles(p, r) && k > 0) {
+      --full;
+      total = key_tiles(sees(p, r, k - 1));
+    }
+    if (c >= 0) return total + floor_sum(full, KEYS, R, c + R + KEYS - 1);
+    for (int64_t i = 0; i < full; ++i) total += key_tiles(sees(p, r, (int32_t)i));
+    return total;
+  }
+  static __device__ __forceinline__ int64_t of(const PagedAttnParams& p, const Request& r) {
+    return (int64_t)p.Hkv * before(p, r, row_tiles(p, r));
+  }
+};
+
+struct Frag {
+  int64_t b, first, last;  // request; blocks that share the unit
+  int32_t q0, n, kv, h, tok0, rows, limit;
+  int32_t t0, t1;          // key tiles
+};
+
+template <int DT_, int D_, int NT_, int KEYS_, int SLOTS_>
+struct Tile {
+  static constexpr int DT = DT_, D = D_, NT = NT_, KEYS = KEYS_, SLOTS = SLOTS_;
+  static constexpr int ROWS = 128 * NT;
+  static constexpr int SOFT = 128 * NT;        // softmax threads
+  static constexpr int THREADS = SOFT + 64;
+  static constexpr int QB = 128 * D * 2;       // bytes of a q tile
+  static constexpr int KB = KEYS * D * 2;      // ... of a k or v tile
+  static constexpr int QHALF = 128 * 128, KHALF = KEYS * 128;  // bytes of 64 columns
+  static constexpr int S_COL = 0, O_COL = NT * KEYS;
+  static_assert(NT * (KEYS + D) <= 512, "TMEM columns");
+  using Cost = TileCost<ROWS, KEYS>;
+  using Split = AttnSplit<THREADS, Cost>;
+  struct Smem {
+    alignas(1024) char q[NT * QB];
+    alignas(1024) char ring[SLOTS * KB];
+    alignas(8) uint64_t full[SLOTS], empty[SLOTS], raw, q_full[NT], s_full[NT], p_full[NT], o_full[NT], drain;
+    uint32_t tmem;
+    volatile int abort, flag;
+    int count;
+    long long x;
+    Frag frag[kFrags];
+    typename Split::Smem split;
+  };
+
+  // ------------------------------------------------------------ load warp
+  struct Load {
+    uint32_t issued = 0;     // slots filled so far
+    uint32_t raws = 0;       // v tiles with a wait of their own
+    bool bad = false;
+  };
+  static __device__ __forceinline__ bool load(const PagedAttnParams& p, const CUtensorMap* mk, const CUtensorMap* mv,
+                                              Smem& s, const Frag& f, Load& st) {
+    const int lane = threadIdx.x & 31;
+    const int32_t* table = p.table + f.b * p.table_rs;
+    const int ps = p.page.d, box = min(ps, KEYS);       // rows of a box
+    for (int32_t t = f.t0; t < f.t1; ++t) {
+      const int32_t j0 = t * KEYS, valid = min(KEYS, f.limit - j0);
+      const int boxes = (valid + box - 1) / box;
+      int32_t page = 0, at = 0;
+      if (lane < boxes) {
+        const uint32_t j = (uint32_t)(j0 + lane * box), pg = fast_div(j, p.page.magic, p.page.shift);
+        at = (int32_t)(j - pg * (uint32_t)ps);
+        page = table[pg];
+        if (page < 0 || page >= p.P) {
+          st.bad = true;
+          page = 0;
+        }
+      }
+      for (int kv = 0; kv < 2; ++kv) {
+        const uint32_t slot = st.issued % SLOTS, use = st.issued / SLOTS;
+        if (!__all_sync(0xffffffffu, mb_wait(smem_at(&s.empty[slot]), (use & 1) ^ 1, p.polls, &s.abort))) return false;
+        const bool tail = kv == 1 && valid % 16 != 0;
+        const uint32_t bar = smem_at(tail ? &s.raw : &s.full[slot]), dst = smem_at(s.ring + slot * KB);
+        if (lane == 0) mb_expect(bar, (uint32_t)(boxes * box * D * 2));
+        __syncwarp();
+        if (lane < boxes)
+          for (int c = 0; c < D / 64; ++c)
+            tma_4d(dst + c * KHALF + lane * box * 128, kv ? mv : mk, c * 64, at, f.h, page, bar);
+        __syncwarp();
+        ++st.issued;
+        if (tail) {  // zeros from the last key to the next 16
+          const uint32_t parity = st.raws++ & 1;
+          if (!__all_sync(0xffffffffu, mb_wait(bar, parity, p.polls, &s.abort))) {
+            mb_drain(bar, parity);
+            mb_arrive_lane0(smem_at(&s.full[slot]));
+            return false;
+          }
+          const int rows = 16 - valid % 16;
+          for (int e = lane; e < rows * (D / 8); e += 32) {
+            const int r = valid + e / (D / 8), c = e % (D / 8);
+            *reinterpret_cast<uint4*>(s.ring + slot * KB + (c / 8) * KHALF + r * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
+          }
+          fence_async();
+          __syncwarp();
+          mb_arrive_lane0(smem_at(&s.full[slot]));
+        }
+      }
+    }
+    return true;
+  }
+  static __device__ __forceinline__ void mb_arrive_lane0(uint32_t bar) {
+    if ((threadIdx.x & 31) == 0) mb_arrive(bar);
+    __syncwarp();
+  }
+
+  // ------------------------------------------------------------ mma warp (one lane)
+  struct Mma {
+    uint32_t taken = 0;                 // slots consumed so far
+    uint32_t px[NT] = {}, qx[NT] = {};  // p and q tiles waited for
+  };
+  static __device__ __forceinline__ void qk(Smem& s, uint32_t tmem, int x, uint32_t slot) {
+    constexpr uint32_t id = idesc_of<DT>(128, KEYS, false);
+    const uint32_t qa = smem_at(s.q + x * QB), ka = smem_at(s.ring + slot * KB);
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+      mma_ss(tmem + S_COL + x * KEYS, desc128(qa + (k / 4) * QHALF + (k % 4) * 32, 16, 1024),
+             desc128(ka + (k / 4) * KHALF + (k % 4) * 32, 16, 1024), id, k > 0);
+  }
+  static __device__ __forceinline__ void pv(Smem& s, uint32_t tmem, int x, uint32_t slot, int steps, bool add) {
+    constexpr uint32_t id = idesc_of<DT>(128, D, true);
+    const uint32_t va = smem_at(s.ring + slot * KB);
+    for (int k = 0; k < steps; ++k)
+      mma_ts(tmem + O_COL + x * D, tmem + S_COL + x * KEYS + k * 8, desc128(va + k * 2048, KHALF, 1024), id, add || k > 0);
+  }
+  static __device__ __forceinline__ bool mma(const PagedAttnParams& p, Smem& s, uint32_t tmem, const Frag& f, Mma& st) {
+    const int tiles = f.rows > 128 ? NT : 1;
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return mb_wait(smem_at(bar), parity, p.polls, &s.abort); };
+    auto slot_ready = [&](uint32_t i) { return wait(&s.full[i % SLOTS], (i / SLOTS) & 1); };
+#pragma unroll
+    for (int x = 0; x < NT; ++x)
+      if (x < tiles && !wait(&s.q_full[x], st.qx[x]++ & 1)) return false;
+    uint32_t k = st.taken;  // slot of the current k tile; v: the next
+    if (!slot_ready(k)) return false;
+    tc_after();
+    for (int x = 0; x < tiles; ++x) {
+      qk(s, tmem, x, k % SLOTS);
+      tc_commit(smem_at(&s.s_full[x]));
+    }
+    tc_commit(smem_at(&s.empty[k % SLOTS]));
+    for (int32_t t = f.t0; t < f.t1; ++t) {
+      const uint32_t v = k + 1;
+      const bool more = t + 1 < f.t1;
+      const int steps = (min(KEYS, f.limit - t * KEYS) + 15) / 16;
+      if (!slot_ready(v)) return false;
+#pragma unroll
+      for (int x = 0; x < NT; ++x) {
+        if (x >= tiles) break;
+        if (!wait(&s.p_full[x], st.px[x]++ & 1)) return false;
+        tc_after();
+        pv(s, tmem, x, v % SLOTS, steps, t > f.t0);
+        if (x == tiles - 1) tc_commit(smem_at(&s.empty[v % SLOTS]));
+        if (more) {
+          if (x == 0 && !slot_ready(v + 1)) return false;
+          tc_after();
+          qk(s, tmem, x, (v + 1) % SLOTS);
+          tc_commit(smem_at(&s.s_full[x]));
+          if (x == tiles - 1) tc_commit(smem_at(&s.empty[(v + 1) % SLOTS]));
+        } else {
+          tc_commit(smem_at(&s.o_full[x]));
+        }
+      }
+      k += 2;
+    }
+    st.taken = k;
+    return true;
+  }
+
+  // ------------------------------------------------------------ softmax warpgroup
+  struct Soft {
+    uint32_t s = 0, o = 0;  // tiles and fragments waited for
+  };
+  // Loads this warpgroup's q rows into the swizzled tile: 16 bytes per lane, D / 8 lanes per row.
+  static __device__ __forceinline__ void load_q(const PagedAttnParams& p, Smem& s, const Frag& f, int x) {
+    constexpr int CH = D / 8, RPI = 32 / CH > 0 ? 32 / CH : 1, ITER = 32 / RPI;
+    const int w = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, c = lane % CH, rr = lane / CH;
+#pragma unroll 8
+    for (int i = 0; i < ITER; ++i) {
+      const int row = w * 32 + i * RPI + rr, r = x * 128 + row;
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (r < f.rows) {
+        const int32_t k = (int32_t)fast_div((uint32_t)r, p.group.magic, p.group.shift);
+        v = ld16(row_ptr(p.q, f.q0 + f.tok0 + k, p.q_rs, 2) + ((int64_t)(f.h * p.G + r - k * p.G) * D + c * 8) * 2);
+      }
+      *reinterpret_cast<uint4*>(s.q + x * QB + (c / 8) * QHALF + row * 128 + (((c % 8) ^ (row & 7)) << 4)) = v;
+    }
+    fence_async();
+    mb_arrive(smem_at(&s.q_full[x]));
+  }
+
+  static __device__ __forceinline__ bool softmax(const PagedAttnParams& p, Smem& s, uint32_t tmem, const Frag& f, int x,
+                                                 Soft& st, float* m_out, float* l_out) {
+    const uint32_t lanes = tmem + (((threadIdx.x >> 5) & 3) << 21);  // TMEM lane 32 * (warp mod 4)
+    const uint32_t sc = lanes + S_COL + x * KEYS, oc = lanes + O_COL + x * D;
+    const int r = x * 128 + (threadIdx.x & 127);
+    const int32_t k = (int32_t)fast_div((uint32_t)r, p.group.magic, p.group.shift);
+    const int32_t see = r < f.rows ? f.kv - f.n + f.tok0 + k + 1 : 0;
+    const float c = p.scale * kLog2e;
+    float m = -INFINITY, l = 0.f;
+    for (int32_t t = f.t0; t < f.t1; ++t) {
+      if (!__all_sync(0xffffffffu, mb_wait(smem_at(&s.s_full[x]), st.s & 1, st.s == 0 ? p.first_polls : p.polls, &s.abort)))
+        return false;
+      ++st.s;
+      tc_after();
+      uint32_t a[KEYS];
+#pragma unroll
+      for (int i = 0; i < KEYS / 32; ++i) tc_ld32(sc + i * 32, a + i * 32);
+      tc_wait_ld();
+      const int32_t left = see - t * KEYS;  // keys of the tile that the row sees
+      if (left < KEYS) {
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i)
+          if (i >= left) a[i] = 0xff800000u;  // -inf
+      }
+      float top[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top[i] = __uint_as_float(a[i]);
+#pragma unroll
+      for (int i = 4; i < KEYS; ++i) top[i & 3] = fmaxf(top[i & 3], __uint_as_float(a[i]));
+      const float hi = c * fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+      if (__any_sync(0xffffffffu, hi > m + kLazy)) {
+        const float m2 = fmaxf(m, hi);
+        const float g = m2 == -INFINITY ? 1.f : fast_exp2(m - m2);
+        m = m2;
+        l *= g;
+        if (t > f.t0) {
+#pragma unroll 1
+          for (int i = 0; i < D / 32; ++i) {
+            uint32_t o[32];
+            tc_ld32(oc + i * 32, o);
+            tc_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * g);
+            tc_st32(oc + i * 32, o);
+          }
+        }
+      }
+      const float base = m == -INFINITY ? 0.f : m;
+      const F2 cc = f2_pack(c, c), mm = f2_pack(-base, -base);
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int h = 0; h < KEYS / 64; ++h) {
+        uint32_t w[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const int e = h * 64 + 2 * i;
+          float u, v;
+          f2_unpack(f2_fma(f2_pack(__uint_as_float(a[e]), __uint_as_float(a[e + 1])), cc, mm), &u, &v);
+          u = fast_exp2(u);
+          v = fast_exp2(v);
+          sum[(2 * i) & 3] += u;
+          sum[(2 * i + 1) & 3] += v;
+          w[i] = ActType<DT>::pack2(u, v);
+        }
+        tc_st32(sc + h * 32, w);
+      }
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      tc_wait_st();
+      tc_before();
+      mb_arrive(smem_at(&s.p_full[x]));
+    }
+    *m_out = m;
+    *l_out = l;
+    if (!__all_sync(0xffffffffu, mb_wait(smem_at(&s.o_full[x]), st.o & 1, p.polls, &s.abort))) return false;
+    ++st.o;
+    tc_after();
+    return true;
+  }
+
+  // Row r's place in out, and in lse (*at).
+  static __device__ __forceinline__ char* out_row(const PagedAttnParams& p, const Frag& f, int r, int64_t* at) {
+    const int32_t k = (int32_t)fast_div((uint32_t)r, p.group.magic, p.group.shift);
+    const int64_t t = f.q0 + f.tok0 + k;
+    const int h = f.h * p.G + r - k * p.G;
+    *at = t * p.Hq + h;
+    return row_ptr(p.out, t, p.o_rs, 2) + (int64_t)h * D * 2;
+  }
+  static __device__ __forceinline__ void put_lse(const PagedAttnParams& p, int64_t at, float m, float l) {
+    p.lse[at] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+  }
+
+  // The finished accumulator to out, or unnormalised to a workspace slot: m[ROWS], l[ROWS], then for every
+  // four columns the rows' float4 side by side, so that a warp writes 512 bytes at a time.
+  static __device__ __forceinline__ void finish(const PagedAttnParams& p, uint32_t tmem, const Frag& f, int x, float m,
+                                                float l, float* slot) {
+    const uint32_t oc = tmem + (((threadIdx.x >> 5) & 3) << 21) + O_COL + x * D;
+    const int r = x * 128 + (threadIdx.x & 127);
+    const bool live = r < f.rows;
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    int64_t at = 0;
+    char* out = live ? out_row(p, f, r, &at) : nullptr;
+#pragma unroll 1
+    for (int i = 0; i < D / 32; ++i) {
+      uint32_t o[32];
+      tc_ld32(oc + i * 32, o);
+      tc_wait_ld();
+      if (live && slot) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          *reinterpret_cast<uint4*>(slot + 2 * ROWS + ((i * 8 + e) * ROWS + r) * 4) =
+              make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+      } else if (live) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float v[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) v[q] = __uint_as_float(o[8 * e + q]) * inv;
+          st16(out + (i * 32 + e * 8) * 2, pack<DT>(v));
+        }
+      }
+      __syncwarp();
+    }
+    tc_before();
+    if (!live) return;
+    if (slot) {
+      slot[r] = m;
+      slot[ROWS + r] = l;
+    } else {
+      put_lse(p, at, m, l);
+    }
+  }
+
+  // Joins n slots, a thread per row, to out or (unnormalised) to dst, the first of them.
+  template <class At>
+  static __device__ __forceinline__ void join(const PagedAttnParams& p, const Frag& f, int r, int n, At at, float* dst) {
+    if (r >= f.rows) return;
+    float m = -INFINITY, l = 0.f;
+    for (int i = 0; i < n; ++i) m = fmaxf(m, __ldcg(at(i) + r));
+    const float base = m == -INFINITY ? 0.f : m;
+    float w[kFanIn];
+#pragma unroll
+    for (int i = 0; i < kFanIn; ++i) {
+      w[i] = 0.f;
+      if (i < n) {
+        w[i] = fast_exp2(__ldcg(at(i) + r) - base);
+        l = fmaf(w[i], __ldcg(at(i) + ROWS + r), l);
+      }
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    int64_t row = 0;
+    char* out = out_row(p, f, r, &row);
+#pragma unroll 1
+    for (int d = 0; d < D / 8; ++d) {
+      float v[8] = {};
+#pragma unroll
+      for (int i = 0; i < kFanIn; ++i) {
+        if (i >= n) break;
+        const float* z = at(i) + 2 * ROWS + ((int64_t)2 * d * ROWS + r) * 4;
+        const float4 a = __ldcg(reinterpret_cast<const float4*>(z)), b = __ldcg(reinterpret_cast<const float4*>(z + ROWS * 4));
+        v[0] = fmaf(w[i], a.x, v[0]); v[1] = fmaf(w[i], a.y, v[1]); v[2] = fmaf(w[i], a.z, v[2]); v[3] = fmaf(w[i], a.w, v[3]);
+        v[4] = fmaf(w[i], b.x, v[4]); v[5] = fmaf(w[i], b.y, v[5]); v[6] = fmaf(w[i], b.z, v[6]); v[7] = fmaf(w[i], b.w, v[7]);
+      }
+      if (dst) {
+        float* z = dst + 2 * ROWS + ((int64_t)2 * d * ROWS + r) * 4;
+        *reinterpret_cast<float4*>(z) = make_float4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<float4*>(z + ROWS * 4) = make_float4(v[4], v[5], v[6], v[7]);
+      } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] *= inv;
+        st16(out + d * 16, pack<DT>(v));
+      }
+    }
+    if (dst) {
+      dst[r] = m;
+      dst[ROWS + r] = l;
+    } else {
+      put_lse(p, row, m, l);
+    }
+  }
+
+  // One fragment of a softmax warpgroup. Both warpgroups pass the same named barriers, whatever failed.
+  static __device__ __forceinline__ bool soft_fragment(const PagedAttnParams& p, Smem& s, uint32_t tmem, const Frag& f,
+                                                       int x, Soft& st, bool ok, float* slots, uint32_t* counters) {
+    constexpr int64_t SLOT = attn_slot_floats(ROWS, D);
+    const int r = x * 128 + (threadIdx.x & 127);
+    if (f.limit == 0) {  // no keys: never split
+      if (ok && r < f.rows) {
+        int64_t at;
+        char* out = out_row(p, f, r, &at);
+        for (int d = 0; d < D / 8; ++d) st16(out + d * 16, make_uint4(0, 0, 0, 0));
+        put_lse(p, at, 0.f, 0.f);
+      }
+      return ok;
+    }
+    const AttnCuts cut{f.first, f.last};
+    float* mine = cut.whole() ? nullptr : slots + cut.slot(blockIdx.x) * SLOT;
+    if (x == 0 || f.rows > 128) {
+      if (ok) {
+        load_q(p, s, f, x);
+        float m, l;
+        ok = softmax(p, s, tmem, f, x, st, &m, &l);
+        if (ok) finish(p, tmem, f, x, m, l, mine);
+      }
+    }
+    if (cut.whole()) return ok;
+    // with a block that failed the count is never met, so nobody joins the unit
+    const int n = (int)(cut.last - cut.first + 1), i0 = (int)(blockIdx.x - cut.first);
+    const int groups = (n + kFanIn - 1) / kFanIn, gr = i0 / kFanIn, size = min(kFanIn, n - gr * kFanIn);
+    const int64_t g0 = cut.first + (int64_t)gr * kFanIn;
+    auto slot = [&](int64_t block) { return slots + cut.slot(block) * SLOT; };
+    const bool leader = threadIdx.x == 0;
+    auto done = [&](uint32_t* counter, uint32_t total) {
+      return attn_completes<1, SOFT>(&s.flag, leader, counter, s.abort ? 0xffffffffu : total);
+    };
+    if (done(counters + cut.slot(g0), size)) {
+      join(p, f, r, size, [&](int i) { return slot(g0 + i); }, groups > 1 ? slot(g0) : nullptr);
+      if (groups > 1 && done(counters + 2 * gridDim.x + cut.slot(cut.first), groups))
+        join(p, f, r, groups, [&](int i) { return slot(cut.first + (int64_t)i * kFanIn); }, nullptr);
+    }
+    return ok;
+  }
+
+  // ------------------------------------------------------------ the block
+  static __device__ __forceinline__ void list(const PagedAttnParams& p, Smem& s, int64_t b0, int64_t x, int64_t run,
+                                              const AttnShare& a) {
+    int count = 0;
+    const int64_t end = min(a.hi, run);
+    while (x < end && count < kFrags) {
+      const int rq = Split::find(s.split, x);
+      const Request r{s.split.q0[rq], s.split.n[rq], s.split.kv[rq]};
+      const int32_t nm = Cost::row_tiles(p, r);
+      const int64_t head = Cost::before(p, r, nm), rel = x - s.split.pre[rq];
+      const int32_t h = (int32_t)(rel / head);
+      const int64_t y = rel - h * head;
+      int32_t k = 0, hi = nm;  // the row tile that holds y
+      while (hi - k > 1) {
+        const int32_t mid = (k + hi) / 2;
+        if (Cost::before(p, r, mid) <= y) k = mid;
+        else hi = mid;
+      }
+      Frag& f = s.frag[count++];
+      const int64_t k0 = Cost::before(p, r, k);
+      f.b = b0 + rq;
+      f.q0 = r.q0;
+      f.n = r.n;
+      f.kv = r.kv;
+      f.h = h;
+      f.tok0 = k * Cost::tokens(p);
+      f.rows = min(Cost::tokens(p), r.n - f.tok0) * p.G;
+      f.limit = Cost::sees(p, r, k);
+      const int32_t nt = Cost::key_tiles(f.limit);
+      f.t0 = (int32_t)(y - k0);
+      f.t1 = (int32_t)min((int64_t)nt, f.t0 + (a.hi - x));
+      const int64_t start = x - f.t0;
+      f.first = start / a.per;
+      f.last = (start + nt - 1) / a.per;
+      x += f.t1 - f.t0;
+    }
+    s.count = count;
+    s.x = x;
+  }
+
+  static __device__ __forceinline__ void run(const PagedAttnParams& p, const CUtensorMap* mk, const CUtensorMap* mv, Smem& s) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int MMA_WARP = SOFT / 32, LOAD_WARP = MMA_WARP + 1;
+    if (warp == MMA_WARP) {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_at(&s.tmem)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+      if (lane == 0) {
+        for (int i = 0; i < SLOTS; ++i) {
+          mb_init(smem_at(&s.full[i]), 1);
+          mb_init(smem_at(&s.empty[i]), 1);
+        }
+        mb_init(smem_at(&s.raw), 1);
+        mb_init(smem_at(&s.drain), 1);
+        for (int x = 0; x < NT; ++x) {
+          mb_init(smem_at(&s.q_full[x]), 128);
+          mb_init(smem_at(&s.s_full[x]), 1);
+          mb_init(smem_at(&s.p_full[x]), 128);
+          mb_init(smem_at(&s.o_full[x]), 1);
+        }
+        s.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      }
+      __syncwarp();
+      tc_before();
+    }
+    pdl_wait();
+    pdl_trigger();  // after the wait: a launch that starts early then finds everything before this one done
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = s.tmem;
+    const AttnShare a = Split::share(p, s.split);
+    attn_fill_tail<THREADS>(p);
+    uint32_t* counters = reinterpret_cast<uint32_t*>(p.work);
+    float* slots = p.work + attn_counters(gridDim.x);
+    Load ld;
+    Mma mm;
+    Soft so;
+    bool ok = true;
+    int64_t run = 0, x = a.lo;
+    for (int64_t b0 = 0; b0 < p.B && x < a.hi; b0 += THREADS) {
+      run = Split::chunk(p, s.split, b0, run);
+      while (x < a.hi && x < run) {
+        if (threadIdx.x == 0) list(p, s, b0, x, run, a);
+        __syncthreads();
+        const int count = s.count;
+        x = s.x;
+        for (int i = 0; i < count; ++i) {
+          const Frag& f = s.frag[i];
+          if (warp < MMA_WARP) {
+            ok = soft_fragment(p, s, tmem, f, warp / 4, so, ok, slots, counters);
+          } else if (f.limit > 0 && ok) {
+            if (warp == LOAD_WARP) {
+              ok = load(p, mk, mv, s, f, ld);
+            } else if (lane == 0) {
+              ok = mma(p, s, tmem, f, mm);
+            }
+          }
+        }
+        __syncwarp();
+        __syncthreads();
+      }
+    }
+    // the way out: every copy and product of the block has to be done before its memory is given back
+    if (warp == LOAD_WARP) {
+      for (uint32_t i = ld.issued > SLOTS ? ld.issued - SLOTS : 0; i < ld.issued; ++i) {
+        mb_drain(smem_at(&s.full[i % SLOTS]), (i / SLOTS) & 1);
+        if (ok) mb_drain(smem_at(&s.empty[i % SLOTS]), (i / SLOTS) & 1);
+      }
+      if (ld.bad) atomicOr(p.err, kErrTable);
+    }
+    if (warp == MMA_WARP && lane == 0) {
+      tc_commit(smem_at(&s.drain));
+      mb_drain(smem_at(&s.drain), 0);
+    }
+    __syncwarp();
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (threadIdx.x == 0 && s.abort) atomicOr(p.err, kErrTimeout);
+    if (warp == MMA_WARP)
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");
+  }
+};
+
+template <class K>
+__global__ void __launch_bounds__(K::THREADS, 1)
+attn_tile_kernel(const __grid_constant__ PagedAttnParams p, const __grid_constant__ CUtensorMap mk,
+                 const __grid_constant__ CUtensorMap mv) {
+  extern __shared__ __align__(128) char smem[];
+  char* at = smem + (1024 - (smem_at(smem) & 1023)) % 1024;  // swizzle atoms start at multiples of 1024
+  K::run(p, &mk, &mv, *reinterpret_cast<typename K::Smem*>(at));
+}
+
+template <class K>
+void pick(AttnEntry* e) {
+  e->fn = (const void*)attn_tile_kernel<K>;
+  e->threads = K::THREADS;
+  e->smem = sizeof(typename K::Smem) + 1024;
+  e->per_sm = 1;
+  e->slot_floats = attn_slot_floats(K::ROWS, K::D);
+  e->keys = K::KEYS;
+  e->rows = K::ROWS;
+  static_assert(sizeof(typename K::Smem) + 1024 <= 232448, "shared memory of a block");
+}
+
+}  // namespace
+
+bool attn_tile_entry(int32_t dtype, int32_t D, AttnEntry* e) {
+  *e = AttnEntry{};
+  if (D == 64) dtype == DT_BF16 ? pick<Tile<DT_BF16, 64, 2, 128, 8>>(e) : pick<Tile<DT_FP16, 64, 2, 128, 8>>(e);
+  else if (D == 128) dtype == DT_BF16 ? pick<Tile<DT_BF16, 128, 2, 128, 4>>(e) : pick<Tile<DT_FP16, 128, 2, 128, 4>>(e);
+  else if (D == 256) dtype == DT_BF16 ? pick<Tile<DT_BF16, 256, 1, 64, 4>>(e) : pick<Tile<DT_FP16, 256, 1, 64, 4>>(e);
+  return e->fn != nullptr;
+}
+
+}  // namespace trident

@@ -221,6 +221,7 @@ struct PagedAttnParams {
   FastDiv page, group;  // by ps; by G = Hq / Hkv
   int64_t rows_above, rows_upto;  // this launch takes the requests of rows_above < n * G <= rows_upto
   int64_t min_tiles;              // a block's run of key tiles is at least this long
+  uint32_t polls, first_polls;    // tile kernel: bounds of its waits, of a warp's first for scores
 };
 
 // Elementwise entries (pointwise_plan): flat and rows kernels with one or two vectors per
@@ -243,6 +244,7 @@ struct AttnEntry {
   const void* fn = nullptr;
   int32_t threads = 0, smem = 0, per_sm = 0;
   int64_t slot_floats = 0;
+  int32_t keys = 0, rows = 0;  // tile kernel: keys and rows of a tile
 };
 
 // Kernel entry (host stub address) plus its launch shape rule.
@@ -272,7 +274,8 @@ struct KernelEntry {
   int32_t threads = 0;   // chain: block size
   const void* nm_fn[kNormEntries] = {};  // norms, by NormEntry (NULL: none for this H)
   int32_t nm_threads[kNormEntries] = {};
-  AttnEntry attn_rows;   // paged attention: requests of few rows
+  AttnEntry attn_rows;   // paged attention: requests of few rows,
+  AttnEntry attn_tile;   // ... and of many
   int32_t rows = 1;      // norms: rows per block of the NM_VEC entry
   int32_t edge_rows = 1;  // ... and of the NM_EDGE_MANY entry,
   int64_t edge_many = 0;  // which calls of at least this many rows take (on 152 SMs)
@@ -354,6 +357,15 @@ bool rope_paged_kernel(int32_t dtype, int32_t variant, int32_t D, int32_t R, boo
 // Which any_fn entry a vector call takes; sets its item split, block size and grid.
 int rope_paged_plan(RopePagedParams* p, int32_t* threads, int64_t* blocks, int32_t sms);
 bool attn_rows_entry(int32_t dtype, int32_t D, AttnEntry* e);
+bool attn_tile_entry(int32_t dtype, int32_t D, AttnEntry* e);
+// Which attention kernels a call of T rows and B requests takes: the one of few rows, the tile kernel,
+// or both, each for its requests (of at most, of more than kTileRows rows; row: token and head of a group).
+constexpr int64_t kTileRows = 128;
+constexpr int64_t kRowsRun = 4, kTileRun = 4;  // key tiles of a block's run at least
+struct AttnPlan {
+  bool rows, tile;
+};
+AttnPlan attn_plan(const AttnEntry& tile, int64_t T, int64_t B, int64_t G, int64_t ps);
 int64_t attn_work_floats(const AttnEntry& e, int32_t sms);
 bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, KernelEntry* out, const char** why);
 const void* empty_kernel_entry();  // the latency-floor probe's kernel (does nothing)

@@ -82,6 +82,7 @@ struct Driver {
   CUresult (*ctx_get)(CUcontext*) = nullptr;
   CUresult (*ctx_push)(CUcontext) = nullptr;
   CUresult (*ctx_pop)(CUcontext*) = nullptr;
+  decltype(&cuTensorMapEncodeTiled) encode = nullptr;
   bool ok = false;
 };
 Driver g_drv;
@@ -103,7 +104,8 @@ bool driver() {
     g_drv.ctx_get = reinterpret_cast<decltype(g_drv.ctx_get)>(get("cuCtxGetCurrent"));
     g_drv.ctx_push = reinterpret_cast<decltype(g_drv.ctx_push)>(get("cuCtxPushCurrent"));
     g_drv.ctx_pop = reinterpret_cast<decltype(g_drv.ctx_pop)>(get("cuCtxPopCurrent"));
-    g_drv.ok = ok && g_drv.launch_ex && g_drv.ctx_get && g_drv.ctx_push && g_drv.ctx_pop;
+    g_drv.encode = reinterpret_cast<decltype(g_drv.encode)>(get("cuTensorMapEncodeTiled"));
+    g_drv.ok = ok && g_drv.encode && g_drv.launch_ex && g_drv.ctx_get && g_drv.ctx_push && g_drv.ctx_pop;
   });
   return g_drv.ok;
 }
@@ -571,6 +573,7 @@ struct Version {
   RopeSplit rope_split[2];      // layer chain: item splits with one and kChainRopeRows rows
   CUfunction pw_fn[kPwEntries];  // elementwise: entries by layout and size (pointwise_plan)
   CUfunction any_fn[2];            // RoPE versions of the generic kind: rope_any_kernel
+  CUfunction attn_tile_fn;       // paged attention: the kernel of many rows
   CUfunction nm_fn[kNormEntries];  // norms: entries by layout and size (norm_plan)
   CUfunction step_fn;           // layer chain: several calls per launch (two blocks per token)
   CUfunction step_fn_inplace;   // ... one block per token
@@ -994,6 +997,18 @@ void pack_paged_attn(const trident_args* a, const Sig& s, uint32_t* err, PagedAt
   p->group = fast_divisor(p->G);
 }
 
+// The tensor map of a paged cache for boxes of 64 elements and a page's rows (at most `keys`).
+bool tile_map(CUtensorMap* m, const trident_tensor& t, int32_t dtype, int32_t keys) {
+  const cuuint64_t dims[4] = {(cuuint64_t)t.shape[3], (cuuint64_t)t.shape[2], (cuuint64_t)t.shape[1], (cuuint64_t)t.shape[0]};
+  cuuint64_t strides[3];  // bytes; of a dimension of one, which no coordinate leaves, any valid value
+  for (int k = 0; k < 3; ++k)
+    strides[k] = t.shape[2 - k] > 1 ? (cuuint64_t)t.stride[2 - k] * 2 : (cuuint64_t)t.shape[3] * 2;
+  const cuuint32_t box[4] = {64, (cuuint32_t)(t.shape[2] < keys ? t.shape[2] : keys), 1, 1}, step[4] = {1, 1, 1, 1};
+  return g_drv.encode(m, dtype == TRIDENT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+                      t.data, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Launch of a paged op. Counts that index in 32 bits are bounded here; bytes are indexed in 64.
 int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, const Sig& s, void* stream) {
   CUlaunchConfig cfg;
@@ -1036,14 +1051,36 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
     cfg.gridDimX = cap_grid((s.T * p.Hq + kThreads / 32 - 1) / (kThreads / 32));
     return launch_on(scm, &cfg, v.fn, kp);
   }
-  if (a->t[6].shape[0] < attn_work_floats(v.ke.attn_rows, scm->sm_count))
+  const AttnEntry &rows = v.ke.attn_rows, &tile = v.ke.attn_tile;
+  const int64_t rows_work = attn_work_floats(rows, scm->sm_count);
+  if (a->t[6].shape[0] < rows_work + attn_work_floats(tile, scm->sm_count))
     return fail(TRIDENT_ERR_INVALID, "the workspace is smaller than trident_scm_workspace says");
+  p.polls = kBulkWaitPolls;
+  p.first_polls = (scm->opt.flags & TRIDENT_OPT_TEST_WAIT_TIMEOUT) ? 0u : kBulkWaitPolls;
+  const AttnPlan pl = attn_plan(tile, s.T, p.B, p.G, p.page.d);
+  if (pl.tile) {
+    CUtensorMap mk, mv;
+    if (!tile_map(&mk, a->t[1], v.d.dtype, tile.keys) || !tile_map(&mv, a->t[2], v.d.dtype, tile.keys))
+      return fail(TRIDENT_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+    PagedAttnParams q = p;
+    q.work += rows_work;
+    q.rows_above = pl.rows ? kTileRows : 0;
+    q.rows_upto = INT64_MAX;
+    q.min_tiles = kTileRun;
+    void* tp[3] = {&q, &mk, &mv};
+    cfg.blockDimX = (unsigned)tile.threads;
+    cfg.gridDimX = (unsigned)(scm->sm_count * tile.per_sm);
+    cfg.sharedMemBytes = (unsigned)tile.smem;
+    const int32_t st = launch_on(scm, &cfg, v.attn_tile_fn, tp);
+    if (st != TRIDENT_OK) return st;
+  }
+  if (!pl.rows) return TRIDENT_OK;
   p.rows_above = 0;
-  p.rows_upto = INT64_MAX;
-  p.min_tiles = 4;
-  cfg.blockDimX = (unsigned)v.ke.attn_rows.threads;
-  cfg.gridDimX = (unsigned)(scm->sm_count * v.ke.attn_rows.per_sm);
-  cfg.sharedMemBytes = (unsigned)v.ke.attn_rows.smem;
+  p.rows_upto = pl.tile ? kTileRows : INT64_MAX;
+  p.min_tiles = kRowsRun;
+  cfg.blockDimX = (unsigned)rows.threads;
+  cfg.gridDimX = (unsigned)(scm->sm_count * rows.per_sm);
+  cfg.sharedMemBytes = (unsigned)rows.smem;
   return launch_on(scm, &cfg, v.fn, kp);
 }
 
@@ -1609,15 +1646,17 @@ int32_t append_version(trident_scm_t* scm, const trident_spec_desc* desc, int32_
           cudaFuncSetAttribute(v.ke.nm_fn[NM_LARGE], cudaFuncAttributeMaxDynamicSharedMemorySize,
                                2 * kNormBlockVecs * 16) != cudaSuccess)
         return fail(TRIDENT_ERR_CUDA, "cannot set the norm kernel's shared-memory size");
-      if (v.ke.attn_rows.fn && cudaFuncSetAttribute(v.ke.attn_rows.fn, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                    v.ke.attn_rows.smem) != cudaSuccess)
-        return fail(TRIDENT_ERR_CUDA, "cannot set the attention kernel's shared-memory size");
+      for (const AttnEntry* e : {&v.ke.attn_rows, &v.ke.attn_tile})
+        if (e->fn && cudaFuncSetAttribute(e->fn, cudaFuncAttributeMaxDynamicSharedMemorySize, e->smem) != cudaSuccess)
+          return fail(TRIDENT_ERR_CUDA, "cannot set the attention kernel's shared-memory size");
       auto resolve = [&](const void* entry, CUfunction* out_fn) {
         cudaFunction_t e = nullptr;
         if (entry && (cudaGetFuncBySymbol(&e, entry) != cudaSuccess || !e)) return false;
         *out_fn = reinterpret_cast<CUfunction>(e);
         return true;
       };
+      if (!resolve(v.ke.attn_tile.fn, &v.attn_tile_fn))
+        return fail(TRIDENT_ERR_CUDA, "cannot resolve the attention kernel entries");
       for (int k = 0; k < kPwEntries; ++k)
         if (!resolve(v.ke.pw_fn[k], &v.pw_fn[k]))
           return fail(TRIDENT_ERR_CUDA, "cannot resolve the elementwise kernel entries");
@@ -1725,7 +1764,8 @@ TRIDENT_API int32_t trident_scm_workspace(const trident_scm_t* scm, int32_t inde
   if (index < 0 || index >= scm->count.load(std::memory_order_acquire))
     return fail(TRIDENT_ERR_INVALID, "no version %d", index);
   if (scm->dry) return fail(TRIDENT_ERR_STATE, "a dry-run SCM has no device to size a workspace for");
-  *out = attn_work_floats(scm->versions[index].ke.attn_rows, scm->sm_count);
+  const KernelEntry& ke = scm->versions[index].ke;
+  *out = attn_work_floats(ke.attn_rows, scm->sm_count) + attn_work_floats(ke.attn_tile, scm->sm_count);
   return TRIDENT_OK;
 }
 
