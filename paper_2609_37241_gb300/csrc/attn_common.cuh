@@ -89,7 +89,7 @@ __device__ __forceinline__ bool attn_takes(const PagedAttnParams& p, int32_t n) 
 
 // One block's share of the call: tiles per block and this block's run [lo, hi).
 struct AttnShare {
-  int64_t per, lo, hi;
+  int64_t per, lo, hi, total;
 };
 
 // Cost::of(p, r): the key tiles of all of request r's units, at least one per unit so that a unit
@@ -106,20 +106,26 @@ struct AttnSplit {
     return attn_takes(p, r.n) ? Cost::of(p, r) : 0;
   }
 
+  // The block's share; with at most NT requests their chunk is filled as well.
   static __device__ __forceinline__ AttnShare share(const PagedAttnParams& p, Smem& s) {
-    bool ok = true;
     long long sum = 0;
-    for (int64_t b = threadIdx.x; b < p.B; b += NT) sum += cost(p, attn_request(p, b, &ok));
-    if (!ok && blockIdx.x == 0) atomicOr(p.err, kErrTable);
+    if (p.B <= NT) {
+      sum = chunk(p, s, 0, 0);
+    } else {
+      bool ok = true;
+      for (int64_t b = threadIdx.x; b < p.B; b += NT) sum += cost(p, attn_request(p, b, &ok));
+      if (!ok && blockIdx.x == 0) atomicOr(p.err, kErrTable);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if ((threadIdx.x & 31) == 0) s.warp[threadIdx.x >> 5] = sum;
-    __syncthreads();
-    sum = 0;
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      if ((threadIdx.x & 31) == 0) s.warp[threadIdx.x >> 5] = sum;
+      __syncthreads();
+      sum = 0;
 #pragma unroll
-    for (int w = 0; w < NT / 32; ++w) sum += s.warp[w];
+      for (int w = 0; w < NT / 32; ++w) sum += s.warp[w];
+    }
     const int64_t even = (sum + gridDim.x - 1) / gridDim.x;
     AttnShare a;
+    a.total = sum;
     a.per = even > p.min_tiles ? even : p.min_tiles;
     a.lo = min((int64_t)sum, (int64_t)blockIdx.x * a.per);
     a.hi = min((int64_t)sum, a.lo + a.per);
@@ -132,6 +138,7 @@ struct AttnSplit {
     bool ok = true;
     Request r{0, 0, 0};
     if (b < p.B) r = attn_request(p, b, &ok);
+    if (!ok && blockIdx.x == 0) atomicOr(p.err, kErrTable);
     const long long own = cost(p, r);
     long long v = own;
 #pragma unroll

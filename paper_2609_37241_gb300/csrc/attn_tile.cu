@@ -1,8 +1,8 @@
 // attn_tile.cu -- paged attention for requests of many rows: chunks of a prompt.
 //
 // Bound: the tensor cores. A unit is NT tiles of 128 rows (tokens x the G heads of a group, so that all of
-// them share the keys' loads) against tiles of KEYS keys; per block NT softmax warpgroups, one warp that
-// issues tcgen05.mma and one that loads:
+// them share the keys' loads) against tiles of KEYS keys; per block NT softmax warpgroups, NT warps that
+// issue tcgen05.mma and one that loads:
 //   load     k and v tiles by TMA, a box per page, into a ring of KEYS x D slots in the 128-byte swizzle;
 //            a unit's last v tile gets zeros in the rows past the last key up to the next 16 (a pool's
 //            unused rows may hold NaN, and 0 * NaN would reach the sums)
@@ -71,19 +71,28 @@ __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sy
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-  asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }"
-               :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+// One lane of the warp, the same one each time.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t is;
+  asm volatile("{ .reg .pred q; elect.sync _|q, 0xffffffff; selp.u32 %0, 1, 0, q; }" : "=r"(is));
+  return is != 0;
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+// D = A B (+ D where add): A and B by descriptor, or A in TMEM.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }"
+               :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
   asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
-               :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+               :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
 }
 // Shared-memory operand descriptor, 128-byte swizzle (layout code 2, bits 61-63; version 1, bits 46-48):
-// start, leading and stride byte offsets in units of 16.
-__device__ __forceinline__ uint64_t desc128(uint32_t at, uint32_t leading, uint32_t stride) {
-  return (uint64_t)((at >> 4) & 0x3fff) | ((uint64_t)(leading >> 4) << 16) | ((uint64_t)(stride >> 4) << 32) |
-         (1ull << 46) | (2ull << 61);
+// start, leading and stride byte offsets in units of 16. The start is in the low word's first 14 bits, so
+// a step inside a tile is an addition there.
+__device__ __forceinline__ uint32_t desc_lo(uint32_t at, uint32_t leading) { return (at >> 4) | ((leading >> 4) << 16); }
+__device__ __forceinline__ uint64_t desc128(uint32_t lo) {  // stride: 1024, eight rows of 128 bytes
+  constexpr uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+  return ((uint64_t)hi << 32) | lo;
 }
 // Instruction descriptor of kind::f16: fp32 accumulators, A and B of the activation type, both K-major
 // unless b_mn, M x N.
@@ -107,19 +116,35 @@ __device__ __forceinline__ void tc_st32(uint32_t at, const uint32_t* r) {
                :: TC_I8(r, 0), TC_I8(r, 8), TC_I8(r, 16), TC_I8(r, 24), "r"(at) : "memory");
 }
 
+__device__ __forceinline__ void tc_st16(uint32_t at, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+               :: TC_I8(r, 0), TC_I8(r, 8), "r"(at) : "memory");
+}
+__device__ __forceinline__ F2 f2_add(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+
 // ---------------------------------------------------------------- units
-// sum of floor((a i + b) / m) for i < n; a, b >= 0 (the Euclid-like reduction of lattice-point counts).
-__device__ __forceinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
+// sum of floor((a i + b) / m) for i < n (the Euclid-like reduction of lattice-point counts), for
+// a n + b + m < 2^32.
+__device__ __forceinline__ int64_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
   int64_t total = 0;
   while (n > 0) {
-    total += n * (n - 1) / 2 * (a / m) + n * (b / m);
-    a %= m;
-    b %= m;
-    const int64_t y = a * n + b;  // the last term's numerator is y - a
+    if (a >= m) {
+      total += (int64_t)n * (n - 1) / 2 * (a / m);
+      a %= m;
+    }
+    if (b >= m) {
+      total += (int64_t)n * (b / m);
+      b %= m;
+    }
+    const uint32_t y = a * n + b;  // the last term's numerator is y - a
     if (y < m) break;
     n = y / m;
     b = y % m;
-    const int64_t t = m;
+    const uint32_t t = m;
     m = a;
     a = t;
   }
@@ -142,15 +167,15 @@ struct TileCost {
   }
   // Key tiles of the first k row tiles of one kv head.
   static __device__ __forceinline__ int64_t before(const PagedAttnParams& p, const Request& r, int32_t k) {
-    const int64_t c = (int64_t)r.kv - r.n, R = tokens(p);
-    int64_t full = k;  // row tiles that end at a whole R
+    const int32_t c = r.kv - r.n, R = tokens(p);
+    int32_t full = k;  // row tiles that end at a whole R
     int64_t total = 0;
     if (k == row_tiles(p, r) && k > 0) {
       --full;
       total = key_tiles(sees(p, r, k - 1));
     }
     if (c >= 0) return total + floor_sum(full, KEYS, R, c + R + KEYS - 1);
-    for (int64_t i = 0; i < full; ++i) total += key_tiles(sees(p, r, (int32_t)i));
+    for (int32_t i = 0; i < full; ++i) total += key_tiles(sees(p, r, i));
     return total;
   }
   static __device__ __forceinline__ int64_t of(const PagedAttnParams& p, const Request& r) {
@@ -169,7 +194,12 @@ struct Tile {
   static constexpr int DT = DT_, D = D_, NT = NT_, KEYS = KEYS_, SLOTS = SLOTS_;
   static constexpr int ROWS = 128 * NT;
   static constexpr int SOFT = 128 * NT;        // softmax threads
-  static constexpr int THREADS = SOFT + 64;
+  static constexpr int THREADS = SOFT + 128;   // mma, load and idle warps: a warpgroup, for setmaxnreg
+  // Registers: a softmax row takes its 128 scores and their numerators' words, the other warps few. The
+  // launch gives every thread kLaunchRegs; SOFT * kSoftRegs + 128 * kOtherRegs is below that in total.
+  static constexpr int LAUNCH_REGS = 65536 / THREADS / 8 * 8, OTHER_REGS = 88;
+  static constexpr int SOFT_REGS = NT == 2 ? 208 : 232;
+  static_assert(SOFT * SOFT_REGS + 128 * OTHER_REGS <= THREADS * (LAUNCH_REGS < 255 ? LAUNCH_REGS : 248), "register split");
   static constexpr int QB = 128 * D * 2;       // bytes of a q tile
   static constexpr int KB = KEYS * D * 2;      // ... of a k or v tile
   static constexpr int QHALF = 128 * 128, KHALF = KEYS * 128;  // bytes of 64 columns
@@ -180,7 +210,7 @@ struct Tile {
   struct Smem {
     alignas(1024) char q[NT * QB];
     alignas(1024) char ring[SLOTS * KB];
-    alignas(8) uint64_t full[SLOTS], empty[SLOTS], raw, q_full[NT], s_full[NT], p_full[NT], o_full[NT], drain;
+    alignas(8) uint64_t full[SLOTS], empty[SLOTS], raw, q_full[NT], s_full[NT], p_half[NT], p_full[NT], o_full[NT], drain;
     uint32_t tmem;
     volatile int abort, flag;
     int count;
@@ -250,63 +280,79 @@ struct Tile {
     __syncwarp();
   }
 
-  // ------------------------------------------------------------ mma warp (one lane)
+  // ------------------------------------------------------------ mma warps, one per q tile
   struct Mma {
-    uint32_t taken = 0;                 // slots consumed so far
-    uint32_t px[NT] = {}, qx[NT] = {};  // p and q tiles waited for
+    uint32_t taken = 0;      // slots consumed so far
+    uint32_t px = 0, qx = 0;  // p and q tiles waited for
   };
-  static __device__ __forceinline__ void qk(Smem& s, uint32_t tmem, int x, uint32_t slot) {
+  static __device__ __forceinline__ void qk(uint32_t q_lo, uint32_t k_lo, uint32_t d) {
     constexpr uint32_t id = idesc_of<DT>(128, KEYS, false);
-    const uint32_t qa = smem_at(s.q + x * QB), ka = smem_at(s.ring + slot * KB);
 #pragma unroll
     for (int k = 0; k < D / 16; ++k)
-      mma_ss(tmem + S_COL + x * KEYS, desc128(qa + (k / 4) * QHALF + (k % 4) * 32, 16, 1024),
-             desc128(ka + (k / 4) * KHALF + (k % 4) * 32, 16, 1024), id, k > 0);
+      mma_ss(d, desc128(q_lo + ((k / 4 * QHALF + k % 4 * 32) >> 4)), desc128(k_lo + ((k / 4 * KHALF + k % 4 * 32) >> 4)), id,
+             k > 0);
   }
-  static __device__ __forceinline__ void pv(Smem& s, uint32_t tmem, int x, uint32_t slot, int steps, bool add) {
+  // Half of P V: 16-key steps [HALF * KEYS / 32, ...), at most `steps` of the tile's.
+  template <int HALF>
+  static __device__ __forceinline__ void pv(uint32_t p_col, uint32_t v_lo, uint32_t d, int steps, bool add) {
     constexpr uint32_t id = idesc_of<DT>(128, D, true);
-    const uint32_t va = smem_at(s.ring + slot * KB);
-    for (int k = 0; k < steps; ++k)
-      mma_ts(tmem + O_COL + x * D, tmem + S_COL + x * KEYS + k * 8, desc128(va + k * 2048, KHALF, 1024), id, add || k > 0);
-  }
-  static __device__ __forceinline__ bool mma(const PagedAttnParams& p, Smem& s, uint32_t tmem, const Frag& f, Mma& st) {
-    const int tiles = f.rows > 128 ? NT : 1;
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return mb_wait(smem_at(bar), parity, p.polls, &s.abort); };
-    auto slot_ready = [&](uint32_t i) { return wait(&s.full[i % SLOTS], (i / SLOTS) & 1); };
+    constexpr int N = KEYS / 32, K0 = HALF * N;
+    if (steps >= K0 + N) {
 #pragma unroll
-    for (int x = 0; x < NT; ++x)
-      if (x < tiles && !wait(&s.q_full[x], st.qx[x]++ & 1)) return false;
-    uint32_t k = st.taken;  // slot of the current k tile; v: the next
-    if (!slot_ready(k)) return false;
-    tc_after();
-    for (int x = 0; x < tiles; ++x) {
-      qk(s, tmem, x, k % SLOTS);
-      tc_commit(smem_at(&s.s_full[x]));
+      for (int k = K0; k < K0 + N; ++k) mma_ts(d, p_col + k * 8, desc128(v_lo + k * (2048 >> 4)), id, k > 0 || add);
+    } else {
+      for (int k = K0; k < steps; ++k) mma_ts(d, p_col + k * 8, desc128(v_lo + k * (2048 >> 4)), id, k > 0 || add);
     }
-    tc_commit(smem_at(&s.empty[k % SLOTS]));
-    for (int32_t t = f.t0; t < f.t1; ++t) {
-      const uint32_t v = k + 1;
-      const bool more = t + 1 < f.t1;
-      const int steps = (min(KEYS, f.limit - t * KEYS) + 15) / 16;
-      if (!slot_ready(v)) return false;
-#pragma unroll
-      for (int x = 0; x < NT; ++x) {
-        if (x >= tiles) break;
-        if (!wait(&s.p_full[x], st.px[x]++ & 1)) return false;
-        tc_after();
-        pv(s, tmem, x, v % SLOTS, steps, t > f.t0);
-        if (x == tiles - 1) tc_commit(smem_at(&s.empty[v % SLOTS]));
+  }
+  static __device__ __forceinline__ bool mma(const PagedAttnParams& p, Smem& s, uint32_t tmem, const Frag& f, int x, Mma& st,
+                                             bool one) {
+    const int32_t t0 = f.t0, t1 = f.t1, limit = f.limit;
+    const uint32_t q_lo = desc_lo(smem_at(s.q + x * QB), 16), k_lo = desc_lo(smem_at(s.ring), 16),
+                   v_lo = desc_lo(smem_at(s.ring), KHALF);
+    const uint32_t sc = tmem + S_COL + x * KEYS, oc = tmem + O_COL + x * D;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      return __all_sync(0xffffffffu, mb_wait(smem_at(bar), parity, p.polls, &s.abort));
+    };
+    auto slot_ready = [&](uint32_t i) { return wait(&s.full[i % SLOTS], (i / SLOTS) & 1); };
+    uint32_t k = st.taken;  // slot of the current k tile; the v tile's is the next
+    if (x > 0 && f.rows <= 128 * x) {  // nothing to do but to give the slots back
+      for (; k < st.taken + 2 * (uint32_t)(t1 - t0); ++k) {
+        if (!slot_ready(k)) return false;
+        if (one) mb_arrive(smem_at(&s.empty[k % SLOTS]));
+      }
+      st.taken = k;
+      return true;
+    }
+    if (!wait(&s.q_full[x], st.qx++ & 1) || !slot_ready(k)) return false;
+    tc_after();
+    if (one) {
+      qk(q_lo, k_lo + k % SLOTS * (KB >> 4), sc);
+      tc_commit(smem_at(&s.s_full[x]));
+      tc_commit(smem_at(&s.empty[k % SLOTS]));
+    }
+    for (int32_t t = t0; t < t1; ++t) {
+      const uint32_t v = k + 1, next = k + 2, parity = st.px++ & 1;
+      const bool more = t + 1 < t1, add = t > t0;
+      const int steps = (min(KEYS, limit - t * KEYS) + 15) / 16;
+      const uint32_t v_at = v_lo + v % SLOTS * (KB >> 4), k_at = k_lo + next % SLOTS * (KB >> 4);
+      if (!slot_ready(v) || (more && !slot_ready(next))) return false;
+      if (!wait(&s.p_half[x], parity)) return false;
+      tc_after();
+      if (one) pv<0>(sc, v_at, oc, steps, add);
+      if (!wait(&s.p_full[x], parity)) return false;
+      tc_after();
+      if (one) {
+        pv<1>(sc, v_at, oc, steps, add);
         if (more) {
-          if (x == 0 && !slot_ready(v + 1)) return false;
-          tc_after();
-          qk(s, tmem, x, (v + 1) % SLOTS);
+          qk(q_lo, k_at, sc);
           tc_commit(smem_at(&s.s_full[x]));
-          if (x == tiles - 1) tc_commit(smem_at(&s.empty[(v + 1) % SLOTS]));
+          tc_commit(smem_at(&s.empty[next % SLOTS]));
         } else {
           tc_commit(smem_at(&s.o_full[x]));
         }
+        tc_commit(smem_at(&s.empty[v % SLOTS]));
       }
-      k += 2;
+      k = next;
     }
     st.taken = k;
     return true;
@@ -315,102 +361,130 @@ struct Tile {
   // ------------------------------------------------------------ softmax warpgroup
   struct Soft {
     uint32_t s = 0, o = 0;  // tiles and fragments waited for
+    bool q_ready = false;   // the next fragment's q has been loaded
   };
   // Loads this warpgroup's q rows into the swizzled tile: 16 bytes per lane, D / 8 lanes per row.
   static __device__ __forceinline__ void load_q(const PagedAttnParams& p, Smem& s, const Frag& f, int x) {
     constexpr int CH = D / 8, RPI = 32 / CH > 0 ? 32 / CH : 1, ITER = 32 / RPI;
     const int w = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, c = lane % CH, rr = lane / CH;
-#pragma unroll 8
-    for (int i = 0; i < ITER; ++i) {
-      const int row = w * 32 + i * RPI + rr, r = x * 128 + row;
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (r < f.rows) {
+    constexpr int BATCH = 8;  // loads in flight, none behind a branch: rows past the unit load its last and drop it
+#pragma unroll 1
+    for (int i = 0; i < ITER; i += BATCH) {
+      uint4 v[BATCH];
+#pragma unroll
+      for (int e = 0; e < BATCH; ++e) {
+        const int r = min(x * 128 + w * 32 + (i + e) * RPI + rr, f.rows - 1);
         const int32_t k = (int32_t)fast_div((uint32_t)r, p.group.magic, p.group.shift);
-        v = ld16(row_ptr(p.q, f.q0 + f.tok0 + k, p.q_rs, 2) + ((int64_t)(f.h * p.G + r - k * p.G) * D + c * 8) * 2);
+        v[e] = ld16(row_ptr(p.q, f.q0 + f.tok0 + k, p.q_rs, 2) + ((int64_t)(f.h * p.G + r - k * p.G) * D + c * 8) * 2);
       }
-      *reinterpret_cast<uint4*>(s.q + x * QB + (c / 8) * QHALF + row * 128 + (((c % 8) ^ (row & 7)) << 4)) = v;
+#pragma unroll
+      for (int e = 0; e < BATCH; ++e) {
+        const int row = w * 32 + (i + e) * RPI + rr;
+        if (x * 128 + row >= f.rows) v[e] = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(s.q + x * QB + (c / 8) * QHALF + row * 128 + (((c % 8) ^ (row & 7)) << 4)) = v[e];
+      }
     }
     fence_async();
     mb_arrive(smem_at(&s.q_full[x]));
   }
 
+  // The two warpgroups take turns (named barriers 2 and 3; every thread passes them as often, whatever
+  // failed): one makes the numerators of its tile while the other's products run. Without turns they fall
+  // into step, both in their softmax and then both waiting for the tensor cores.
+  static __device__ __forceinline__ void turn_wait(int x) { asm volatile("bar.sync %0, 256;" :: "r"(2 + x) : "memory"); }
+  static __device__ __forceinline__ void turn_pass(int x) { asm volatile("bar.arrive %0, 256;" :: "r"(3 - x) : "memory"); }
+
   static __device__ __forceinline__ bool softmax(const PagedAttnParams& p, Smem& s, uint32_t tmem, const Frag& f, int x,
-                                                 Soft& st, float* m_out, float* l_out) {
+                                                 Soft& st, bool ok, float* m_out, float* l_out) {
     const uint32_t lanes = tmem + (((threadIdx.x >> 5) & 3) << 21);  // TMEM lane 32 * (warp mod 4)
     const uint32_t sc = lanes + S_COL + x * KEYS, oc = lanes + O_COL + x * D;
     const int r = x * 128 + (threadIdx.x & 127);
     const int32_t k = (int32_t)fast_div((uint32_t)r, p.group.magic, p.group.shift);
     const int32_t see = r < f.rows ? f.kv - f.n + f.tok0 + k + 1 : 0;
     const float c = p.scale * kLog2e;
+    const bool turns = NT == 2 && f.rows > 128;
+    const int32_t t0 = f.t0, t1 = f.t1;
     float m = -INFINITY, l = 0.f;
-    for (int32_t t = f.t0; t < f.t1; ++t) {
-      if (!__all_sync(0xffffffffu, mb_wait(smem_at(&s.s_full[x]), st.s & 1, st.s == 0 ? p.first_polls : p.polls, &s.abort)))
-        return false;
+    if (turns && x == 1) turn_pass(1);
+    for (int32_t t = t0; t < t1; ++t) {
+      ok = ok && __all_sync(0xffffffffu, mb_wait(smem_at(&s.s_full[x]), st.s & 1, st.s == 0 ? p.first_polls : p.polls, &s.abort));
       ++st.s;
-      tc_after();
       uint32_t a[KEYS];
+      if (turns) turn_wait(x);
+      F2 sum[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
+      F2 cc = f2_pack(c, c), mm = cc;
+      // numerators of half the tile's keys, to the columns of its scores
+      auto half = [&](int h) {
+        uint32_t w[KEYS / 4];
 #pragma unroll
-      for (int i = 0; i < KEYS / 32; ++i) tc_ld32(sc + i * 32, a + i * 32);
-      tc_wait_ld();
-      const int32_t left = see - t * KEYS;  // keys of the tile that the row sees
-      if (left < KEYS) {
-#pragma unroll
-        for (int i = 0; i < KEYS; ++i)
-          if (i >= left) a[i] = 0xff800000u;  // -inf
-      }
-      float top[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) top[i] = __uint_as_float(a[i]);
-#pragma unroll
-      for (int i = 4; i < KEYS; ++i) top[i & 3] = fmaxf(top[i & 3], __uint_as_float(a[i]));
-      const float hi = c * fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-      if (__any_sync(0xffffffffu, hi > m + kLazy)) {
-        const float m2 = fmaxf(m, hi);
-        const float g = m2 == -INFINITY ? 1.f : fast_exp2(m - m2);
-        m = m2;
-        l *= g;
-        if (t > f.t0) {
-#pragma unroll 1
-          for (int i = 0; i < D / 32; ++i) {
-            uint32_t o[32];
-            tc_ld32(oc + i * 32, o);
-            tc_wait_ld();
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * g);
-            tc_st32(oc + i * 32, o);
-          }
-        }
-      }
-      const float base = m == -INFINITY ? 0.f : m;
-      const F2 cc = f2_pack(c, c), mm = f2_pack(-base, -base);
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int h = 0; h < KEYS / 64; ++h) {
-        uint32_t w[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const int e = h * 64 + 2 * i;
+        for (int i = 0; i < KEYS / 4; ++i) {
+          const int e = h * (KEYS / 2) + 2 * i;
           float u, v;
           f2_unpack(f2_fma(f2_pack(__uint_as_float(a[e]), __uint_as_float(a[e + 1])), cc, mm), &u, &v);
           u = fast_exp2(u);
           v = fast_exp2(v);
-          sum[(2 * i) & 3] += u;
-          sum[(2 * i + 1) & 3] += v;
+          sum[i & 1] = f2_add(sum[i & 1], f2_pack(u, v));
           w[i] = ActType<DT>::pack2(u, v);
         }
-        tc_st32(sc + h * 32, w);
+        if constexpr (KEYS == 128) tc_st32(sc + h * 32, w);
+        else tc_st16(sc + h * 16, w);
+        tc_wait_st();
+        tc_before();
+        mb_arrive(smem_at(h == 0 ? &s.p_half[x] : &s.p_full[x]));
+      };
+      if (ok) {
+        tc_after();
+#pragma unroll
+        for (int i = 0; i < KEYS / 32; ++i) tc_ld32(sc + i * 32, a + i * 32);
+        tc_wait_ld();
+        const int32_t left = see - t * KEYS;  // keys of the tile that the row sees
+        if (left < KEYS) {
+#pragma unroll
+          for (int i = 0; i < KEYS; ++i)
+            if (i >= left) a[i] = 0xff800000u;  // -inf
+        }
+        float top[4];  // three-operand maxima
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top[i] = fmaxf(__uint_as_float(a[2 * i]), __uint_as_float(a[2 * i + 1]));
+#pragma unroll
+        for (int i = 8; i < KEYS; i += 2)
+          top[i / 2 & 3] = fmaxf(fmaxf(top[i / 2 & 3], __uint_as_float(a[i])), __uint_as_float(a[i + 1]));
+        const float hi = c * fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        if (__any_sync(0xffffffffu, hi > m + kLazy)) {
+          const float m2 = fmaxf(m, hi);
+          const float g = m2 == -INFINITY ? 1.f : fast_exp2(m - m2);
+          m = m2;
+          l *= g;
+          if (t > t0) {
+#pragma unroll 1
+            for (int i = 0; i < D / 32; ++i) {
+              uint32_t o[32];
+              tc_ld32(oc + i * 32, o);
+              tc_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * g);
+              tc_st32(oc + i * 32, o);
+            }
+          }
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        mm = f2_pack(-base, -base);
+        half(0);  // its products start while the second half's numerators are made
       }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      tc_wait_st();
-      tc_before();
-      mb_arrive(smem_at(&s.p_full[x]));
+      if (turns && (x == 0 || t + 1 < t1)) turn_pass(x);
+      if (ok) {
+        half(1);
+        float s0, s1;
+        f2_unpack(f2_add(sum[0], sum[1]), &s0, &s1);
+        l += s0 + s1;
+      }
     }
     *m_out = m;
     *l_out = l;
-    if (!__all_sync(0xffffffffu, mb_wait(smem_at(&s.o_full[x]), st.o & 1, p.polls, &s.abort))) return false;
+    ok = ok && __all_sync(0xffffffffu, mb_wait(smem_at(&s.o_full[x]), st.o & 1, p.polls, &s.abort));
     ++st.o;
     tc_after();
-    return true;
+    return ok;
   }
 
   // Row r's place in out, and in lse (*at).
@@ -470,40 +544,56 @@ struct Tile {
   template <class At>
   static __device__ __forceinline__ void join(const PagedAttnParams& p, const Frag& f, int r, int n, At at, float* dst) {
     if (r >= f.rows) return;
-    float m = -INFINITY, l = 0.f;
-    for (int i = 0; i < n; ++i) m = fmaxf(m, __ldcg(at(i) + r));
+    float m = -INFINITY, l = 0.f, w[kFanIn], ls[kFanIn];
+#pragma unroll
+    for (int i = 0; i < kFanIn; ++i) {  // the last slot's again past it
+      const float* z = at(min(i, n - 1)) + r;
+      w[i] = __ldcg(z);
+      ls[i] = __ldcg(z + ROWS);
+    }
+#pragma unroll
+    for (int i = 0; i < kFanIn; ++i) m = fmaxf(m, w[i]);
     const float base = m == -INFINITY ? 0.f : m;
-    float w[kFanIn];
 #pragma unroll
     for (int i = 0; i < kFanIn; ++i) {
-      w[i] = 0.f;
-      if (i < n) {
-        w[i] = fast_exp2(__ldcg(at(i) + r) - base);
-        l = fmaf(w[i], __ldcg(at(i) + ROWS + r), l);
-      }
+      w[i] = i < n ? fast_exp2(w[i] - base) : 0.f;
+      l = fmaf(w[i], ls[i], l);
     }
     const float inv = l > 0.f ? 1.f / l : 0.f;
     int64_t row = 0;
     char* out = out_row(p, f, r, &row);
 #pragma unroll 1
-    for (int d = 0; d < D / 8; ++d) {
-      float v[8] = {};
+    for (int d = 0; d < D; d += 32) {  // 32 columns at a time: eight loads of a slot in flight, two slots'
+      float v[32] = {};
 #pragma unroll
-      for (int i = 0; i < kFanIn; ++i) {
+      for (int i = 0; i < kFanIn; i += 2) {
         if (i >= n) break;
-        const float* z = at(i) + 2 * ROWS + ((int64_t)2 * d * ROWS + r) * 4;
-        const float4 a = __ldcg(reinterpret_cast<const float4*>(z)), b = __ldcg(reinterpret_cast<const float4*>(z + ROWS * 4));
-        v[0] = fmaf(w[i], a.x, v[0]); v[1] = fmaf(w[i], a.y, v[1]); v[2] = fmaf(w[i], a.z, v[2]); v[3] = fmaf(w[i], a.w, v[3]);
-        v[4] = fmaf(w[i], b.x, v[4]); v[5] = fmaf(w[i], b.y, v[5]); v[6] = fmaf(w[i], b.z, v[6]); v[7] = fmaf(w[i], b.w, v[7]);
-      }
-      if (dst) {
-        float* z = dst + 2 * ROWS + ((int64_t)2 * d * ROWS + r) * 4;
-        *reinterpret_cast<float4*>(z) = make_float4(v[0], v[1], v[2], v[3]);
-        *reinterpret_cast<float4*>(z + ROWS * 4) = make_float4(v[4], v[5], v[6], v[7]);
-      } else {
+        float4 a[8], b[8];
+        const float* z = at(i) + 2 * ROWS + ((int64_t)d / 4 * ROWS + r) * 4;
+        const float* y = at(min(i + 1, n - 1)) + 2 * ROWS + ((int64_t)d / 4 * ROWS + r) * 4;  // weight 0 past the last
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] *= inv;
-        st16(out + d * 16, pack<DT>(v));
+        for (int e = 0; e < 8; ++e) {
+          a[e] = __ldcg(reinterpret_cast<const float4*>(z + e * ROWS * 4));
+          b[e] = __ldcg(reinterpret_cast<const float4*>(y + e * ROWS * 4));
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          v[4 * e] = fmaf(w[i + 1], b[e].x, fmaf(w[i], a[e].x, v[4 * e]));
+          v[4 * e + 1] = fmaf(w[i + 1], b[e].y, fmaf(w[i], a[e].y, v[4 * e + 1]));
+          v[4 * e + 2] = fmaf(w[i + 1], b[e].z, fmaf(w[i], a[e].z, v[4 * e + 2]));
+          v[4 * e + 3] = fmaf(w[i + 1], b[e].w, fmaf(w[i], a[e].w, v[4 * e + 3]));
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (dst) *reinterpret_cast<float4*>(dst + 2 * ROWS + ((int64_t)(d / 4 + e) * ROWS + r) * 4) =
+            make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+      }
+      if (!dst) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] *= inv;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) st16(out + (d + 8 * e) * 2, pack<DT>(v + 8 * e));
       }
     }
     if (dst) {
@@ -516,7 +606,8 @@ struct Tile {
 
   // One fragment of a softmax warpgroup. Both warpgroups pass the same named barriers, whatever failed.
   static __device__ __forceinline__ bool soft_fragment(const PagedAttnParams& p, Smem& s, uint32_t tmem, const Frag& f,
-                                                       int x, Soft& st, bool ok, float* slots, uint32_t* counters) {
+                                                       const Frag* next, int x, Soft& st, bool ok, float* slots,
+                                                       uint32_t* counters) {
     constexpr int64_t SLOT = attn_slot_floats(ROWS, D);
     const int r = x * 128 + (threadIdx.x & 127);
     if (f.limit == 0) {  // no keys: never split
@@ -531,12 +622,13 @@ struct Tile {
     const AttnCuts cut{f.first, f.last};
     float* mine = cut.whole() ? nullptr : slots + cut.slot(blockIdx.x) * SLOT;
     if (x == 0 || f.rows > 128) {
-      if (ok) {
-        load_q(p, s, f, x);
-        float m, l;
-        ok = softmax(p, s, tmem, f, x, st, &m, &l);
-        if (ok) finish(p, tmem, f, x, m, l, mine);
-      }
+      float m, l;
+      if (ok && !st.q_ready) load_q(p, s, f, x);
+      ok = softmax(p, s, tmem, f, x, st, ok, &m, &l);
+      // the next unit's q before this one's end: its first scores are made meanwhile
+      st.q_ready = ok && next && next->limit > 0 && (x == 0 || next->rows > 128);
+      if (st.q_ready) load_q(p, s, *next, x);
+      if (ok) finish(p, tmem, f, x, m, l, mine);
     }
     if (cut.whole()) return ok;
     // with a block that failed the count is never met, so nobody joins the unit
@@ -557,61 +649,106 @@ struct Tile {
   }
 
   // ------------------------------------------------------------ the block
+  static __device__ __forceinline__ int64_t div64(int64_t a, int64_t b) {
+    return ((uint64_t)a | (uint64_t)b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+  }
+  // The place of tile x is looked for once; the units after it follow one another.
   static __device__ __forceinline__ void list(const PagedAttnParams& p, Smem& s, int64_t b0, int64_t x, int64_t run,
                                               const AttnShare& a) {
     int count = 0;
     const int64_t end = min(a.hi, run);
-    while (x < end && count < kFrags) {
-      const int rq = Split::find(s.split, x);
-      const Request r{s.split.q0[rq], s.split.n[rq], s.split.kv[rq]};
-      const int32_t nm = Cost::row_tiles(p, r);
-      const int64_t head = Cost::before(p, r, nm), rel = x - s.split.pre[rq];
-      const int32_t h = (int32_t)(rel / head);
-      const int64_t y = rel - h * head;
-      int32_t k = 0, hi = nm;  // the row tile that holds y
+    const int32_t R = Cost::tokens(p);
+    int rq = Split::find(s.split, x);
+    Request r{s.split.q0[rq], s.split.n[rq], s.split.kv[rq]};
+    int32_t nm = Cost::row_tiles(p, r), h, k = 0;
+    int64_t start = s.split.pre[rq];  // the unit's first tile
+    {
+      const int64_t head = div64(s.split.pre[rq + 1] - start, p.Hkv);
+      h = (int32_t)div64(x - start, head);
+      start += h * head;
+      int32_t hi = nm;  // the row tile that holds x
+      int64_t at = 0;
       while (hi - k > 1) {
         const int32_t mid = (k + hi) / 2;
-        if (Cost::before(p, r, mid) <= y) k = mid;
-        else hi = mid;
+        const int64_t y = Cost::before(p, r, mid);
+        if (y <= x - start) {
+          k = mid;
+          at = y;
+        } else {
+          hi = mid;
+        }
       }
+      start += at;
+    }
+    while (true) {
       Frag& f = s.frag[count++];
-      const int64_t k0 = Cost::before(p, r, k);
       f.b = b0 + rq;
       f.q0 = r.q0;
       f.n = r.n;
       f.kv = r.kv;
       f.h = h;
-      f.tok0 = k * Cost::tokens(p);
-      f.rows = min(Cost::tokens(p), r.n - f.tok0) * p.G;
+      f.tok0 = k * R;
+      f.rows = min(R, r.n - k * R) * p.G;
       f.limit = Cost::sees(p, r, k);
       const int32_t nt = Cost::key_tiles(f.limit);
-      f.t0 = (int32_t)(y - k0);
+      f.t0 = (int32_t)(x - start);
       f.t1 = (int32_t)min((int64_t)nt, f.t0 + (a.hi - x));
-      const int64_t start = x - f.t0;
-      f.first = start / a.per;
-      f.last = (start + nt - 1) / a.per;
+      f.first = start >= a.lo ? (int64_t)blockIdx.x : div64(start, a.per);
+      f.last = start + nt <= a.hi ? (int64_t)blockIdx.x : div64(start + nt - 1, a.per);
       x += f.t1 - f.t0;
+      if (x >= end || count == kFrags) break;
+      start = x;  // the unit ended inside the run: the next one
+      if (++k == nm) {
+        k = 0;
+        if (++h == p.Hkv) {
+          h = 0;
+          do ++rq;
+          while (s.split.pre[rq + 1] <= x);
+          r = Request{s.split.q0[rq], s.split.n[rq], s.split.kv[rq]};
+          nm = Cost::row_tiles(p, r);
+        }
+      }
     }
     s.count = count;
     s.x = x;
   }
 
+  // Lists the fragments of the block's run, kFrags at a time, and has every warp go through them. All warps
+  // pass the same block barriers, each role from its own copy of this loop.
+  template <bool LISTS, class Body>
+  static __device__ __forceinline__ void fragments(const PagedAttnParams& p, Smem& s, const AttnShare& a, Body body) {
+    int64_t run = 0, x = a.lo;
+    for (int64_t b0 = 0; b0 < p.B && x < a.hi; b0 += THREADS) {
+      run = p.B <= THREADS ? a.total : Split::chunk(p, s.split, b0, run);
+      while (x < a.hi && x < run) {
+        if (LISTS && threadIdx.x == 0) list(p, s, b0, x, run, a);
+        __syncthreads();
+        const int count = s.count;
+        x = s.x;
+        for (int i = 0; i < count; ++i) body(s.frag[i], i + 1 < count ? &s.frag[i + 1] : nullptr);
+        __syncwarp();
+        __syncthreads();
+      }
+    }
+  }
+
   static __device__ __forceinline__ void run(const PagedAttnParams& p, const CUtensorMap* mk, const CUtensorMap* mv, Smem& s) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int MMA_WARP = SOFT / 32, LOAD_WARP = MMA_WARP + 1;
+    constexpr int MMA_WARP = SOFT / 32, LOAD_WARP = MMA_WARP + NT;
     if (warp == MMA_WARP) {
       asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_at(&s.tmem)) : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
       if (lane == 0) {
         for (int i = 0; i < SLOTS; ++i) {
           mb_init(smem_at(&s.full[i]), 1);
-          mb_init(smem_at(&s.empty[i]), 1);
+          mb_init(smem_at(&s.empty[i]), NT);
         }
         mb_init(smem_at(&s.raw), 1);
-        mb_init(smem_at(&s.drain), 1);
+        mb_init(smem_at(&s.drain), NT);
         for (int x = 0; x < NT; ++x) {
           mb_init(smem_at(&s.q_full[x]), 128);
           mb_init(smem_at(&s.s_full[x]), 1);
+          mb_init(smem_at(&s.p_half[x]), 128);
           mb_init(smem_at(&s.p_full[x]), 128);
           mb_init(smem_at(&s.o_full[x]), 1);
         }
@@ -631,32 +768,22 @@ struct Tile {
     uint32_t* counters = reinterpret_cast<uint32_t*>(p.work);
     float* slots = p.work + attn_counters(gridDim.x);
     Load ld;
-    Mma mm;
-    Soft so;
     bool ok = true;
-    int64_t run = 0, x = a.lo;
-    for (int64_t b0 = 0; b0 < p.B && x < a.hi; b0 += THREADS) {
-      run = Split::chunk(p, s.split, b0, run);
-      while (x < a.hi && x < run) {
-        if (threadIdx.x == 0) list(p, s, b0, x, run, a);
-        __syncthreads();
-        const int count = s.count;
-        x = s.x;
-        for (int i = 0; i < count; ++i) {
-          const Frag& f = s.frag[i];
-          if (warp < MMA_WARP) {
-            ok = soft_fragment(p, s, tmem, f, warp / 4, so, ok, slots, counters);
-          } else if (f.limit > 0 && ok) {
-            if (warp == LOAD_WARP) {
-              ok = load(p, mk, mv, s, f, ld);
-            } else if (lane == 0) {
-              ok = mma(p, s, tmem, f, mm);
-            }
-          }
-        }
-        __syncwarp();
-        __syncthreads();
-      }
+    if (warp < MMA_WARP) {
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(SOFT_REGS));
+      Soft so;
+      fragments<true>(p, s, a, [&](const Frag& f, const Frag* next) {
+        ok = soft_fragment(p, s, tmem, f, next, warp / 4, so, ok, slots, counters);
+      });
+    } else {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(OTHER_REGS));
+      Mma mm;
+      const bool one = elect_one();
+      fragments<false>(p, s, a, [&](const Frag& f, const Frag*) {
+        if (f.limit == 0 || !ok) return;
+        if (warp == LOAD_WARP) ok = load(p, mk, mv, s, f, ld);
+        else if (warp < LOAD_WARP) ok = mma(p, s, tmem, f, warp - MMA_WARP, mm, one);
+      });
     }
     // the way out: every copy and product of the block has to be done before its memory is given back
     if (warp == LOAD_WARP) {
@@ -666,8 +793,8 @@ struct Tile {
       }
       if (ld.bad) atomicOr(p.err, kErrTable);
     }
-    if (warp == MMA_WARP && lane == 0) {
-      tc_commit(smem_at(&s.drain));
+    if (warp >= MMA_WARP && warp < LOAD_WARP) {
+      if (elect_one()) tc_commit(smem_at(&s.drain));
       mb_drain(smem_at(&s.drain), 0);
     }
     __syncwarp();
