@@ -2,9 +2,9 @@
 //
 // Bound: the tensor cores. A unit is NT tiles of 128 rows (tokens x the G heads of a group, so that all of
 // them share the keys' loads) against tiles of KEYS keys; per block NT softmax warpgroups, NT warps that
-// issue tcgen05.mma and one that loads:
-//   load     k and v tiles by TMA, a box per page, into a ring of KEYS x D slots in the 128-byte swizzle;
-//            a unit's last v tile gets zeros in the rows past the last key up to the next 16 (a pool's
+// issue tcgen05.mma and two that load:
+//   load     two warps, k and v tiles by TMA, a box per page, into rings of KEYS x D slots in the 128-byte
+//            swizzle; a unit's last v tile gets zeros in the rows past the last key up to the next 16 (a pool's
 //            unused rows may hold NaN, and 0 * NaN would reach the sums)
 //   mma      S_x = Q_x K^T into TMEM, then for each tile O_x += P_x V with P_x from TMEM; the tiles take
 //            turns, so that one tile's products run while the other tile's softmax does
@@ -155,31 +155,31 @@ __device__ __forceinline__ int64_t floor_sum(uint32_t n, uint32_t m, uint32_t a,
 // kv - n + min(n, (k + 1) R) keys (its last token's).
 template <int ROWS, int KEYS>
 struct TileCost {
-  static __device__ __forceinline__ int32_t tokens(const PagedAttnParams& p) { return ROWS / p.G; }
   static __device__ __forceinline__ int32_t sees(const PagedAttnParams& p, const Request& r, int32_t k) {
-    const int64_t i = min((int64_t)r.n, (int64_t)(k + 1) * tokens(p));
+    const int64_t i = min((int64_t)r.n, (int64_t)(k + 1) * p.tokens);
     return (int32_t)max((int64_t)0, min((int64_t)r.kv, (int64_t)r.kv - r.n + i));
   }
-  static __device__ __forceinline__ int32_t key_tiles(int32_t keys) { return keys > KEYS ? (keys + KEYS - 1) / KEYS : 1; }
-  static __device__ __forceinline__ int32_t row_tiles(const PagedAttnParams& p, const Request& r) {
-    const int32_t R = tokens(p);
-    return (int32_t)(((int64_t)r.n + R - 1) / R);
+  static __device__ __forceinline__ int32_t key_tiles(int32_t keys) {
+    return keys > KEYS ? (int32_t)(((uint32_t)keys + KEYS - 1) / KEYS) : 1;
   }
-  // Key tiles of the first k row tiles of one kv head.
-  static __device__ __forceinline__ int64_t before(const PagedAttnParams& p, const Request& r, int32_t k) {
-    const int32_t c = r.kv - r.n, R = tokens(p);
-    int32_t full = k;  // row tiles that end at a whole R
+  static __device__ __forceinline__ int32_t row_tiles(const PagedAttnParams& p, const Request& r) {
+    return (int32_t)(((uint32_t)r.n + (uint32_t)(p.tokens - 1)) / (uint32_t)p.tokens);
+  }
+  // Key tiles of the first k row tiles of one kv head; all of them end at a whole R (last: but the k-th).
+  static __device__ __forceinline__ int64_t before(const PagedAttnParams& p, const Request& r, int32_t k, bool last) {
+    const int32_t c = r.kv - r.n;
     int64_t total = 0;
-    if (k == row_tiles(p, r) && k > 0) {
-      --full;
-      total = key_tiles(sees(p, r, k - 1));
+    if (last) total = key_tiles(sees(p, r, --k));
+    if (c < 0) {
+      for (int32_t i = 0; i < k; ++i) total += key_tiles(sees(p, r, i));
+      return total;
     }
-    if (c >= 0) return total + floor_sum(full, KEYS, R, c + R + KEYS - 1);
-    for (int32_t i = 0; i < full; ++i) total += key_tiles(sees(p, r, i));
-    return total;
+    // sum of ceil((c + (i + 1) R) / KEYS); whole multiples of KEYS taken out with constant divisors
+    const uint32_t R = (uint32_t)p.tokens, b = (uint32_t)c + R + KEYS - 1;
+    return total + (int64_t)k * (b / KEYS) + (int64_t)k * (k - 1) / 2 * (R / KEYS) + floor_sum(k, KEYS, R % KEYS, b % KEYS);
   }
   static __device__ __forceinline__ int64_t of(const PagedAttnParams& p, const Request& r) {
-    return (int64_t)p.Hkv * before(p, r, row_tiles(p, r));
+    return (int64_t)p.Hkv * before(p, r, row_tiles(p, r), true);
   }
 };
 
@@ -192,6 +192,7 @@ struct Frag {
 template <int DT_, int D_, int NT_, int KEYS_, int SLOTS_>
 struct Tile {
   static constexpr int DT = DT_, D = D_, NT = NT_, KEYS = KEYS_, SLOTS = SLOTS_;
+  static constexpr int KS = SLOTS / 2;         // ring slots of k, and as many of v after them
   static constexpr int ROWS = 128 * NT;
   static constexpr int SOFT = 128 * NT;        // softmax threads
   static constexpr int THREADS = SOFT + 128;   // mma, load and idle warps: a warpgroup, for setmaxnreg
@@ -219,70 +220,79 @@ struct Tile {
     typename Split::Smem split;
   };
 
-  // ------------------------------------------------------------ load warp
+  // ------------------------------------------------------------ load warps, one for k and one for v
   struct Load {
-    uint32_t issued = 0;     // slots filled so far
+    uint32_t tiles = 0;      // tiles loaded so far
     uint32_t raws = 0;       // v tiles with a wait of their own
     bool bad = false;
   };
-  static __device__ __forceinline__ bool load(const PagedAttnParams& p, const CUtensorMap* mk, const CUtensorMap* mv,
-                                              Smem& s, const Frag& f, Load& st) {
+  static __device__ __forceinline__ void arrive_lane0(uint32_t bar) {
+    if ((threadIdx.x & 31) == 0) mb_arrive(bar);
+    __syncwarp();
+  }
+  static __device__ __forceinline__ bool load(const PagedAttnParams& p, const CUtensorMap* map, Smem& s, const Frag& f,
+                                              bool is_v, Load& st) {
     const int lane = threadIdx.x & 31;
     const int32_t* table = p.table + f.b * p.table_rs;
     const int ps = p.page.d, box = min(ps, KEYS);       // rows of a box
-    for (int32_t t = f.t0; t < f.t1; ++t) {
-      const int32_t j0 = t * KEYS, valid = min(KEYS, f.limit - j0);
-      const int boxes = (valid + box - 1) / box;
-      int32_t page = 0, at = 0;
-      if (lane < boxes) {
-        const uint32_t j = (uint32_t)(j0 + lane * box), pg = fast_div(j, p.page.magic, p.page.shift);
-        at = (int32_t)(j - pg * (uint32_t)ps);
+    const int32_t limit = f.limit, t1 = f.t1, h = f.h;
+    // the page of the lane's box in tile t, and its row there; read a tile ahead
+    auto locate = [&](int32_t t, int32_t* at) {
+      const int32_t j = t * KEYS + lane * box;
+      int32_t page = 0;
+      *at = 0;
+      if (lane * box < KEYS && j < limit) {
+        const uint32_t pg = fast_div((uint32_t)j, p.page.magic, p.page.shift);
+        *at = (int32_t)((uint32_t)j - pg * (uint32_t)ps);
         page = table[pg];
         if (page < 0 || page >= p.P) {
           st.bad = true;
           page = 0;
         }
       }
-      for (int kv = 0; kv < 2; ++kv) {
-        const uint32_t slot = st.issued % SLOTS, use = st.issued / SLOTS;
-        if (!__all_sync(0xffffffffu, mb_wait(smem_at(&s.empty[slot]), (use & 1) ^ 1, p.polls, &s.abort))) return false;
-        const bool tail = kv == 1 && valid % 16 != 0;
-        const uint32_t bar = smem_at(tail ? &s.raw : &s.full[slot]), dst = smem_at(s.ring + slot * KB);
-        if (lane == 0) mb_expect(bar, (uint32_t)(boxes * box * D * 2));
-        __syncwarp();
-        if (lane < boxes)
-          for (int c = 0; c < D / 64; ++c)
-            tma_4d(dst + c * KHALF + lane * box * 128, kv ? mv : mk, c * 64, at, f.h, page, bar);
-        __syncwarp();
-        ++st.issued;
-        if (tail) {  // zeros from the last key to the next 16
-          const uint32_t parity = st.raws++ & 1;
-          if (!__all_sync(0xffffffffu, mb_wait(bar, parity, p.polls, &s.abort))) {
-            mb_drain(bar, parity);
-            mb_arrive_lane0(smem_at(&s.full[slot]));
-            return false;
-          }
-          const int rows = 16 - valid % 16;
-          for (int e = lane; e < rows * (D / 8); e += 32) {
-            const int r = valid + e / (D / 8), c = e % (D / 8);
-            *reinterpret_cast<uint4*>(s.ring + slot * KB + (c / 8) * KHALF + r * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
-          }
-          fence_async();
-          __syncwarp();
-          mb_arrive_lane0(smem_at(&s.full[slot]));
+      return page;
+    };
+    int32_t at, at_next, page = locate(f.t0, &at), page_next = 0;
+    for (int32_t t = f.t0; t < t1; ++t, page = page_next, at = at_next) {
+      page_next = at_next = 0;
+      if (t + 1 < t1) page_next = locate(t + 1, &at_next);
+      const int32_t valid = min(KEYS, limit - t * KEYS);
+      const int boxes = (valid + box - 1) / box;
+      const uint32_t slot = st.tiles % KS + (is_v ? KS : 0), use = st.tiles / KS;
+      if (!__all_sync(0xffffffffu, mb_wait(smem_at(&s.empty[slot]), (use & 1) ^ 1, p.polls, &s.abort))) return false;
+      const bool tail = is_v && valid % 16 != 0;
+      const uint32_t bar = smem_at(tail ? &s.raw : &s.full[slot]), dst = smem_at(s.ring + slot * KB);
+      if (lane == 0) mb_expect(bar, (uint32_t)(boxes * box * D * 2));
+      __syncwarp();
+      if (lane < boxes) {
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) tma_4d(dst + c * KHALF + lane * box * 128, map, c * 64, at, h, page, bar);
+      }
+      __syncwarp();
+      ++st.tiles;
+      if (tail) {  // zeros from the last key to the next 16
+        const uint32_t parity = st.raws++ & 1;
+        if (!__all_sync(0xffffffffu, mb_wait(bar, parity, p.polls, &s.abort))) {
+          mb_drain(bar, parity);
+          arrive_lane0(smem_at(&s.full[slot]));
+          return false;
         }
+        const int rows = 16 - valid % 16;
+        for (int e = lane; e < rows * (D / 8); e += 32) {
+          const int r = valid + e / (D / 8), c = e % (D / 8);
+          *reinterpret_cast<uint4*>(s.ring + slot * KB + (c / 8) * KHALF + r * 128 + (c % 8) * 16) = make_uint4(0, 0, 0, 0);
+        }
+        fence_async();
+        __syncwarp();
+        arrive_lane0(smem_at(&s.full[slot]));
       }
     }
     return true;
   }
-  static __device__ __forceinline__ void mb_arrive_lane0(uint32_t bar) {
-    if ((threadIdx.x & 31) == 0) mb_arrive(bar);
-    __syncwarp();
-  }
 
   // ------------------------------------------------------------ mma warps, one per q tile
   struct Mma {
-    uint32_t taken = 0;      // slots consumed so far
+    uint32_t tiles = 0;       // key tiles consumed so far
     uint32_t px = 0, qx = 0;  // p and q tiles waited for
   };
   static __device__ __forceinline__ void qk(uint32_t q_lo, uint32_t k_lo, uint32_t d) {
@@ -313,29 +323,34 @@ struct Tile {
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       return __all_sync(0xffffffffu, mb_wait(smem_at(bar), parity, p.polls, &s.abort));
     };
-    auto slot_ready = [&](uint32_t i) { return wait(&s.full[i % SLOTS], (i / SLOTS) & 1); };
-    uint32_t k = st.taken;  // slot of the current k tile; the v tile's is the next
+    uint32_t i = st.tiles;
+    auto k_slot = [](uint32_t i) { return i % KS; };
+    auto v_slot = [](uint32_t i) { return KS + i % KS; };
+    auto ready = [&](uint32_t slot, uint32_t i) { return wait(&s.full[slot], (i / KS) & 1); };
+    st.tiles += (uint32_t)(t1 - t0);
     if (x > 0 && f.rows <= 128 * x) {  // nothing to do but to give the slots back
-      for (; k < st.taken + 2 * (uint32_t)(t1 - t0); ++k) {
-        if (!slot_ready(k)) return false;
-        if (one) mb_arrive(smem_at(&s.empty[k % SLOTS]));
+      for (; i < st.tiles; ++i) {
+        if (!ready(k_slot(i), i) || !ready(v_slot(i), i)) return false;
+        if (one) {
+          mb_arrive(smem_at(&s.empty[k_slot(i)]));
+          mb_arrive(smem_at(&s.empty[v_slot(i)]));
+        }
       }
-      st.taken = k;
       return true;
     }
-    if (!wait(&s.q_full[x], st.qx++ & 1) || !slot_ready(k)) return false;
+    if (!wait(&s.q_full[x], st.qx++ & 1) || !ready(k_slot(i), i)) return false;
     tc_after();
     if (one) {
-      qk(q_lo, k_lo + k % SLOTS * (KB >> 4), sc);
+      qk(q_lo, k_lo + k_slot(i) * (KB >> 4), sc);
       tc_commit(smem_at(&s.s_full[x]));
-      tc_commit(smem_at(&s.empty[k % SLOTS]));
+      tc_commit(smem_at(&s.empty[k_slot(i)]));
     }
-    for (int32_t t = t0; t < t1; ++t) {
-      const uint32_t v = k + 1, next = k + 2, parity = st.px++ & 1;
+    for (int32_t t = t0; t < t1; ++t, ++i) {
+      const uint32_t parity = st.px++ & 1;
       const bool more = t + 1 < t1, add = t > t0;
       const int steps = (min(KEYS, limit - t * KEYS) + 15) / 16;
-      const uint32_t v_at = v_lo + v % SLOTS * (KB >> 4), k_at = k_lo + next % SLOTS * (KB >> 4);
-      if (!slot_ready(v) || (more && !slot_ready(next))) return false;
+      const uint32_t v_at = v_lo + v_slot(i) * (KB >> 4), k_at = k_lo + k_slot(i + 1) * (KB >> 4);
+      if (!ready(v_slot(i), i) || (more && !ready(k_slot(i + 1), i + 1))) return false;
       if (!wait(&s.p_half[x], parity)) return false;
       tc_after();
       if (one) pv<0>(sc, v_at, oc, steps, add);
@@ -346,15 +361,13 @@ struct Tile {
         if (more) {
           qk(q_lo, k_at, sc);
           tc_commit(smem_at(&s.s_full[x]));
-          tc_commit(smem_at(&s.empty[next % SLOTS]));
+          tc_commit(smem_at(&s.empty[k_slot(i + 1)]));
         } else {
           tc_commit(smem_at(&s.o_full[x]));
         }
-        tc_commit(smem_at(&s.empty[v % SLOTS]));
+        tc_commit(smem_at(&s.empty[v_slot(i)]));
       }
-      k = next;
     }
-    st.taken = k;
     return true;
   }
 
@@ -652,12 +665,13 @@ struct Tile {
   static __device__ __forceinline__ int64_t div64(int64_t a, int64_t b) {
     return ((uint64_t)a | (uint64_t)b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
   }
-  // The place of tile x is looked for once; the units after it follow one another.
+  // The place of tile x is looked for once, by a warp: its lanes try 32 row tiles at a time. The units after
+  // it follow one another.
   static __device__ __forceinline__ void list(const PagedAttnParams& p, Smem& s, int64_t b0, int64_t x, int64_t run,
                                               const AttnShare& a) {
     int count = 0;
     const int64_t end = min(a.hi, run);
-    const int32_t R = Cost::tokens(p);
+    const int32_t R = p.tokens;
     int rq = Split::find(s.split, x);
     Request r{s.split.q0[rq], s.split.n[rq], s.split.kv[rq]};
     int32_t nm = Cost::row_tiles(p, r), h, k = 0;
@@ -666,17 +680,15 @@ struct Tile {
       const int64_t head = div64(s.split.pre[rq + 1] - start, p.Hkv);
       h = (int32_t)div64(x - start, head);
       start += h * head;
-      int32_t hi = nm;  // the row tile that holds x
       int64_t at = 0;
-      while (hi - k > 1) {
-        const int32_t mid = (k + hi) / 2;
-        const int64_t y = Cost::before(p, r, mid);
-        if (y <= x - start) {
-          k = mid;
-          at = y;
-        } else {
-          hi = mid;
-        }
+      int32_t step = 1;
+      while (step < nm) step *= 32;
+      for (step /= 32; step > 0; step /= 32) {  // before(k) <= x - start < before(k + 32 step)
+        const int32_t mine = k + (int32_t)(threadIdx.x & 31) * step;
+        const int64_t y = mine < nm ? Cost::before(p, r, mine, false) : INT64_MAX;
+        const int last = 31 - __clz(__ballot_sync(0xffffffffu, y <= x - start));
+        k += last * step;
+        at = __shfl_sync(0xffffffffu, y, last);
       }
       start += at;
     }
@@ -721,7 +733,7 @@ struct Tile {
     for (int64_t b0 = 0; b0 < p.B && x < a.hi; b0 += THREADS) {
       run = p.B <= THREADS ? a.total : Split::chunk(p, s.split, b0, run);
       while (x < a.hi && x < run) {
-        if (LISTS && threadIdx.x == 0) list(p, s, b0, x, run, a);
+        if (LISTS && threadIdx.x < 32) list(p, s, b0, x, run, a);
         __syncthreads();
         const int count = s.count;
         x = s.x;
@@ -781,15 +793,16 @@ struct Tile {
       const bool one = elect_one();
       fragments<false>(p, s, a, [&](const Frag& f, const Frag*) {
         if (f.limit == 0 || !ok) return;
-        if (warp == LOAD_WARP) ok = load(p, mk, mv, s, f, ld);
+        if (warp >= LOAD_WARP && warp < LOAD_WARP + 2) ok = load(p, warp == LOAD_WARP ? mk : mv, s, f, warp > LOAD_WARP, ld);
         else if (warp < LOAD_WARP) ok = mma(p, s, tmem, f, warp - MMA_WARP, mm, one);
       });
     }
     // the way out: every copy and product of the block has to be done before its memory is given back
-    if (warp == LOAD_WARP) {
-      for (uint32_t i = ld.issued > SLOTS ? ld.issued - SLOTS : 0; i < ld.issued; ++i) {
-        mb_drain(smem_at(&s.full[i % SLOTS]), (i / SLOTS) & 1);
-        if (ok) mb_drain(smem_at(&s.empty[i % SLOTS]), (i / SLOTS) & 1);
+    if (warp >= LOAD_WARP && warp < LOAD_WARP + 2) {
+      for (uint32_t i = ld.tiles > KS ? ld.tiles - KS : 0; i < ld.tiles; ++i) {
+        const uint32_t slot = i % KS + (warp > LOAD_WARP ? KS : 0);
+        mb_drain(smem_at(&s.full[slot]), (i / KS) & 1);
+        if (ok) mb_drain(smem_at(&s.empty[slot]), (i / KS) & 1);
       }
       if (ld.bad) atomicOr(p.err, kErrTable);
     }

@@ -221,6 +221,7 @@ struct PagedAttnParams {
   FastDiv page, group;  // by ps; by G = Hq / Hkv
   int64_t rows_above, rows_upto;  // this launch takes the requests of rows_above < n * G <= rows_upto
   int64_t min_tiles;              // a block's run of key tiles is at least this long
+  int32_t tokens;                 // tile kernel: tokens of a row tile
   uint32_t polls, first_polls;    // tile kernel: bounds of its waits, of a warp's first for scores
 };
 

@@ -1067,6 +1067,7 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
     q.rows_above = pl.rows ? kTileRows : 0;
     q.rows_upto = INT64_MAX;
     q.min_tiles = kTileRun;
+    q.tokens = tile.rows / p.G;
     void* tp[3] = {&q, &mk, &mv};
     cfg.blockDimX = (unsigned)tile.threads;
     cfg.gridDimX = (unsigned)(scm->sm_count * tile.per_sm);
