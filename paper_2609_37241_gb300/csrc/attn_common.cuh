@@ -87,59 +87,82 @@ __device__ __forceinline__ bool attn_takes(const PagedAttnParams& p, int32_t n) 
   return n > 0 && rows > p.rows_above && rows <= p.rows_upto;
 }
 
-// One block's share of the call: tiles per block and this block's run [lo, hi).
+// One block's share of the call: tiles per block and this block's run [lo, hi). whole: a unit per block
+// instead, all of it, where there are at most as many units as blocks and none is longer than an even run
+// and what a cut costs (a partial written, counted and joined: about join_tiles tiles' time); per, lo and
+// hi then count units.
 struct AttnShare {
   int64_t per, lo, hi, total;
+  bool whole;
 };
 
 // Cost::of(p, r): the key tiles of all of request r's units, at least one per unit so that a unit
-// without keys is written too. NT: threads of the block.
+// without keys is written too; Cost::units and Cost::longest: its units, and the tiles of the longest.
+// NT: threads of the block.
 template <int NT, class Cost>
 struct AttnSplit {
   struct Smem {
-    long long warp[(NT + 31) / 32];
-    long long pre[NT + 1];  // tiles before each request of the current chunk, from the call's start
+    long long warp[NT / 32], units[NT / 32];
+    int32_t longest[NT / 32];
+    long long pre[NT + 1];  // tiles (units) before each request of the current chunk, from the call's start
     int32_t q0[NT], n[NT], kv[NT];
   };
 
-  static __device__ __forceinline__ int64_t cost(const PagedAttnParams& p, const Request& r) {
-    return attn_takes(p, r.n) ? Cost::of(p, r) : 0;
-  }
-
   // The block's share; with at most NT requests their chunk is filled as well.
   static __device__ __forceinline__ AttnShare share(const PagedAttnParams& p, Smem& s) {
-    long long sum = 0;
-    if (p.B <= NT) {
-      sum = chunk(p, s, 0, 0);
-    } else {
-      bool ok = true;
-      for (int64_t b = threadIdx.x; b < p.B; b += NT) sum += cost(p, attn_request(p, b, &ok));
-      if (!ok && blockIdx.x == 0) atomicOr(p.err, kErrTable);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      if ((threadIdx.x & 31) == 0) s.warp[threadIdx.x >> 5] = sum;
-      __syncthreads();
-      sum = 0;
-#pragma unroll
-      for (int w = 0; w < NT / 32; ++w) sum += s.warp[w];
+    bool ok = true;
+    long long sum = 0, units = 0;
+    int32_t longest = 0;
+    for (int64_t b = threadIdx.x; b < p.B; b += NT) {
+      const Request r = attn_request(p, b, &ok);
+      if (!attn_takes(p, r.n)) continue;
+      sum += Cost::of(p, r);
+      if (p.join_tiles > 0) {
+        units += Cost::units(p, r);
+        longest = max(longest, Cost::longest(p, r));
+      }
     }
-    const int64_t even = (sum + gridDim.x - 1) / gridDim.x;
+    if (!ok && blockIdx.x == 0) atomicOr(p.err, kErrTable);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (p.join_tiles > 0) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        units += __shfl_xor_sync(0xffffffffu, units, o);
+        longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
+      }
+    }
+    if ((threadIdx.x & 31) == 0) {
+      s.warp[threadIdx.x >> 5] = sum;
+      s.units[threadIdx.x >> 5] = units;
+      s.longest[threadIdx.x >> 5] = longest;
+    }
+    __syncthreads();
+    sum = units = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) {
+      sum += s.warp[w];
+      units += s.units[w];
+      longest = max(longest, s.longest[w]);
+    }
+    const int64_t even = (uint64_t)sum >> 31 ? (sum + gridDim.x - 1) / gridDim.x
+                                             : (int64_t)(((uint32_t)sum + gridDim.x - 1) / gridDim.x);
     AttnShare a;
-    a.total = sum;
-    a.per = even > p.min_tiles ? even : p.min_tiles;
-    a.lo = min((int64_t)sum, (int64_t)blockIdx.x * a.per);
-    a.hi = min((int64_t)sum, a.lo + a.per);
+    a.whole = p.join_tiles > 0 && units <= gridDim.x && longest <= even + p.join_tiles;
+    a.total = a.whole ? units : sum;
+    a.per = a.whole ? 1 : (even > p.min_tiles ? even : p.min_tiles);
+    a.lo = min(a.total, (int64_t)blockIdx.x * a.per);
+    a.hi = min(a.total, a.lo + a.per);
     return a;
   }
 
   // Fills the chunk of NT requests from b0 on; run: the tiles before it. Returns those after it.
-  static __device__ __forceinline__ int64_t chunk(const PagedAttnParams& p, Smem& s, int64_t b0, int64_t run) {
+  static __device__ __forceinline__ int64_t chunk(const PagedAttnParams& p, Smem& s, int64_t b0, int64_t run, bool whole) {
     const int64_t b = b0 + threadIdx.x;
     bool ok = true;
     Request r{0, 0, 0};
     if (b < p.B) r = attn_request(p, b, &ok);
-    if (!ok && blockIdx.x == 0) atomicOr(p.err, kErrTable);
-    const long long own = cost(p, r);
+    const long long own = !attn_takes(p, r.n) ? 0 : whole ? Cost::units(p, r) : Cost::of(p, r);
     long long v = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {

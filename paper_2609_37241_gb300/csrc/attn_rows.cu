@@ -74,8 +74,12 @@ struct RowsCost {
   static __device__ __forceinline__ int64_t key_tiles(int32_t kv) {
     return kv > kRowsKeys ? ((int64_t)kv + kRowsKeys - 1) / kRowsKeys : 1;
   }
+  static __device__ __forceinline__ int64_t units(const PagedAttnParams& p, const Request& r) {
+    return (int64_t)p.Hkv * row_tiles(p, r.n);
+  }
+  static __device__ __forceinline__ int32_t longest(const PagedAttnParams&, const Request& r) { return (int32_t)key_tiles(r.kv); }
   static __device__ __forceinline__ int64_t of(const PagedAttnParams& p, const Request& r) {
-    return (int64_t)p.Hkv * row_tiles(p, r.n) * key_tiles(r.kv);
+    return units(p, r) * key_tiles(r.kv);
   }
 };
 
@@ -365,7 +369,7 @@ struct RowsKernel {
     bool bad = false;
     int64_t run = 0, x = a.lo;
     for (int64_t b0 = 0; b0 < p.B && x < a.hi; b0 += kRowsThreads) {
-      run = p.B <= kRowsThreads ? a.total : Split::chunk(p, s.split, b0, run);
+      run = Split::chunk(p, s.split, b0, run, false);
       while (x < a.hi && x < run) {
         const int rq = Split::find(s.split, x);
         Unit u;
@@ -412,9 +416,14 @@ struct RowsKernel {
 template <int DT, int D>
 __global__ void __launch_bounds__(kRowsThreads, RowsGeom<D>::PER_SM) attn_rows_kernel(const PagedAttnParams p) {
   extern __shared__ __align__(128) char smem[];
-  pdl_prologue();
+  // After the tile kernel of the same call, which waits for everything before it and only then lets this
+  // launch start, nothing has to be waited for: the two write different rows. This grid then must not be
+  // over before that one, so the wait comes last.
+  pdl_trigger();
+  if (!p.beside) pdl_wait();
   using K = RowsKernel<DT, D>;
   K::run(p, *reinterpret_cast<typename K::Smem*>(smem));
+  if (p.beside) pdl_wait();
 }
 
 template <int DT, int D>

@@ -178,6 +178,10 @@ struct TileCost {
     const uint32_t R = (uint32_t)p.tokens, b = (uint32_t)c + R + KEYS - 1;
     return total + (int64_t)k * (b / KEYS) + (int64_t)k * (k - 1) / 2 * (R / KEYS) + floor_sum(k, KEYS, R % KEYS, b % KEYS);
   }
+  static __device__ __forceinline__ int64_t units(const PagedAttnParams& p, const Request& r) {
+    return (int64_t)p.Hkv * row_tiles(p, r);
+  }
+  static __device__ __forceinline__ int32_t longest(const PagedAttnParams&, const Request& r) { return key_tiles(r.kv); }
   static __device__ __forceinline__ int64_t of(const PagedAttnParams& p, const Request& r) {
     return (int64_t)p.Hkv * before(p, r, row_tiles(p, r), true);
   }
@@ -553,10 +557,14 @@ struct Tile {
     }
   }
 
-  // Joins n slots, a thread per row, to out or (unnormalised) to dst, the first of them.
-  template <class At>
-  static __device__ __forceinline__ void join(const PagedAttnParams& p, const Frag& f, int r, int n, At at, float* dst) {
-    if (r >= f.rows) return;
+  // Joins n slots, a thread per row, to out or (unnormalised) to dst, the first of them. own >= 0: slot
+  // `own` is this block's accumulator in TMEM with its m and l.
+  template <bool OWN, class At>
+  static __device__ __forceinline__ void join(const PagedAttnParams& p, uint32_t tmem, const Frag& f, int x, int n, At at,
+                                              float* dst, int own, float m_own, float l_own) {
+    const int row = x * 128 + (threadIdx.x & 127), r = min(row, f.rows - 1);  // rows past the unit do the last's again
+    const bool live = row < f.rows;
+    const uint32_t oc = tmem + (((threadIdx.x >> 5) & 3) << 21) + O_COL + x * D;
     float m = -INFINITY, l = 0.f, w[kFanIn], ls[kFanIn];
 #pragma unroll
     for (int i = 0; i < kFanIn; ++i) {  // the last slot's again past it
@@ -565,16 +573,28 @@ struct Tile {
       ls[i] = __ldcg(z + ROWS);
     }
 #pragma unroll
-    for (int i = 0; i < kFanIn; ++i) m = fmaxf(m, w[i]);
+    for (int i = 0; i < kFanIn; ++i) {
+      if (OWN && min(i, n - 1) == own) {
+        w[i] = m_own;
+        ls[i] = l_own;
+      }
+      m = fmaxf(m, w[i]);
+    }
     const float base = m == -INFINITY ? 0.f : m;
+    float w_own = 0.f;
 #pragma unroll
     for (int i = 0; i < kFanIn; ++i) {
       w[i] = i < n ? fast_exp2(w[i] - base) : 0.f;
       l = fmaf(w[i], ls[i], l);
+      if (OWN && i == own) {
+        w_own = w[i];
+        w[i] = 0.f;
+      }
     }
     const float inv = l > 0.f ? 1.f / l : 0.f;
-    int64_t row = 0;
-    char* out = out_row(p, f, r, &row);
+    int64_t at_row = 0;
+    char* out = out_row(p, f, r, &at_row);
+    const int skip = own == 0 ? 1 : 0;  // a slot to read in the place of this block's (n > 1)
 #pragma unroll 1
     for (int d = 0; d < D; d += 32) {  // 32 columns at a time: eight loads of a slot in flight, two slots'
       float v[32] = {};
@@ -582,8 +602,9 @@ struct Tile {
       for (int i = 0; i < kFanIn; i += 2) {
         if (i >= n) break;
         float4 a[8], b[8];
-        const float* z = at(i) + 2 * ROWS + ((int64_t)d / 4 * ROWS + r) * 4;
-        const float* y = at(min(i + 1, n - 1)) + 2 * ROWS + ((int64_t)d / 4 * ROWS + r) * 4;  // weight 0 past the last
+        const int i0 = OWN && i == own ? skip : i, i1 = OWN && (i + 1 == own || i + 1 >= n) ? skip : min(i + 1, n - 1);
+        const float* z = at(i0) + 2 * ROWS + ((int64_t)d / 4 * ROWS + r) * 4;
+        const float* y = at(i1) + 2 * ROWS + ((int64_t)d / 4 * ROWS + r) * 4;  // weight 0 past the last
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           a[e] = __ldcg(reinterpret_cast<const float4*>(z + e * ROWS * 4));
@@ -597,23 +618,34 @@ struct Tile {
           v[4 * e + 3] = fmaf(w[i + 1], b[e].w, fmaf(w[i], a[e].w, v[4 * e + 3]));
         }
       }
+      if (OWN) {
+        uint32_t o[32];
+        __syncwarp();
+        tc_ld32(oc + d, o);
+        tc_wait_ld();
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (dst) *reinterpret_cast<float4*>(dst + 2 * ROWS + ((int64_t)(d / 4 + e) * ROWS + r) * 4) =
-            make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+        for (int e = 0; e < 32; ++e) v[e] = fmaf(w_own, __uint_as_float(o[e]), v[e]);
       }
-      if (!dst) {
+      if (dst && live) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          *reinterpret_cast<float4*>(dst + 2 * ROWS + ((int64_t)(d / 4 + e) * ROWS + r) * 4) =
+              make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+      }
+      if (!dst && live) {
 #pragma unroll
         for (int e = 0; e < 32; ++e) v[e] *= inv;
 #pragma unroll
         for (int e = 0; e < 4; ++e) st16(out + (d + 8 * e) * 2, pack<DT>(v + 8 * e));
       }
     }
+    if (OWN) tc_before();
+    if (!live) return;
     if (dst) {
       dst[r] = m;
       dst[ROWS + r] = l;
     } else {
-      put_lse(p, row, m, l);
+      put_lse(p, at_row, m, l);
     }
   }
 
@@ -634,29 +666,45 @@ struct Tile {
     }
     const AttnCuts cut{f.first, f.last};
     float* mine = cut.whole() ? nullptr : slots + cut.slot(blockIdx.x) * SLOT;
-    if (x == 0 || f.rows > 128) {
-      float m, l;
+    const int n = (int)(cut.last - cut.first + 1), i0 = (int)(blockIdx.x - cut.first);
+    const int groups = (n + kFanIn - 1) / kFanIn, gr = i0 / kFanIn, size = min(kFanIn, n - gr * kFanIn);
+    const int64_t g0 = cut.first + (int64_t)gr * kFanIn;
+    auto slot = [&](int64_t block) { return slots + cut.slot(block) * SLOT; };
+    auto in_group = [&](int i) { return slot(g0 + i); };
+    uint32_t* counter = counters + cut.slot(g0);
+    const bool leader = threadIdx.x == 0, used = x == 0 || f.rows > 128;
+    float m = -INFINITY, l = 0.f;
+    if (used) {
       if (ok && !st.q_ready) load_q(p, s, f, x);
       ok = softmax(p, s, tmem, f, x, st, ok, &m, &l);
       // the next unit's q before this one's end: its first scores are made meanwhile
       st.q_ready = ok && next && next->limit > 0 && (x == 0 || next->rows > 128);
       if (st.q_ready) load_q(p, s, *next, x);
-      if (ok) finish(p, tmem, f, x, m, l, mine);
     }
+    // A unit that goes on past this block's run: the blocks after this one began with it, so they mostly are
+    // done. Then this one's part is the last and is joined from TMEM without a turn through the workspace.
+    if (f.last > blockIdx.x && groups == 1) {
+      if (leader) s.flag = !s.abort && *reinterpret_cast<volatile uint32_t*>(counter) + 1 == (uint32_t)size;
+      attn_sync<1, SOFT>();
+      const bool last = s.flag != 0;
+      attn_sync<1, SOFT>();
+      if (last) {
+        __threadfence();
+        if (used && ok) join<true>(p, tmem, f, x, size, in_group, nullptr, i0, m, l);
+        if (leader) *counter = 0u;
+        return ok;
+      }
+    }
+    if (used && ok) finish(p, tmem, f, x, m, l, mine);
     if (cut.whole()) return ok;
     // with a block that failed the count is never met, so nobody joins the unit
-    const int n = (int)(cut.last - cut.first + 1), i0 = (int)(blockIdx.x - cut.first);
-    const int groups = (n + kFanIn - 1) / kFanIn, gr = i0 / kFanIn, size = min(kFanIn, n - gr * kFanIn);
-    const int64_t g0 = cut.first + (int64_t)gr * kFanIn;
-    auto slot = [&](int64_t block) { return slots + cut.slot(block) * SLOT; };
-    const bool leader = threadIdx.x == 0;
     auto done = [&](uint32_t* counter, uint32_t total) {
       return attn_completes<1, SOFT>(&s.flag, leader, counter, s.abort ? 0xffffffffu : total);
     };
-    if (done(counters + cut.slot(g0), size)) {
-      join(p, f, r, size, [&](int i) { return slot(g0 + i); }, groups > 1 ? slot(g0) : nullptr);
-      if (groups > 1 && done(counters + 2 * gridDim.x + cut.slot(cut.first), groups))
-        join(p, f, r, groups, [&](int i) { return slot(cut.first + (int64_t)i * kFanIn); }, nullptr);
+    if (done(counter, size)) {
+      if (used) join<false>(p, tmem, f, x, size, in_group, groups > 1 ? slot(g0) : nullptr, -1, 0.f, 0.f);
+      if (groups > 1 && done(counters + 2 * gridDim.x + cut.slot(cut.first), groups) && used)
+        join<false>(p, tmem, f, x, groups, [&](int i) { return slot(cut.first + (int64_t)i * kFanIn); }, nullptr, -1, 0.f, 0.f);
     }
     return ok;
   }
@@ -683,6 +731,11 @@ struct Tile {
       int64_t at = 0;
       int32_t step = 1;
       while (step < nm) step *= 32;
+      if (a.whole) {
+        k = (int32_t)(x - start);
+        at = k;
+        step = 0;
+      }
       for (step /= 32; step > 0; step /= 32) {  // before(k) <= x - start < before(k + 32 step)
         const int32_t mine = k + (int32_t)(threadIdx.x & 31) * step;
         const int64_t y = mine < nm ? Cost::before(p, r, mine, false) : INT64_MAX;
@@ -703,11 +756,11 @@ struct Tile {
       f.rows = min(R, r.n - k * R) * p.G;
       f.limit = Cost::sees(p, r, k);
       const int32_t nt = Cost::key_tiles(f.limit);
-      f.t0 = (int32_t)(x - start);
-      f.t1 = (int32_t)min((int64_t)nt, f.t0 + (a.hi - x));
+      f.t0 = a.whole ? 0 : (int32_t)(x - start);
+      f.t1 = a.whole ? nt : (int32_t)min((int64_t)nt, f.t0 + (a.hi - x));
       f.first = start >= a.lo ? (int64_t)blockIdx.x : div64(start, a.per);
-      f.last = start + nt <= a.hi ? (int64_t)blockIdx.x : div64(start + nt - 1, a.per);
-      x += f.t1 - f.t0;
+      f.last = a.whole || start + nt <= a.hi ? (int64_t)blockIdx.x : div64(start + nt - 1, a.per);
+      x += a.whole ? 1 : f.t1 - f.t0;
       if (x >= end || count == kFrags) break;
       start = x;  // the unit ended inside the run: the next one
       if (++k == nm) {
@@ -731,7 +784,7 @@ struct Tile {
   static __device__ __forceinline__ void fragments(const PagedAttnParams& p, Smem& s, const AttnShare& a, Body body) {
     int64_t run = 0, x = a.lo;
     for (int64_t b0 = 0; b0 < p.B && x < a.hi; b0 += THREADS) {
-      run = p.B <= THREADS ? a.total : Split::chunk(p, s.split, b0, run);
+      run = Split::chunk(p, s.split, b0, run, a.whole);
       while (x < a.hi && x < run) {
         if (LISTS && threadIdx.x < 32) list(p, s, b0, x, run, a);
         __syncthreads();

@@ -221,6 +221,8 @@ struct PagedAttnParams {
   FastDiv page, group;  // by ps; by G = Hq / Hkv
   int64_t rows_above, rows_upto;  // this launch takes the requests of rows_above < n * G <= rows_upto
   int64_t min_tiles;              // a block's run of key tiles is at least this long
+  int64_t join_tiles;             // what a cut unit costs, in tiles' time (0: units are always cut to even runs)
+  int32_t beside;                 // rows kernel: launched after the tile kernel of the same call
   int32_t tokens;                 // tile kernel: tokens of a row tile
   uint32_t polls, first_polls;    // tile kernel: bounds of its waits, of a warp's first for scores
 };
@@ -362,6 +364,7 @@ bool attn_tile_entry(int32_t dtype, int32_t D, AttnEntry* e);
 // Which attention kernels a call of T rows and B requests takes: the one of few rows, the tile kernel,
 // or both, each for its requests (of at most, of more than kTileRows rows; row: token and head of a group).
 constexpr int64_t kTileRows = 128;
+constexpr int64_t kTileJoin = 8;  // tile kernel: a cut unit's cost in tiles (12 us of 1.45 us tiles)
 constexpr int64_t kRowsRun = 4, kTileRun = 4;  // key tiles of a block's run at least
 struct AttnPlan {
   bool rows, tile;

@@ -1067,6 +1067,7 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
     q.rows_above = pl.rows ? kTileRows : 0;
     q.rows_upto = INT64_MAX;
     q.min_tiles = kTileRun;
+    q.join_tiles = kTileJoin;
     q.tokens = tile.rows / p.G;
     void* tp[3] = {&q, &mk, &mv};
     cfg.blockDimX = (unsigned)tile.threads;
@@ -1079,6 +1080,13 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
   p.rows_above = 0;
   p.rows_upto = pl.tile ? kTileRows : INT64_MAX;
   p.min_tiles = kRowsRun;
+  p.join_tiles = 0;
+  p.beside = pl.tile ? 1 : 0;
+  if (pl.tile) {  // starts beside the tile kernel (see the kernel)
+    attr.id = CU_LAUNCH_ATTRIBUTE_PROGRAMMATIC_STREAM_SERIALIZATION;
+    attr.value.programmaticStreamSerializationAllowed = 1;
+    cfg.numAttrs = 1;
+  }
   cfg.blockDimX = (unsigned)rows.threads;
   cfg.gridDimX = (unsigned)(scm->sm_count * rows.per_sm);
   cfg.sharedMemBytes = (unsigned)rows.smem;
