@@ -113,8 +113,9 @@ struct AttnSplit {
     bool ok = true;
     long long sum = 0, units = 0;
     int32_t longest = 0;
+    Request r{0, 0, 0};
     for (int64_t b = threadIdx.x; b < p.B; b += NT) {
-      const Request r = attn_request(p, b, &ok);
+      r = attn_request(p, b, &ok);
       if (!attn_takes(p, r.n)) continue;
       sum += Cost::of(p, r);
       if (p.join_tiles > 0) {
@@ -122,6 +123,7 @@ struct AttnSplit {
         longest = max(longest, Cost::longest(p, r));
       }
     }
+    const long long own = sum, own_units = units;  // of one request, where there are at most NT
     if (!ok && blockIdx.x == 0) atomicOr(p.err, kErrTable);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -153,16 +155,21 @@ struct AttnSplit {
     a.per = a.whole ? 1 : (even > p.min_tiles ? even : p.min_tiles);
     a.lo = min(a.total, (int64_t)blockIdx.x * a.per);
     a.hi = min(a.total, a.lo + a.per);
+    if (p.B <= NT) scan(s, r, a.whole ? own_units : own, 0);
     return a;
   }
 
-  // Fills the chunk of NT requests from b0 on; run: the tiles before it. Returns those after it.
-  static __device__ __forceinline__ int64_t chunk(const PagedAttnParams& p, Smem& s, int64_t b0, int64_t run, bool whole) {
+  // Fills the chunk of NT requests from b0 on (share has filled the only one of at most NT requests); run:
+  // the tiles before it. Returns those after it.
+  static __device__ __forceinline__ int64_t chunk(const PagedAttnParams& p, Smem& s, int64_t b0, int64_t run, const AttnShare& a) {
+    if (p.B <= NT) return a.total;
     const int64_t b = b0 + threadIdx.x;
     bool ok = true;
     Request r{0, 0, 0};
     if (b < p.B) r = attn_request(p, b, &ok);
-    const long long own = !attn_takes(p, r.n) ? 0 : whole ? Cost::units(p, r) : Cost::of(p, r);
+    return scan(s, r, !attn_takes(p, r.n) ? 0 : a.whole ? Cost::units(p, r) : Cost::of(p, r), run);
+  }
+  static __device__ __forceinline__ int64_t scan(Smem& s, const Request& r, long long own, int64_t run) {
     long long v = own;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {

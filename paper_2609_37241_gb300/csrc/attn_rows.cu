@@ -369,7 +369,7 @@ struct RowsKernel {
     bool bad = false;
     int64_t run = 0, x = a.lo;
     for (int64_t b0 = 0; b0 < p.B && x < a.hi; b0 += kRowsThreads) {
-      run = Split::chunk(p, s.split, b0, run, false);
+      run = Split::chunk(p, s.split, b0, run, a);
       while (x < a.hi && x < run) {
         const int rq = Split::find(s.split, x);
         Unit u;

@@ -384,7 +384,7 @@ struct Tile {
   static __device__ __forceinline__ void load_q(const PagedAttnParams& p, Smem& s, const Frag& f, int x) {
     constexpr int CH = D / 8, RPI = 32 / CH > 0 ? 32 / CH : 1, ITER = 32 / RPI;
     const int w = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, c = lane % CH, rr = lane / CH;
-    constexpr int BATCH = 8;  // loads in flight, none behind a branch: rows past the unit load its last and drop it
+    constexpr int BATCH = ITER < 16 ? ITER : 16;  // loads in flight, none behind a branch: rows past the unit load its last and drop it
 #pragma unroll 1
     for (int i = 0; i < ITER; i += BATCH) {
       uint4 v[BATCH];
@@ -565,83 +565,74 @@ struct Tile {
     const int row = x * 128 + (threadIdx.x & 127), r = min(row, f.rows - 1);  // rows past the unit do the last's again
     const bool live = row < f.rows;
     const uint32_t oc = tmem + (((threadIdx.x >> 5) & 3) << 21) + O_COL + x * D;
-    float m = -INFINITY, l = 0.f, w[kFanIn], ls[kFanIn];
+    float m = OWN ? m_own : -INFINITY;
+#pragma unroll 1
+    for (int i = 0; i < n; i += 4) {  // four slots' maxima at a time (the last one's again past it)
+      float z[4];
 #pragma unroll
-    for (int i = 0; i < kFanIn; ++i) {  // the last slot's again past it
-      const float* z = at(min(i, n - 1)) + r;
-      w[i] = __ldcg(z);
-      ls[i] = __ldcg(z + ROWS);
-    }
+      for (int e = 0; e < 4; ++e) z[e] = __ldcg(at(min(i + e, n - 1)) + r);
 #pragma unroll
-    for (int i = 0; i < kFanIn; ++i) {
-      if (OWN && min(i, n - 1) == own) {
-        w[i] = m_own;
-        ls[i] = l_own;
-      }
-      m = fmaxf(m, w[i]);
+      for (int e = 0; e < 4; ++e)
+        if (!OWN || min(i + e, n - 1) != own) m = fmaxf(m, z[e]);
     }
     const float base = m == -INFINITY ? 0.f : m;
-    float w_own = 0.f;
-#pragma unroll
-    for (int i = 0; i < kFanIn; ++i) {
-      w[i] = i < n ? fast_exp2(w[i] - base) : 0.f;
-      l = fmaf(w[i], ls[i], l);
-      if (OWN && i == own) {
-        w_own = w[i];
-        w[i] = 0.f;
-      }
-    }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
     int64_t at_row = 0;
     char* out = out_row(p, f, r, &at_row);
-    const int skip = own == 0 ? 1 : 0;  // a slot to read in the place of this block's (n > 1)
+    float l = 0.f;
+    // 64 columns at a time, a slot at a time with all of its loads in flight: little code, which a block that
+    // seldom comes here first has to fetch.
 #pragma unroll 1
-    for (int d = 0; d < D; d += 32) {  // 32 columns at a time: eight loads of a slot in flight, two slots'
-      float v[32] = {};
+    for (int c = 0; c < D; c += 64) {
+      float v[64];
 #pragma unroll
-      for (int i = 0; i < kFanIn; i += 2) {
-        if (i >= n) break;
-        float4 a[8], b[8];
-        const int i0 = OWN && i == own ? skip : i, i1 = OWN && (i + 1 == own || i + 1 >= n) ? skip : min(i + 1, n - 1);
-        const float* z = at(i0) + 2 * ROWS + ((int64_t)d / 4 * ROWS + r) * 4;
-        const float* y = at(i1) + 2 * ROWS + ((int64_t)d / 4 * ROWS + r) * 4;  // weight 0 past the last
+      for (int e = 0; e < 64; ++e) v[e] = 0.f;
+      l = 0.f;
+#pragma unroll 1
+      for (int i = 0; i < n; ++i) {
+        if (OWN && i == own) {
+          const float w = fast_exp2(m_own - base);
+          l = fmaf(w, l_own, l);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          a[e] = __ldcg(reinterpret_cast<const float4*>(z + e * ROWS * 4));
-          b[e] = __ldcg(reinterpret_cast<const float4*>(y + e * ROWS * 4));
+          for (int d = 0; d < 64; d += 32) {
+            uint32_t o[32];
+            __syncwarp();
+            tc_ld32(oc + c + d, o);
+            tc_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[d + e] = fmaf(w, __uint_as_float(o[e]), v[d + e]);
+          }
+          continue;
         }
+        const float* z = at(i);
+        const float w = fast_exp2(__ldcg(z + r) - base);
+        l = fmaf(w, __ldcg(z + ROWS + r), l);
+        const float4* q = reinterpret_cast<const float4*>(z + 2 * ROWS) + c / 4 * ROWS + r;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          v[4 * e] = fmaf(w[i + 1], b[e].x, fmaf(w[i], a[e].x, v[4 * e]));
-          v[4 * e + 1] = fmaf(w[i + 1], b[e].y, fmaf(w[i], a[e].y, v[4 * e + 1]));
-          v[4 * e + 2] = fmaf(w[i + 1], b[e].z, fmaf(w[i], a[e].z, v[4 * e + 2]));
-          v[4 * e + 3] = fmaf(w[i + 1], b[e].w, fmaf(w[i], a[e].w, v[4 * e + 3]));
+        for (int e = 0; e < 16; ++e) {
+          const float4 a = __ldcg(q + e * ROWS);
+          v[4 * e] = fmaf(w, a.x, v[4 * e]);
+          v[4 * e + 1] = fmaf(w, a.y, v[4 * e + 1]);
+          v[4 * e + 2] = fmaf(w, a.z, v[4 * e + 2]);
+          v[4 * e + 3] = fmaf(w, a.w, v[4 * e + 3]);
         }
       }
-      if (OWN) {
-        uint32_t o[32];
-        __syncwarp();
-        tc_ld32(oc + d, o);
-        tc_wait_ld();
+      if (!live) continue;
+      if (dst) {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] = fmaf(w_own, __uint_as_float(o[e]), v[e]);
-      }
-      if (dst && live) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          *reinterpret_cast<float4*>(dst + 2 * ROWS + ((int64_t)(d / 4 + e) * ROWS + r) * 4) =
+        for (int e = 0; e < 16; ++e)
+          *reinterpret_cast<float4*>(dst + 2 * ROWS + ((c / 4 + e) * ROWS + r) * 4) =
               make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
-      }
-      if (!dst && live) {
+      } else {
+        const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] *= inv;
+        for (int e = 0; e < 64; ++e) v[e] *= inv;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) st16(out + (d + 8 * e) * 2, pack<DT>(v + 8 * e));
+        for (int e = 0; e < 8; ++e) st16(out + (c + e * 8) * 2, pack<DT>(v + 8 * e));
       }
     }
     if (OWN) tc_before();
     if (!live) return;
-    if (dst) {
+    if (dst) {  // the group's first slot, whose m and l this thread has read
       dst[r] = m;
       dst[ROWS + r] = l;
     } else {
@@ -784,7 +775,7 @@ struct Tile {
   static __device__ __forceinline__ void fragments(const PagedAttnParams& p, Smem& s, const AttnShare& a, Body body) {
     int64_t run = 0, x = a.lo;
     for (int64_t b0 = 0; b0 < p.B && x < a.hi; b0 += THREADS) {
-      run = Split::chunk(p, s.split, b0, run, a.whole);
+      run = Split::chunk(p, s.split, b0, run, a);
       while (x < a.hi && x < run) {
         if (LISTS && threadIdx.x < 32) list(p, s, b0, x, run, a);
         __syncthreads();
