@@ -90,8 +90,13 @@ AttnPlan attn_plan(const AttnEntry& tile, int64_t T, int64_t B, int64_t G, int64
   return {B > 1, true};
 }
 
+// per_sm blocks on every SM; at most kMaxAttnBlocks, whose parts two rounds of kFanIn join.
+int32_t attn_blocks(const AttnEntry& e, int32_t sms) {
+  return sms * e.per_sm < kMaxAttnBlocks ? sms * e.per_sm : kMaxAttnBlocks;
+}
+
 int64_t attn_work_floats(const AttnEntry& e, int32_t sms) {
-  const int64_t blocks = (int64_t)sms * e.per_sm;
+  const int64_t blocks = attn_blocks(e, sms);
   return e.fn ? attn_counters(blocks) + 2 * blocks * e.slot_floats : 0;
 }
 

@@ -41,7 +41,6 @@ __device__ __forceinline__ Request attn_request(const PagedAttnParams& p, int64_
 
 // Workspace: counters (zero between calls), then two slots of rows * (D + 2) floats per block: slot 2c
 // for the unit that a block's run starts within, 2c + 1 for the one that it ends within.
-constexpr int kFanIn = 16;
 __host__ __device__ constexpr int64_t attn_counters(int64_t blocks) { return (4 * blocks + 31) / 32 * 32; }
 __host__ __device__ constexpr int64_t attn_slot_floats(int rows, int D) { return (int64_t)rows * (D + 2); }
 
@@ -205,6 +204,10 @@ struct AttnSplit {
     return r;
   }
 };
+
+__device__ __forceinline__ int64_t attn_div(int64_t a, int64_t b) {  // a, b >= 0
+  return ((uint64_t)a | (uint64_t)b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
 
 // A fragment's place: unit tiles [u0, u1) of the call, cut into runs of `per` tiles.
 struct AttnCuts {

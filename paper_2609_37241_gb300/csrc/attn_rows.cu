@@ -30,7 +30,7 @@ struct RowsGeom {
   static constexpr int NS = D == 64 ? 6 : 3;    // stages per warp: 24 KB in flight, D 256 48 KB
   static constexpr int RING = 4 * NS * STAGE;
   static constexpr int PER_SM = D == 256 ? 1 : 2;
-  // after the ring's use, in its place: out of four warps, 16 rows each; then the joins' weights
+  static constexpr int PASS = 512 / D;          // rows that the warps join at a time: a float4 per thread
   static constexpr int LDO = D + 4;
 };
 
@@ -59,14 +59,18 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool live) {
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
 
-// A unit: 16 rows from r0 of request (q0, n, kv), kv head h.
+// A fragment of a unit: 16 rows from r0 of request (q0, n, kv), kv head h, key tiles [t0, t1).
 struct Unit {
-  int64_t b;
+  int64_t b, first, last;                 // request; blocks that share the unit
   int32_t q0, n, kv, h, r0, rows, limit;  // rows: of the 16 that exist; limit: keys that the last one sees
+  int32_t t0, t1;
 };
 
 // Every row tile counted with all of the request's keys: exact for decode steps, a little unequal where a
-// long chunk comes this way.
+// long chunk comes this way; and with kUnitTiles for its beginning and end, which take a block as long as
+// that many tiles do (a block of many short units would otherwise be the last: 48 requests of about 3 rows of
+// D 64, the slowest block 38.9 us, the median one 28.7). A cut in these tiles moves to the unit's beginning.
+constexpr int kUnitTiles = 3;
 struct RowsCost {
   static __device__ __forceinline__ int64_t row_tiles(const PagedAttnParams& p, int32_t n) {
     return ((int64_t)n * p.G + kRowsTile - 1) / kRowsTile;
@@ -79,7 +83,7 @@ struct RowsCost {
   }
   static __device__ __forceinline__ int32_t longest(const PagedAttnParams&, const Request& r) { return (int32_t)key_tiles(r.kv); }
   static __device__ __forceinline__ int64_t of(const PagedAttnParams& p, const Request& r) {
-    return units(p, r) * key_tiles(r.kv);
+    return units(p, r) * (key_tiles(r.kv) + kUnitTiles);
   }
 };
 
@@ -87,31 +91,40 @@ template <int DT, int D>
 struct RowsKernel {
   using G = RowsGeom<D>;
   using Split = AttnSplit<kRowsThreads, RowsCost>;
+  static constexpr int kSlots = kFanIn > kJoinGroups ? kFanIn : kJoinGroups;  // slots of a join at most
   struct Smem {
     alignas(128) char ring[G::RING];
+    alignas(16) float part[4][G::PASS][G::LDO];
     typename Split::Smem split;
     float m[4][16], l[4][16];
+    float sm[kSlots][16], sl[kSlots][16];  // m and l of the slots of a join
     int last;
   };
 
-  // Issues the copies of 16 keys from j0 on into a stage.
+  // The table's entry for the lane's row (lane mod 16) of the 16 keys from j0 on. It is asked for a stage
+  // before its copies are issued, so that they do not wait for it.
+  static __device__ __forceinline__ int32_t entry(const PagedAttnParams& p, const Unit& u, int32_t j0) {
+    const uint32_t j = (uint32_t)min(j0 + (int32_t)(threadIdx.x & 15), u.limit - 1);
+    return p.table[u.b * p.table_rs + fast_div(j, p.page.magic, p.page.shift)];
+  }
+
+  // Issues the copies of 16 keys from j0 on into a stage; page: what entry() gave for them.
   static __device__ __forceinline__ void load(const PagedAttnParams& p, const Unit& u, const char* kb, const char* vb,
-                                              int32_t j0, uint32_t stage, bool* bad) {
+                                              int32_t j0, int32_t page, uint32_t stage, bool* bad) {
     const int lane = threadIdx.x & 31;
     constexpr int RPI = 32 / G::CH > 0 ? 32 / G::CH : 1;  // rows per instruction (D 256: one)
     constexpr int ITER = 16 / RPI;
     const int c = lane % G::CH, rr = lane / G::CH;
-    const int32_t* table = p.table + u.b * p.table_rs;
+    if (page < 0 || page >= p.P) {
+      *bad = true;
+      page = 0;
+    }
+    const uint32_t j = (uint32_t)min(j0 + (lane & 15), u.limit - 1);
+    const int32_t at = (int32_t)(j - fast_div(j, p.page.magic, p.page.shift) * (uint32_t)p.page.d);
     if (p.page.d % 16 == 0) {  // one page for all 16 rows
-      const uint32_t pg = fast_div((uint32_t)j0, p.page.magic, p.page.shift);
-      const uint32_t at = (uint32_t)j0 - pg * (uint32_t)p.page.d;
-      int64_t page = table[pg];
-      if (page < 0 || page >= p.P) {
-        *bad = true;
-        page = 0;
-      }
-      const char* ks = kb + (page * p.kc.page + (int64_t)(at + rr) * p.kc.row + c * 8) * 2;
-      const char* vs = vb + (page * p.vc.page + (int64_t)(at + rr) * p.vc.row + c * 8) * 2;
+      const int32_t at0 = __shfl_sync(0xffffffffu, at, 0);
+      const char* ks = kb + ((int64_t)page * p.kc.page + (int64_t)(at0 + rr) * p.kc.row + c * 8) * 2;
+      const char* vs = vb + ((int64_t)page * p.vc.page + (int64_t)(at0 + rr) * p.vc.row + c * 8) * 2;
       const int64_t kstep = RPI * p.kc.row * 2, vstep = RPI * p.vc.row * 2;
 #pragma unroll
       for (int i = 0; i < ITER; ++i) {
@@ -121,97 +134,110 @@ struct RowsKernel {
         cp16(dst, live ? ks + i * kstep : kb, live);
         cp16(dst + G::HALF, live ? vs + i * vstep : vb, live);
       }
-    } else {
-#pragma unroll 2
+    } else {  // each row's place from the lane that looked it up
+      const int64_t ko = ((int64_t)page * p.kc.page + (int64_t)at * p.kc.row) * 2;
+      const int64_t vo = ((int64_t)page * p.vc.page + (int64_t)at * p.vc.row) * 2;
+#pragma unroll
       for (int i = 0; i < ITER; ++i) {
         const int r = rr + i * RPI;
         const bool live = j0 + r < u.limit;
-        int64_t ko = 0, vo = 0;
-        if (live) {
-          const uint32_t j = (uint32_t)(j0 + r), pg = fast_div(j, p.page.magic, p.page.shift);
-          const int64_t at = j - pg * (uint32_t)p.page.d;
-          int64_t page = table[pg];
-          if (page < 0 || page >= p.P) {
-            *bad = true;
-            page = 0;
-          }
-          ko = (page * p.kc.page + at * p.kc.row + c * 8) * 2;
-          vo = (page * p.vc.page + at * p.vc.row + c * 8) * 2;
-        }
+        const int64_t kr = __shfl_sync(0xffffffffu, ko, r), vr = __shfl_sync(0xffffffffu, vo, r);
         const uint32_t dst = stage + r * (D * 2) + ((c ^ (r & 7)) << 4);
-        cp16(dst, kb + ko, live);
-        cp16(dst + G::HALF, vb + vo, live);
+        cp16(dst, live ? kb + kr + c * 16 : kb, live);
+        cp16(dst + G::HALF, live ? vb + vr + c * 16 : vb, live);
       }
     }
   }
 
-  // Key tiles [t0, t1) of a unit; leaves every warp's m, l and unnormalised out in shared memory.
-  static __device__ __forceinline__ void fragment(const PagedAttnParams& p, Smem& s, const Unit& u, int64_t t0,
-                                                  int64_t t1, bool* bad) {
+  // What a warp holds of a fragment between its first loads and its last product.
+  struct State {
+    const char *kb, *vb;
+    int32_t first, groups;  // its 16-key groups: keys first + 64 x, x < groups
+    int32_t page;           // entry() of the next group to copy
+    int32_t see[2];         // keys that rows g and g + 8 see
+    uint32_t q[D / 16][4];
+  };
+
+  // Starts a fragment: q, and the copies of the first NS - 1 stages. The ring is the warp's own, so this comes
+  // before the fragment before has been joined.
+  static __device__ __forceinline__ void start(const PagedAttnParams& p, Smem& s, const Unit& u, State& st, bool* bad) {
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const char* kb = reinterpret_cast<const char*>(p.kc.base) + (int64_t)u.h * p.kc.head * 2;
-    const char* vb = reinterpret_cast<const char*>(p.vc.base) + (int64_t)u.h * p.vc.head * 2;
+    const char* src[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int32_t r = u.r0 + min(g + 8 * k, u.rows - 1);
+      const int32_t i = (int32_t)fast_div((uint32_t)r, p.group.magic, p.group.shift);
+      st.see[k] = u.kv - u.n + i + 1;
+      src[k] = row_ptr(p.q, u.q0 + i, p.q_rs, 2) + ((int64_t)u.h * p.G + (r - i * p.G)) * D * 2;
+    }
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        st.q[kk][e] = *reinterpret_cast<const uint32_t*>(src[e & 1] + (kk * 16 + (e >> 1) * 8 + 2 * t) * 2);
+    st.kb = reinterpret_cast<const char*>(p.kc.base) + (int64_t)u.h * p.kc.head * 2;
+    st.vb = reinterpret_cast<const char*>(p.vc.base) + (int64_t)u.h * p.vc.head * 2;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s.ring) + w * (G::NS * G::STAGE);
-    // this warp's 16-key groups: keys 16 (4 x + w), x in [t0, t1), up to the limit
-    const int32_t first = (int32_t)t0 * kRowsKeys + 16 * w;
-    const int32_t upto = (int32_t)min((int64_t)u.limit, t1 * kRowsKeys);
-    const int groups = first < upto ? (upto - first + kRowsKeys - 1) / kRowsKeys : 0;
+    st.first = u.t0 * kRowsKeys + 16 * w;
+    const int32_t upto = (int32_t)min((int64_t)u.limit, (int64_t)u.t1 * kRowsKeys);
+    st.groups = st.first < upto ? (upto - st.first + kRowsKeys - 1) / kRowsKeys : 0;
+    int32_t page[G::NS];
+#pragma unroll
+    for (int i = 0; i < G::NS; ++i) page[i] = i < st.groups ? entry(p, u, st.first + i * kRowsKeys) : 0;
 #pragma unroll
     for (int i = 0; i < G::NS - 1; ++i) {
-      if (i < groups) load(p, u, kb, vb, first + i * kRowsKeys, ring + i * G::STAGE, bad);
+      if (i < st.groups) load(p, u, st.kb, st.vb, st.first + i * kRowsKeys, page[i], ring + i * G::STAGE, bad);
       cp_commit();
     }
-    // rows g and g + 8 of the unit: q and how far they see
-    uint32_t qf[D / 16][4];
-    int32_t see[2];
-    {
-      const char* src[2];
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int32_t r = u.r0 + min(g + 8 * k, u.rows - 1);
-        const int32_t i = (int32_t)fast_div((uint32_t)r, p.group.magic, p.group.shift);
-        see[k] = u.kv - u.n + i + 1;
-        src[k] = row_ptr(p.q, u.q0 + i, p.q_rs, 2) + ((int64_t)u.h * p.G + (r - i * p.G)) * D * 2;
-      }
-#pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          qf[kk][e] = *reinterpret_cast<const uint32_t*>(src[e & 1] + (kk * 16 + (e >> 1) * 8 + 2 * t) * 2);
-    }
+    st.page = page[G::NS - 1];
+  }
+
+  // The warp's keys of a fragment: m, l (of rows g and g + 8) and the unnormalised out.
+  static __device__ __forceinline__ void body(const PagedAttnParams& p, Smem& s, const Unit& u, State& st, float* m,
+                                              float* l, float (*o)[4], bool* bad) {
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, t = lane & 3;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s.ring) + w * (G::NS * G::STAGE);
     const float c = p.scale * kLog2e;
-    float o[D / 8][4];
 #pragma unroll
     for (int i = 0; i < D / 8; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    m[0] = m[1] = -INFINITY;
+    l[0] = l[1] = 0.f;
     const int mi = lane >> 3, mr = lane & 7;
-    for (int x = 0; x < groups; ++x) {
+    for (int x = 0; x < st.groups; ++x) {
       cp_wait<G::NS - 2>();
       __syncwarp();  // all lanes' copies have landed, and the stage refilled below has been read
       {
         const int y = x + G::NS - 1;
-        if (y < groups) load(p, u, kb, vb, first + y * kRowsKeys, ring + (y % G::NS) * G::STAGE, bad);
+        if (y < st.groups) {
+          const int32_t page = st.page;
+          if (y + 1 < st.groups) st.page = entry(p, u, st.first + (y + 1) * kRowsKeys);
+          load(p, u, st.kb, st.vb, st.first + y * kRowsKeys, page, ring + (y % G::NS) * G::STAGE, bad);
+        }
         cp_commit();
       }
-      const uint32_t st = ring + (x % G::NS) * G::STAGE;
-      float sc[2][4] = {};
+      const uint32_t at = ring + (x % G::NS) * G::STAGE;
+      float sc[2][4] = {}, odd[2][4] = {};  // two chains of products, half as long
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
         uint32_t kf[4];
         const int key = (mi >> 1) * 8 + mr, ch = kk * 2 + (mi & 1);
-        ldsm4(kf, st + key * (D * 2) + ((ch ^ (key & 7)) << 4));
-        mma16816<DT>(sc[0], qf[kk], kf[0], kf[1]);
-        mma16816<DT>(sc[1], qf[kk], kf[2], kf[3]);
+        ldsm4(kf, at + key * (D * 2) + ((ch ^ (key & 7)) << 4));
+        mma16816<DT>(kk & 1 ? odd[0] : sc[0], st.q[kk], kf[0], kf[1]);
+        mma16816<DT>(kk & 1 ? odd[1] : sc[1], st.q[kk], kf[2], kf[3]);
       }
-      const int32_t j0 = first + x * kRowsKeys;
-      if (j0 + 16 > min(see[0], see[1]))  // some key is hidden from a row
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[nt][e] += odd[nt][e];
+      const int32_t j0 = st.first + x * kRowsKeys;
+      if (j0 + 16 > min(st.see[0], st.see[1]))  // some key is hidden from a row
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (j0 + nt * 8 + 2 * t + (e & 1) >= see[e >> 1]) sc[nt][e] = -INFINITY;
+            if (j0 + nt * 8 + 2 * t + (e & 1) >= st.see[e >> 1]) sc[nt][e] = -INFINITY;
       float top[2];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -248,62 +274,109 @@ struct RowsKernel {
       for (int dd = 0; dd < D / 16; ++dd) {
         uint32_t vf[4];
         const int key = (mi & 1) * 8 + mr, ch = dd * 2 + (mi >> 1);
-        ldsm4t(vf, st + G::HALF + key * (D * 2) + ((ch ^ (key & 7)) << 4));
+        ldsm4t(vf, at + G::HALF + key * (D * 2) + ((ch ^ (key & 7)) << 4));
         mma16816<DT>(o[2 * dd], pf, vf[0], vf[1]);
         mma16816<DT>(o[2 * dd + 1], pf, vf[2], vf[3]);
       }
     }
     cp_wait<0>();
+    __syncwarp();  // the ring has been read by all lanes
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       l[k] += __shfl_xor_sync(0xffffffffu, l[k], 1);
       l[k] += __shfl_xor_sync(0xffffffffu, l[k], 2);
     }
-    __syncthreads();  // every warp is done with its ring: the partial outs take its place
-    float* so = reinterpret_cast<float*>(s.ring);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int row = g + 8 * k;
-      if (row < u.rows) {
-        if (t == 0) {
-          s.m[w][row] = m[k];
-          s.l[w][row] = l[k];
-        }
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i)
-          *reinterpret_cast<float2*>(so + (w * 16 + row) * G::LDO + i * 8 + 2 * t) = make_float2(o[i][2 * k], o[i][2 * k + 1]);
-      }
-    }
-    __syncthreads();
   }
 
-  // Joins the four warps of a fragment: into out and lse, or unnormalised into a workspace slot.
-  static __device__ __forceinline__ void join_warps(const PagedAttnParams& p, Smem& s, const Unit& u, float* slot) {
-    const float* so = reinterpret_cast<const float*>(s.ring);
-    for (int e = threadIdx.x; e < u.rows * (D / 4); e += kRowsThreads) {
-      const int row = e / (D / 4), d = e % (D / 4) * 4;
-      float m = -INFINITY;
+  // m and l of the slots at(i), i < n, i != own, into shared memory: one round of loads.
+  template <class At>
+  static __device__ __forceinline__ void slot_stats(Smem& s, const Unit& u, int n, int own, At at) {
+    for (int e = threadIdx.x; e < n * 16; e += kRowsThreads) {
+      const int i = e / 16, row = e % 16;
+      if (i == own || row >= u.rows) continue;
+      s.sm[i][row] = __ldcg(at(i) + row);
+      s.sl[i][row] = __ldcg(at(i) + kRowsTile + row);
+    }
+  }
+  static __device__ __forceinline__ float slot_max(const Smem& s, int row, int n, int own) {
+    float m = -INFINITY;
+    for (int i = 0; i < n; ++i)
+      if (i != own) m = fmaxf(m, s.sm[i][row]);
+    return m;
+  }
+  // Adds the slots scaled to `base`, four loads in flight at a time.
+  template <class At>
+  static __device__ __forceinline__ void add_slots(const Smem& s, float4& a, float& l, float base, int row, int d, int n,
+                                                   int own, At at) {
+    for (int i0 = 0; i0 < n; i0 += 8) {
+      float4 v[8];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) m = fmaxf(m, s.m[w][row]);
-      const float base = m == -INFINITY ? 0.f : m;
-      float l = 0.f;
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float f = fast_exp2(s.m[w][row] - base);
-        const float4 v = *reinterpret_cast<const float4*>(so + (w * 16 + row) * G::LDO + d);
-        l = fmaf(f, s.l[w][row], l);
-        a.x = fmaf(f, v.x, a.x); a.y = fmaf(f, v.y, a.y); a.z = fmaf(f, v.z, a.z); a.w = fmaf(f, v.w, a.w);
+      for (int e = 0; e < 8; ++e) {
+        const int i = min(i0 + e, n - 1);
+        v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i != own) v[e] = __ldcg(reinterpret_cast<const float4*>(at(i) + 2 * kRowsTile + row * D + d));
       }
-      if (slot) {
-        *reinterpret_cast<float4*>(slot + 2 * kRowsTile + row * D + d) = a;
-        if (d == 0) {
-          slot[row] = m;
-          slot[kRowsTile + row] = l;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int i = i0 + e;
+        if (i >= n || i == own) continue;
+        const float f = fast_exp2(s.sm[i][row] - base);
+        l = fmaf(f, s.sl[i][row], l);
+        a.x = fmaf(f, v[e].x, a.x); a.y = fmaf(f, v[e].y, a.y); a.z = fmaf(f, v[e].z, a.z); a.w = fmaf(f, v[e].w, a.w);
+      }
+    }
+  }
+
+  // Joins the four warps of a fragment, PASS rows at a time: into out and lse; unnormalised into a workspace
+  // slot; or, where it is the unit's last part, with the n - 1 other slots `at(i)`, i != own, into out and lse.
+  template <class At>
+  static __device__ __forceinline__ void join_warps(const PagedAttnParams& p, Smem& s, const Unit& u, const float* m,
+                                                    const float* l, const float (*o)[4], float* slot, int n, int own, At at) {
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (t == 0) {
+        s.m[w][g + 8 * k] = m[k];
+        s.l[w][g + 8 * k] = l[k];
+      }
+    slot_stats(s, u, n, own, at);
+    for (int p0 = 0; p0 < u.rows; p0 += G::PASS) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int row = g + 8 * k;
+        if (row >= p0 && row < p0 + G::PASS) {
+#pragma unroll
+          for (int i = 0; i < D / 8; ++i)
+            *reinterpret_cast<float2*>(&s.part[w][row - p0][i * 8 + 2 * t]) = make_float2(o[i][2 * k], o[i][2 * k + 1]);
         }
-      } else {
-        put(p, u, row, d, a, m, l);
       }
+      __syncthreads();
+      const int at_row = threadIdx.x / (D / 4), row = p0 + at_row, d = threadIdx.x % (D / 4) * 4;
+      if (row < u.rows) {
+        float mm = slot_max(s, row, n, own), ll = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mm = fmaxf(mm, s.m[i][row]);
+        const float base = mm == -INFINITY ? 0.f : mm;
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float f = fast_exp2(s.m[i][row] - base);
+          const float4 v = *reinterpret_cast<const float4*>(&s.part[i][at_row][d]);
+          ll = fmaf(f, s.l[i][row], ll);
+          a.x = fmaf(f, v.x, a.x); a.y = fmaf(f, v.y, a.y); a.z = fmaf(f, v.z, a.z); a.w = fmaf(f, v.w, a.w);
+        }
+        add_slots(s, a, ll, base, row, d, n, own, at);
+        if (slot) {
+          *reinterpret_cast<float4*>(slot + 2 * kRowsTile + row * D + d) = a;
+          if (d == 0) {
+            slot[row] = mm;
+            slot[kRowsTile + row] = ll;
+          }
+        } else {
+          put(p, u, row, d, a, mm, ll);
+        }
+      }
+      __syncthreads();
     }
   }
 
@@ -321,93 +394,133 @@ struct RowsKernel {
     if (d == 0) p.lse[t * p.Hq + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
   }
 
-  // Joins n workspace slots, `at(i)` the i-th; as join_warps otherwise (dst may be the first of them).
+  // Joins n workspace slots, `at(i)` the i-th, into out and lse or into dst, the first of them.
   template <class At>
   static __device__ __forceinline__ void join_slots(const PagedAttnParams& p, Smem& s, const Unit& u, int n, At at,
                                                     float* dst) {
+    slot_stats(s, u, n, -1, at);
+    __syncthreads();
     for (int e = threadIdx.x; e < u.rows * (D / 4); e += kRowsThreads) {
       const int row = e / (D / 4), d = e % (D / 4) * 4;
-      float m = -INFINITY;
-#pragma unroll 4
-      for (int i = 0; i < n; ++i) m = fmaxf(m, __ldcg(at(i) + row));
-      const float base = m == -INFINITY ? 0.f : m;
+      const float m = slot_max(s, row, n, -1);
       float l = 0.f;
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-      for (int i = 0; i < n; ++i) {
-        const float* z = at(i);
-        const float f = fast_exp2(__ldcg(z + row) - base);
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(z + 2 * kRowsTile + row * D + d));
-        l = fmaf(f, __ldcg(z + kRowsTile + row), l);
-        a.x = fmaf(f, v.x, a.x); a.y = fmaf(f, v.y, a.y); a.z = fmaf(f, v.z, a.z); a.w = fmaf(f, v.w, a.w);
-      }
-      if (dst) {
+      add_slots(s, a, l, m == -INFINITY ? 0.f : m, row, d, n, -1, at);
+      if (dst) {  // its m and l have been read by all, and its elements d .. d + 3 by this thread alone
         *reinterpret_cast<float4*>(dst + 2 * kRowsTile + row * D + d) = a;
         if (d == 0) {
-          s.m[0][row] = m;
-          s.l[0][row] = l;
+          dst[row] = m;
+          dst[kRowsTile + row] = l;
         }
       } else {
         put(p, u, row, d, a, m, l);
       }
     }
-    if (dst) {  // m and l last (dst is a slot, whose m and l every thread of the row reads)
+  }
+
+  // The end of a fragment whose keys are done.
+  static __device__ __forceinline__ void finish(const PagedAttnParams& p, Smem& s, const Unit& u, const float* m,
+                                                const float* l, const float (*o)[4]) {
+    uint32_t* counters = reinterpret_cast<uint32_t*>(p.work);
+    float* slots = p.work + attn_counters(gridDim.x);
+    constexpr int64_t SLOT = attn_slot_floats(kRowsTile, D);
+    const AttnCuts cut{u.first, u.last};
+    const int n = (int)(cut.last - cut.first + 1), f = (int)(blockIdx.x - cut.first);
+    const int groups = (n + kFanIn - 1) / kFanIn, gr = f / kFanIn;
+    const int64_t g0 = cut.first + (int64_t)gr * kFanIn;
+    const int size = min(kFanIn, n - gr * kFanIn);
+    uint32_t* counter = counters + cut.slot(g0);
+    auto slot = [&](int64_t block) { return slots + cut.slot(block) * SLOT; };
+    auto in_group = [&](int i) { return slot(g0 + i); };
+    // A unit that goes on past this block's run: the blocks after this one began with it, so they mostly are
+    // done, and this part is joined with theirs without a turn through the workspace.
+    bool last = false;
+    if (u.last > blockIdx.x && groups == 1) {
+      if (threadIdx.x == 0) s.last = *reinterpret_cast<volatile uint32_t*>(counter) + 1 == (uint32_t)size;
       __syncthreads();
-      if (threadIdx.x < u.rows) {
-        dst[threadIdx.x] = s.m[0][threadIdx.x];
-        dst[kRowsTile + threadIdx.x] = s.l[0][threadIdx.x];
-      }
+      last = s.last != 0;
+      if (last) __threadfence();
+    }
+    const bool done = cut.whole() || last;
+    join_warps(p, s, u, m, l, o, done ? nullptr : slot(blockIdx.x), last ? size : 0, f, in_group);
+    if (last && threadIdx.x == 0) *counter = 0u;
+    if (done) return;
+    if (attn_completes<0, kRowsThreads>(&s.last, threadIdx.x == 0, counter, size)) {
+      join_slots(p, s, u, size, in_group, groups > 1 ? slot(g0) : nullptr);
+      if (groups > 1 && attn_completes<0, kRowsThreads>(&s.last, threadIdx.x == 0,
+                                                        counters + 2 * gridDim.x + cut.slot(cut.first), groups))
+        join_slots(p, s, u, groups, [&](int i) { return slot(cut.first + (int64_t)i * kFanIn); }, nullptr);
     }
   }
 
   static __device__ __forceinline__ void run(const PagedAttnParams& p, Smem& s) {
     const AttnShare a = Split::share(p, s.split);
     attn_fill_tail<kRowsThreads>(p);
-    uint32_t* counters = reinterpret_cast<uint32_t*>(p.work);
-    float* slots = p.work + attn_counters(gridDim.x);
-    constexpr int64_t SLOT = attn_slot_floats(kRowsTile, D);
     bool bad = false;
     int64_t run = 0, x = a.lo;
     for (int64_t b0 = 0; b0 < p.B && x < a.hi; b0 += kRowsThreads) {
       run = Split::chunk(p, s.split, b0, run, a);
-      while (x < a.hi && x < run) {
-        const int rq = Split::find(s.split, x);
-        Unit u;
+      const int64_t end = min(a.hi, run);
+      if (x >= end) continue;
+      // the unit that holds x; those after it follow one another
+      int rq = Split::find(s.split, x);
+      Unit u;
+      int64_t start_of;  // its first tile, of kUnitTiles + nt
+      int32_t nt, nm, mt;
+      auto request_of = [&]() {
         u.b = b0 + rq;
         u.q0 = s.split.q0[rq];
         u.n = s.split.n[rq];
         u.kv = s.split.kv[rq];
-        const int64_t nt = RowsCost::key_tiles(u.kv), nm = RowsCost::row_tiles(p, u.n);
-        const int64_t rel = x - s.split.pre[rq], unit = rel / nt, t0 = rel - unit * nt;
-        const int64_t t1 = min(nt, t0 + a.hi - x);
-        u.h = (int32_t)(unit / nm);
-        u.r0 = (int32_t)(unit - u.h * nm) * kRowsTile;
+        nt = (int32_t)RowsCost::key_tiles(u.kv);
+        nm = (int32_t)RowsCost::row_tiles(p, u.n);
+      };
+      request_of();
+      {
+        const int64_t unit = attn_div(x - s.split.pre[rq], nt + kUnitTiles);
+        start_of = s.split.pre[rq] + unit * (nt + kUnitTiles);
+        u.h = (int32_t)attn_div(unit, nm);
+        mt = (int32_t)(unit - (int64_t)u.h * nm);
+      }
+      // This block's part of the unit at x; false where its run ends before the unit's keys.
+      auto part = [&]() {
+        const int64_t keys = start_of + kUnitTiles;
+        u.t0 = (int32_t)max((int64_t)0, x - keys);
+        u.t1 = (int32_t)min((int64_t)nt, a.hi - keys);
+        u.first = keys >= a.lo ? (int64_t)blockIdx.x : attn_div(keys, a.per);
+        u.last = keys + nt <= a.hi ? (int64_t)blockIdx.x : attn_div(keys + nt - 1, a.per);
+        u.r0 = mt * kRowsTile;
         u.rows = (int32_t)min((int64_t)kRowsTile, (int64_t)u.n * p.G - u.r0);
         const int32_t ilast = (int32_t)fast_div((uint32_t)(u.r0 + u.rows - 1), p.group.magic, p.group.shift);
         u.limit = max(0, min(u.kv, u.kv - u.n + ilast + 1));
-        fragment(p, s, u, t0, t1, &bad);
-        const int64_t start = x - t0;  // the unit's first tile
-        AttnCuts cut{start / a.per, (start + nt - 1) / a.per};
-        if (cut.whole()) {
-          join_warps(p, s, u, nullptr);
-        } else {
-          float* mine = slots + cut.slot(blockIdx.x) * SLOT;
-          join_warps(p, s, u, mine);
-          const int n = (int)(cut.last - cut.first + 1), f = (int)(blockIdx.x - cut.first);
-          const int groups = (n + kFanIn - 1) / kFanIn, gr = f / kFanIn;
-          const int64_t g0 = cut.first + (int64_t)gr * kFanIn;
-          const int size = min(kFanIn, n - gr * kFanIn);
-          auto slot = [&](int64_t block) { return slots + cut.slot(block) * SLOT; };
-          if (attn_completes<0, kRowsThreads>(&s.last, threadIdx.x == 0, counters + cut.slot(g0), size)) {
-            join_slots(p, s, u, size, [&](int i) { return slot(g0 + i); }, groups > 1 ? slot(g0) : nullptr);
-            if (groups > 1 && attn_completes<0, kRowsThreads>(&s.last, threadIdx.x == 0,
-                                                            counters + 2 * gridDim.x + cut.slot(cut.first), groups))
-              join_slots(p, s, u, groups, [&](int i) { return slot(cut.first + (int64_t)i * kFanIn); }, nullptr);
+        x = keys + nt;
+        return u.t1 > u.t0;
+      };
+      State st;
+      bool more = part();
+      if (more) start(p, s, u, st, &bad);
+      while (more) {
+        float m[2], l[2], o[D / 8][4];
+        body(p, s, u, st, m, l, o, &bad);
+        const Unit done = u;
+        more = x < end;
+        if (more) {
+          start_of = x;
+          if (++mt == nm) {
+            mt = 0;
+            if (++u.h == p.Hkv) {
+              u.h = 0;
+              do ++rq;
+              while (s.split.pre[rq + 1] <= x);
+              request_of();
+            }
           }
+          more = part();
+          if (more) start(p, s, u, st, &bad);
         }
-        __syncthreads();  // the shared partial outs have been read
-        x += t1 - t0;
+        finish(p, s, done, m, l, o);
       }
+      x = max(x, end);  // a last unit of which only the beginning's tiles were this block's
     }
     if (bad) atomicOr(p.err, kErrTable);
   }
@@ -416,14 +529,10 @@ struct RowsKernel {
 template <int DT, int D>
 __global__ void __launch_bounds__(kRowsThreads, RowsGeom<D>::PER_SM) attn_rows_kernel(const PagedAttnParams p) {
   extern __shared__ __align__(128) char smem[];
-  // After the tile kernel of the same call, which waits for everything before it and only then lets this
-  // launch start, nothing has to be waited for: the two write different rows. This grid then must not be
-  // over before that one, so the wait comes last.
-  pdl_trigger();
-  if (!p.beside) pdl_wait();
+  pdl_wait();
+  pdl_trigger();  // after the wait: the tile kernel of the same call, which may start now, need not wait
   using K = RowsKernel<DT, D>;
   K::run(p, *reinterpret_cast<typename K::Smem*>(smem));
-  if (p.beside) pdl_wait();
 }
 
 template <int DT, int D>

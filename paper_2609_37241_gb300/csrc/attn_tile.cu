@@ -701,9 +701,6 @@ struct Tile {
   }
 
   // ------------------------------------------------------------ the block
-  static __device__ __forceinline__ int64_t div64(int64_t a, int64_t b) {
-    return ((uint64_t)a | (uint64_t)b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
-  }
   // The place of tile x is looked for once, by a warp: its lanes try 32 row tiles at a time. The units after
   // it follow one another.
   static __device__ __forceinline__ void list(const PagedAttnParams& p, Smem& s, int64_t b0, int64_t x, int64_t run,
@@ -716,8 +713,8 @@ struct Tile {
     int32_t nm = Cost::row_tiles(p, r), h, k = 0;
     int64_t start = s.split.pre[rq];  // the unit's first tile
     {
-      const int64_t head = div64(s.split.pre[rq + 1] - start, p.Hkv);
-      h = (int32_t)div64(x - start, head);
+      const int64_t head = attn_div(s.split.pre[rq + 1] - start, p.Hkv);
+      h = (int32_t)attn_div(x - start, head);
       start += h * head;
       int64_t at = 0;
       int32_t step = 1;
@@ -749,8 +746,8 @@ struct Tile {
       const int32_t nt = Cost::key_tiles(f.limit);
       f.t0 = a.whole ? 0 : (int32_t)(x - start);
       f.t1 = a.whole ? nt : (int32_t)min((int64_t)nt, f.t0 + (a.hi - x));
-      f.first = start >= a.lo ? (int64_t)blockIdx.x : div64(start, a.per);
-      f.last = a.whole || start + nt <= a.hi ? (int64_t)blockIdx.x : div64(start + nt - 1, a.per);
+      f.first = start >= a.lo ? (int64_t)blockIdx.x : attn_div(start, a.per);
+      f.last = a.whole || start + nt <= a.hi ? (int64_t)blockIdx.x : attn_div(start + nt - 1, a.per);
       x += a.whole ? 1 : f.t1 - f.t0;
       if (x >= end || count == kFrags) break;
       start = x;  // the unit ended inside the run: the next one
@@ -814,8 +811,11 @@ struct Tile {
       __syncwarp();
       tc_before();
     }
-    pdl_wait();
-    pdl_trigger();  // after the wait: a launch that starts early then finds everything before this one done
+    // After the kernel of few rows of the same call, which has waited for everything before it when it lets
+    // this launch start, nothing has to be waited for: the two write different rows. This grid then must not be
+    // over before that one, so the wait comes last.
+    if (!p.beside) pdl_wait();
+    pdl_trigger();
     __syncthreads();
     tc_after();
     const uint32_t tmem = s.tmem;
@@ -858,6 +858,7 @@ struct Tile {
     tc_before();
     __syncthreads();
     tc_after();
+    if (p.beside) pdl_wait();
     if (threadIdx.x == 0 && s.abort) atomicOr(p.err, kErrTimeout);
     if (warp == MMA_WARP)
       asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");

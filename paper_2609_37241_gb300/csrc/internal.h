@@ -222,7 +222,7 @@ struct PagedAttnParams {
   int64_t rows_above, rows_upto;  // this launch takes the requests of rows_above < n * G <= rows_upto
   int64_t min_tiles;              // a block's run of key tiles is at least this long
   int64_t join_tiles;             // what a cut unit costs, in tiles' time (0: units are always cut to even runs)
-  int32_t beside;                 // rows kernel: launched after the tile kernel of the same call
+  int32_t beside;                 // tile kernel: launched after the kernel of few rows of the same call
   int32_t tokens;                 // tile kernel: tokens of a row tile
   uint32_t polls, first_polls;    // tile kernel: bounds of its waits, of a warp's first for scores
 };
@@ -365,11 +365,14 @@ bool attn_tile_entry(int32_t dtype, int32_t D, AttnEntry* e);
 // or both, each for its requests (of at most, of more than kTileRows rows; row: token and head of a group).
 constexpr int64_t kTileRows = 128;
 constexpr int64_t kTileJoin = 8;  // tile kernel: a cut unit's cost in tiles (12 us of 1.45 us tiles)
-constexpr int64_t kRowsRun = 4, kTileRun = 4;  // key tiles of a block's run at least
+constexpr int64_t kRowsRun = 2, kTileRun = 4;  // key tiles of a block's run at least
 struct AttnPlan {
   bool rows, tile;
 };
 AttnPlan attn_plan(const AttnEntry& tile, int64_t T, int64_t B, int64_t G, int64_t ps);
+constexpr int kFanIn = 16, kJoinGroups = 20;  // slots joined in one round; groups of them at most
+constexpr int32_t kMaxAttnBlocks = kFanIn * kJoinGroups;
+int32_t attn_blocks(const AttnEntry& e, int32_t sms);
 int64_t attn_work_floats(const AttnEntry& e, int32_t sms);
 bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, KernelEntry* out, const char** why);
 const void* empty_kernel_entry();  // the latency-floor probe's kernel (does nothing)

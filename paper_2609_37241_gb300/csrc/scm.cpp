@@ -1058,39 +1058,36 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
   p.polls = kBulkWaitPolls;
   p.first_polls = (scm->opt.flags & TRIDENT_OPT_TEST_WAIT_TIMEOUT) ? 0u : kBulkWaitPolls;
   const AttnPlan pl = attn_plan(tile, s.T, p.B, p.G, p.page.d);
-  if (pl.tile) {
-    CUtensorMap mk, mv;
-    if (!tile_map(&mk, a->t[1], v.d.dtype, tile.keys) || !tile_map(&mv, a->t[2], v.d.dtype, tile.keys))
-      return fail(TRIDENT_ERR_CUDA, "cuTensorMapEncodeTiled failed");
-    PagedAttnParams q = p;
-    q.work += rows_work;
-    q.rows_above = pl.rows ? kTileRows : 0;
-    q.rows_upto = INT64_MAX;
-    q.min_tiles = kTileRun;
-    q.join_tiles = kTileJoin;
-    q.tokens = tile.rows / p.G;
-    void* tp[3] = {&q, &mk, &mv};
-    cfg.blockDimX = (unsigned)tile.threads;
-    cfg.gridDimX = (unsigned)(scm->sm_count * tile.per_sm);
-    cfg.sharedMemBytes = (unsigned)tile.smem;
-    const int32_t st = launch_on(scm, &cfg, v.attn_tile_fn, tp);
-    if (st != TRIDENT_OK) return st;
-  }
-  if (!pl.rows) return TRIDENT_OK;
-  p.rows_above = 0;
-  p.rows_upto = pl.tile ? kTileRows : INT64_MAX;
-  p.min_tiles = kRowsRun;
-  p.join_tiles = 0;
-  p.beside = pl.tile ? 1 : 0;
-  if (pl.tile) {  // starts beside the tile kernel (see the kernel)
+  if (pl.rows) {
+    p.rows_above = 0;
+    p.rows_upto = pl.tile ? kTileRows : INT64_MAX;
+    p.min_tiles = kRowsRun;
+    p.join_tiles = 0;
+    cfg.blockDimX = (unsigned)rows.threads;
+    cfg.gridDimX = (unsigned)attn_blocks(rows, scm->sm_count);
+    cfg.sharedMemBytes = (unsigned)rows.smem;
+    const int32_t st = launch_on(scm, &cfg, v.fn, kp);
+    if (st != TRIDENT_OK || !pl.tile) return st;
+    // the tile kernel starts beside it (see there)
     attr.id = CU_LAUNCH_ATTRIBUTE_PROGRAMMATIC_STREAM_SERIALIZATION;
     attr.value.programmaticStreamSerializationAllowed = 1;
     cfg.numAttrs = 1;
   }
-  cfg.blockDimX = (unsigned)rows.threads;
-  cfg.gridDimX = (unsigned)(scm->sm_count * rows.per_sm);
-  cfg.sharedMemBytes = (unsigned)rows.smem;
-  return launch_on(scm, &cfg, v.fn, kp);
+  CUtensorMap mk, mv;
+  if (!tile_map(&mk, a->t[1], v.d.dtype, tile.keys) || !tile_map(&mv, a->t[2], v.d.dtype, tile.keys))
+    return fail(TRIDENT_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+  p.work += rows_work;
+  p.rows_above = pl.rows ? kTileRows : 0;
+  p.rows_upto = INT64_MAX;
+  p.min_tiles = kTileRun;
+  p.join_tiles = kTileJoin;
+  p.tokens = tile.rows / p.G;
+  p.beside = pl.rows ? 1 : 0;
+  void* tp[3] = {&p, &mk, &mv};
+  cfg.blockDimX = (unsigned)tile.threads;
+  cfg.gridDimX = (unsigned)attn_blocks(tile, scm->sm_count);
+  cfg.sharedMemBytes = (unsigned)tile.smem;
+  return launch_on(scm, &cfg, v.attn_tile_fn, tp);
 }
 
 int32_t do_launch(trident_scm* scm, const Version& v, const trident_args* a, const Sig& s,
