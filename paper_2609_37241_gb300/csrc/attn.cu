@@ -80,14 +80,26 @@ __global__ void __launch_bounds__(kThreads) attn_generic_kernel(const PagedAttnP
 
 }  // namespace
 
-// The lengths are on the device, so the choice goes by what T and B leave possible. Pages that do not
-// divide a tile's keys (or are no multiple of them), or hold fewer than the eight rows of a swizzle atom,
-// and groups of more than a tile's rows stay with the kernel of few rows. Where T - B extra rows cannot
-// make a request of more than kTileRows (every request with a row at least), so does the call.
-AttnPlan attn_plan(const AttnEntry& tile, int64_t T, int64_t B, int64_t G, int64_t ps) {
+// The kernel of few rows takes 16 of them (tokens x heads of a group) to a unit and reads the keys again for
+// every further 16; the tile kernel reads them once, but its units cost more to begin and to end. Measured,
+// few rows / tile kernel: 32 requests of 32 rows over 8000 keys of D 128 314 / 203 us, of 20 rows over 1000
+// keys 52.7 / 54.5; 16 of 128 rows over 2000 123 / 41; 4 of 24 over 500 15.7 / 18.0; 48 of 7 to 35 rows over
+// 400 to 3000 of D 64 36.5 / 49.5, of 35 rows over 3000 79 / 65; 8 of 32 over 4000 of D 256 100 / 57. So the
+// bound is by elements read again: kReread.
+constexpr int64_t kReread = 6000 * 128;
+
+// The lengths are on the device, so the choice goes by what T, B and the table's width (keys) leave
+// possible: both kernels, unless no request can pass the bound, or there is one request only. Pages that do
+// not divide a tile's keys (or are no multiple of them), or hold fewer than the eight rows of a swizzle
+// atom, and groups of more than 128 heads stay with the kernel of few rows.
+AttnPlan attn_plan(const AttnEntry& tile, int64_t T, int64_t B, int64_t G, int64_t D, int64_t ps, int64_t keys) {
   const bool fits = tile.fn && G <= 128 && ps % 8 == 0 && (tile.keys % ps == 0 || ps % tile.keys == 0);
-  if (!fits || T * G <= kTileRows || (T - B + 1) * G <= kTileRows) return {true, false};
-  return {B > 1, true};
+  const int64_t most = T > B ? T - B + 1 : 1;  // rows of a request, if every one has some
+  AttnPlan pl;
+  pl.reread = (kReread + D - 1) / D;
+  pl.tile = fits && ((most * G + 15) / 16 - 1) * keys >= pl.reread;
+  pl.rows = !pl.tile || B > 1;
+  return pl;
 }
 
 // per_sm blocks on every SM; at most kMaxAttnBlocks, whose parts two rounds of kFanIn join.

@@ -80,10 +80,12 @@ __device__ __forceinline__ void attn_fill_tail(const PagedAttnParams& p) {
   }
 }
 
-// Does this launch take the request? Rows outside (above, upto] are the other kernel's.
-__device__ __forceinline__ bool attn_takes(const PagedAttnParams& p, int32_t n) {
-  const int64_t rows = (int64_t)n * p.G;
-  return n > 0 && rows > p.rows_above && rows <= p.rows_upto;
+// Does this launch take the request? Where both kernels run, by the keys that the kernel of few rows would
+// read again for row tiles after the first: the tile kernel's from p.reread of them on.
+__device__ __forceinline__ bool attn_takes(const PagedAttnParams& p, const Request& r) {
+  if (p.part == ATTN_ALL) return r.n > 0;
+  const int64_t again = (((int64_t)r.n * p.G + 15) / 16 - 1) * r.kv;
+  return r.n > 0 && (again >= p.reread) == (p.part == ATTN_MANY);
 }
 
 // One block's share of the call: tiles per block and this block's run [lo, hi). whole: a unit per block
@@ -115,7 +117,7 @@ struct AttnSplit {
     Request r{0, 0, 0};
     for (int64_t b = threadIdx.x; b < p.B; b += NT) {
       r = attn_request(p, b, &ok);
-      if (!attn_takes(p, r.n)) continue;
+      if (!attn_takes(p, r)) continue;
       sum += Cost::of(p, r);
       if (p.join_tiles > 0) {
         units += Cost::units(p, r);
@@ -166,7 +168,7 @@ struct AttnSplit {
     bool ok = true;
     Request r{0, 0, 0};
     if (b < p.B) r = attn_request(p, b, &ok);
-    return scan(s, r, !attn_takes(p, r.n) ? 0 : a.whole ? Cost::units(p, r) : Cost::of(p, r), run);
+    return scan(s, r, !attn_takes(p, r) ? 0 : a.whole ? Cost::units(p, r) : Cost::of(p, r), run);
   }
   static __device__ __forceinline__ int64_t scan(Smem& s, const Request& r, long long own, int64_t run) {
     long long v = own;

@@ -304,24 +304,25 @@ struct RowsKernel {
       if (i != own) m = fmaxf(m, s.sm[i][row]);
     return m;
   }
-  // Adds the slots scaled to `base`, four loads in flight at a time.
+  // The slots in their order, scaled to `base`; in the place of slot `own` the part (a0, l0, m0), which is the
+  // same as if it had gone through its slot.
   template <class At>
   static __device__ __forceinline__ void add_slots(const Smem& s, float4& a, float& l, float base, int row, int d, int n,
-                                                   int own, At at) {
+                                                   At at, int own, const float4& a0, float l0, float m0) {
     for (int i0 = 0; i0 < n; i0 += 8) {
       float4 v[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < 8; ++e) {  // eight loads in flight
         const int i = min(i0 + e, n - 1);
-        v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+        v[e] = a0;
         if (i != own) v[e] = __ldcg(reinterpret_cast<const float4*>(at(i) + 2 * kRowsTile + row * D + d));
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int i = i0 + e;
-        if (i >= n || i == own) continue;
-        const float f = fast_exp2(s.sm[i][row] - base);
-        l = fmaf(f, s.sl[i][row], l);
+        if (i >= n) continue;
+        const float f = fast_exp2((i == own ? m0 : s.sm[i][row]) - base);
+        l = fmaf(f, i == own ? l0 : s.sl[i][row], l);
         a.x = fmaf(f, v[e].x, a.x); a.y = fmaf(f, v[e].y, a.y); a.z = fmaf(f, v[e].z, a.z); a.w = fmaf(f, v[e].w, a.w);
       }
     }
@@ -353,7 +354,7 @@ struct RowsKernel {
       __syncthreads();
       const int at_row = threadIdx.x / (D / 4), row = p0 + at_row, d = threadIdx.x % (D / 4) * 4;
       if (row < u.rows) {
-        float mm = slot_max(s, row, n, own), ll = 0.f;
+        float mm = -INFINITY, ll = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) mm = fmaxf(mm, s.m[i][row]);
         const float base = mm == -INFINITY ? 0.f : mm;
@@ -365,7 +366,14 @@ struct RowsKernel {
           ll = fmaf(f, s.l[i][row], ll);
           a.x = fmaf(f, v.x, a.x); a.y = fmaf(f, v.y, a.y); a.z = fmaf(f, v.z, a.z); a.w = fmaf(f, v.w, a.w);
         }
-        add_slots(s, a, ll, base, row, d, n, own, at);
+        if (n > 0) {
+          const float4 a0 = a;
+          const float l0 = ll, m0 = mm;
+          mm = fmaxf(mm, slot_max(s, row, n, own));
+          a = make_float4(0.f, 0.f, 0.f, 0.f);
+          ll = 0.f;
+          add_slots(s, a, ll, mm == -INFINITY ? 0.f : mm, row, d, n, at, own, a0, l0, m0);
+        }
         if (slot) {
           *reinterpret_cast<float4*>(slot + 2 * kRowsTile + row * D + d) = a;
           if (d == 0) {
@@ -405,7 +413,7 @@ struct RowsKernel {
       const float m = slot_max(s, row, n, -1);
       float l = 0.f;
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-      add_slots(s, a, l, m == -INFINITY ? 0.f : m, row, d, n, -1, at);
+      add_slots(s, a, l, m == -INFINITY ? 0.f : m, row, d, n, at, -1, a, 0.f, 0.f);
       if (dst) {  // its m and l have been read by all, and its elements d .. d + 3 by this thread alone
         *reinterpret_cast<float4*>(dst + 2 * kRowsTile + row * D + d) = a;
         if (d == 0) {

@@ -205,6 +205,7 @@ struct RopePagedParams {
 };
 
 // Attention of each request's last rows over its pages.
+enum AttnPart : int32_t { ATTN_ALL, ATTN_FEW, ATTN_MANY };
 struct PagedAttnParams {
   const void* q;
   PagedCache kc, vc;  // read only
@@ -219,7 +220,8 @@ struct PagedAttnParams {
   int32_t Hq, Hkv, G, D;
   float scale;
   FastDiv page, group;  // by ps; by G = Hq / Hkv
-  int64_t rows_above, rows_upto;  // this launch takes the requests of rows_above < n * G <= rows_upto
+  int32_t part;                   // AttnPart: which requests this launch takes
+  int64_t reread;                 // ... the bound between them (attn_takes)
   int64_t min_tiles;              // a block's run of key tiles is at least this long
   int64_t join_tiles;             // what a cut unit costs, in tiles' time (0: units are always cut to even runs)
   int32_t beside;                 // tile kernel: launched after the kernel of few rows of the same call
@@ -361,15 +363,15 @@ bool rope_paged_kernel(int32_t dtype, int32_t variant, int32_t D, int32_t R, boo
 int rope_paged_plan(RopePagedParams* p, int32_t* threads, int64_t* blocks, int32_t sms);
 bool attn_rows_entry(int32_t dtype, int32_t D, AttnEntry* e);
 bool attn_tile_entry(int32_t dtype, int32_t D, AttnEntry* e);
-// Which attention kernels a call of T rows and B requests takes: the one of few rows, the tile kernel,
-// or both, each for its requests (of at most, of more than kTileRows rows; row: token and head of a group).
-constexpr int64_t kTileRows = 128;
+// Which attention kernels a call of T rows and B requests takes: the one of few rows, the tile kernel, or
+// both, each for its requests (attn_takes).
 constexpr int64_t kTileJoin = 8;  // tile kernel: a cut unit's cost in tiles (12 us of 1.45 us tiles)
 constexpr int64_t kRowsRun = 2, kTileRun = 4;  // key tiles of a block's run at least
 struct AttnPlan {
   bool rows, tile;
+  int64_t reread;
 };
-AttnPlan attn_plan(const AttnEntry& tile, int64_t T, int64_t B, int64_t G, int64_t ps);
+AttnPlan attn_plan(const AttnEntry& tile, int64_t T, int64_t B, int64_t G, int64_t D, int64_t ps, int64_t keys);
 constexpr int kFanIn = 16, kJoinGroups = 20;  // slots joined in one round; groups of them at most
 constexpr int32_t kMaxAttnBlocks = kFanIn * kJoinGroups;
 int32_t attn_blocks(const AttnEntry& e, int32_t sms);

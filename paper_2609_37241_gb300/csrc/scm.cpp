@@ -1057,10 +1057,10 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
     return fail(TRIDENT_ERR_INVALID, "the workspace is smaller than trident_scm_workspace says");
   p.polls = kBulkWaitPolls;
   p.first_polls = (scm->opt.flags & TRIDENT_OPT_TEST_WAIT_TIMEOUT) ? 0u : kBulkWaitPolls;
-  const AttnPlan pl = attn_plan(tile, s.T, p.B, p.G, p.page.d);
+  const AttnPlan pl = attn_plan(tile, s.T, p.B, p.G, p.D, p.page.d, p.M * p.page.d);
+  p.reread = pl.reread;
   if (pl.rows) {
-    p.rows_above = 0;
-    p.rows_upto = pl.tile ? kTileRows : INT64_MAX;
+    p.part = pl.tile ? ATTN_FEW : ATTN_ALL;
     p.min_tiles = kRowsRun;
     p.join_tiles = 0;
     cfg.blockDimX = (unsigned)rows.threads;
@@ -1077,8 +1077,7 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
   if (!tile_map(&mk, a->t[1], v.d.dtype, tile.keys) || !tile_map(&mv, a->t[2], v.d.dtype, tile.keys))
     return fail(TRIDENT_ERR_CUDA, "cuTensorMapEncodeTiled failed");
   p.work += rows_work;
-  p.rows_above = pl.rows ? kTileRows : 0;
-  p.rows_upto = INT64_MAX;
+  p.part = pl.rows ? ATTN_MANY : ATTN_ALL;
   p.min_tiles = kTileRun;
   p.join_tiles = kTileJoin;
   p.tokens = tile.rows / p.G;
