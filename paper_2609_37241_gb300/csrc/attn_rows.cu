@@ -32,6 +32,10 @@ struct RowsGeom {
   static constexpr int PER_SM = D == 256 ? 1 : 2;
   static constexpr int PASS = 512 / D;          // rows that the warps join at a time: a float4 per thread
   static constexpr int LDO = D + 4;
+  // q in registers; for D 256, whose accumulators fill them, in shared memory, a buffer for the fragment under
+  // way and one for the next
+  static constexpr bool QS = D > 128;
+  static constexpr int QREG = QS ? 1 : D / 16, QBUF = QS ? 16 * D * 2 : 16;
 };
 
 template <int DT>
@@ -94,6 +98,7 @@ struct RowsKernel {
   static constexpr int kSlots = kFanIn > kJoinGroups ? kFanIn : kJoinGroups;  // slots of a join at most
   struct Smem {
     alignas(128) char ring[G::RING];
+    alignas(128) char q[2][G::QBUF];
     alignas(16) float part[4][G::PASS][G::LDO];
     typename Split::Smem split;
     float m[4][16], l[4][16];
@@ -155,26 +160,41 @@ struct RowsKernel {
     int32_t first, groups;  // its 16-key groups: keys first + 64 x, x < groups
     int32_t page;           // entry() of the next group to copy
     int32_t see[2];         // keys that rows g and g + 8 see
-    uint32_t q[D / 16][4];
+    uint32_t q[G::QREG][4];
+    int32_t buf;            // QS: which buffer q is in
   };
 
   // Starts a fragment: q, and the copies of the first NS - 1 stages. The ring is the warp's own, so this comes
   // before the fragment before has been joined.
   static __device__ __forceinline__ void start(const PagedAttnParams& p, Smem& s, const Unit& u, State& st, bool* bad) {
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    auto q_row = [&](int row, int32_t* i) {
+      const int32_t r = u.r0 + min(row, u.rows - 1);
+      *i = (int32_t)fast_div((uint32_t)r, p.group.magic, p.group.shift);
+      return row_ptr(p.q, u.q0 + *i, p.q_rs, 2) + ((int64_t)u.h * p.G + (r - *i * p.G)) * D * 2;
+    };
     const char* src[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const int32_t r = u.r0 + min(g + 8 * k, u.rows - 1);
-      const int32_t i = (int32_t)fast_div((uint32_t)r, p.group.magic, p.group.shift);
+      int32_t i;
+      src[k] = q_row(g + 8 * k, &i);
       st.see[k] = u.kv - u.n + i + 1;
-      src[k] = row_ptr(p.q, u.q0 + i, p.q_rs, 2) + ((int64_t)u.h * p.G + (r - i * p.G)) * D * 2;
     }
+    if constexpr (G::QS) {  // read after the next block barrier
+      st.buf ^= 1;
 #pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk)
+      for (int e = 0; e < 16 * G::CH / kRowsThreads; ++e) {
+        const int at = threadIdx.x + e * kRowsThreads, row = at / G::CH, ch = at % G::CH;
+        int32_t i;
+        st16(s.q[st.buf] + row * (D * 2) + ((ch ^ (row & 7)) << 4), ld16(q_row(row, &i) + ch * 16));
+      }
+    } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        st.q[kk][e] = *reinterpret_cast<const uint32_t*>(src[e & 1] + (kk * 16 + (e >> 1) * 8 + 2 * t) * 2);
+      for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          st.q[kk][e] = *reinterpret_cast<const uint32_t*>(src[e & 1] + (kk * 16 + (e >> 1) * 8 + 2 * t) * 2);
+    }
     st.kb = reinterpret_cast<const char*>(p.kc.base) + (int64_t)u.h * p.kc.head * 2;
     st.vb = reinterpret_cast<const char*>(p.vc.base) + (int64_t)u.h * p.vc.head * 2;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s.ring) + w * (G::NS * G::STAGE);
@@ -205,6 +225,7 @@ struct RowsKernel {
     m[0] = m[1] = -INFINITY;
     l[0] = l[1] = 0.f;
     const int mi = lane >> 3, mr = lane & 7;
+    const uint32_t q_at = (uint32_t)__cvta_generic_to_shared(s.q[st.buf & 1]);
     for (int x = 0; x < st.groups; ++x) {
       cp_wait<G::NS - 2>();
       __syncwarp();  // all lanes' copies have landed, and the stage refilled below has been read
@@ -224,8 +245,16 @@ struct RowsKernel {
         uint32_t kf[4];
         const int key = (mi >> 1) * 8 + mr, ch = kk * 2 + (mi & 1);
         ldsm4(kf, at + key * (D * 2) + ((ch ^ (key & 7)) << 4));
-        mma16816<DT>(kk & 1 ? odd[0] : sc[0], st.q[kk], kf[0], kf[1]);
-        mma16816<DT>(kk & 1 ? odd[1] : sc[1], st.q[kk], kf[2], kf[3]);
+        uint32_t qf[4];
+        if constexpr (G::QS) {
+          const int row = (mi & 1) * 8 + mr, qch = kk * 2 + (mi >> 1);
+          ldsm4(qf, q_at + row * (D * 2) + ((qch ^ (row & 7)) << 4));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) qf[e] = st.q[kk][e];
+        }
+        mma16816<DT>(kk & 1 ? odd[0] : sc[0], qf, kf[0], kf[1]);
+        mma16816<DT>(kk & 1 ? odd[1] : sc[1], qf, kf[2], kf[3]);
       }
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt)
@@ -505,8 +534,10 @@ struct RowsKernel {
         return u.t1 > u.t0;
       };
       State st;
+      st.buf = 0;
       bool more = part();
       if (more) start(p, s, u, st, &bad);
+      if (G::QS) __syncthreads();
       while (more) {
         float m[2], l[2], o[D / 8][4];
         body(p, s, u, st, m, l, o, &bad);
