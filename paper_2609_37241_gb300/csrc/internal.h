@@ -264,7 +264,8 @@ struct KernelEntry {
   const void* fn_step = nullptr;          // chain only: several calls per launch (ChainStepParams)
   const void* fn_step_inplace = nullptr;  // ... one block per token for the norms
   const void* fn_large = nullptr;  // RoPE: the bulk-copy entry (rope_plan chooses)
-  const void* any_fn[2] = {};      // RoPE versions of the generic kind: rope_any_kernel (or NULL)
+  const void* any_fn[4] = {};      // RoPE versions of the generic kind: rope_any_kernel (two, or NULL); paged
+                                   // RoPE: rope_paged_kernel by rows per lane group
   const void* fn_mid = nullptr;    // RoPE: two head-rows per lane group
   const void* fn_blocks = nullptr;  // RoPE, D 64: fn for blocks of 128 or 256 threads
   const void* pw_fn[kPwEntries] = {};  // elementwise, by PointwiseEntry
@@ -298,7 +299,7 @@ enum KernelKind : int32_t {
 };
 
 constexpr int kMapThreads = 256;  // PAGE_MAP: block size
-constexpr int kMapTokens = 1024;  // ... and tokens per block
+constexpr int kMapTokens = 256;  // ... and tokens per block
 constexpr int64_t kPosLimit = 1 << 24;  // paged RoPE: positions are exact in fp32
 
 // Lookup of compiled kernels. Return false (with a reason) if no kernel fits.

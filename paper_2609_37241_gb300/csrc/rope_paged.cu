@@ -244,29 +244,36 @@ __global__ void __launch_bounds__(kThreads) rope_paged_generic_kernel(const Rope
   }
 }
 
+template <int DT, int LPG, bool QK, bool INTER>
+void pick_rows(KernelEntry* out) {
+  out->any_fn[0] = (const void*)rope_paged_kernel<DT, LPG, QK, INTER, 1>;
+  out->any_fn[1] = (const void*)rope_paged_kernel<DT, LPG, QK, INTER, 2>;
+  out->any_fn[2] = (const void*)rope_paged_kernel<DT, LPG, QK, INTER, 3>;
+  out->any_fn[3] = (const void*)rope_paged_kernel<DT, LPG, QK, INTER, 4>;
+}
+
 template <int DT, bool QK, bool INTER>
 void pick(int32_t variant, int32_t D, KernelEntry* out) {
-  if (variant == 1) {
-    out->fn = (const void*)rope_paged_generic_kernel<DT, QK, INTER>;
-  } else if (D <= 64) {
-    out->any_fn[0] = (const void*)rope_paged_kernel<DT, 4, QK, INTER, 1>;
-    out->any_fn[1] = (const void*)rope_paged_kernel<DT, 4, QK, INTER, 3>;
-  } else if (D <= 128) {
-    out->any_fn[0] = (const void*)rope_paged_kernel<DT, 8, QK, INTER, 1>;
-    out->any_fn[1] = (const void*)rope_paged_kernel<DT, 8, QK, INTER, 3>;
-  } else {
-    out->any_fn[0] = (const void*)rope_paged_kernel<DT, 16, QK, INTER, 1>;
-    out->any_fn[1] = (const void*)rope_paged_kernel<DT, 16, QK, INTER, 3>;
-  }
+  if (variant == 1) out->fn = (const void*)rope_paged_generic_kernel<DT, QK, INTER>;
+  else if (D <= 64) pick_rows<DT, 4, QK, INTER>(out);
+  else if (D <= 128) pick_rows<DT, 8, QK, INTER>(out);
+  else pick_rows<DT, 16, QK, INTER>(out);
 }
 
 }  // namespace
 
+// Rows per lane group at most: one up to three items (of one row each) per SM, three beyond, four from
+// kRopePagedMany such items of three per SM on; the kernel is that of the rows that the item split leaves to
+// a group. Measured, one / two / three / four rows at most: 200 tokens of 32 + 8 + 8 heads of 128 with q/k
+// norm 3.56 / 3.49 / 3.82 / 3.93 us, 1000 tokens 8.20 / 6.40 / 6.33 / 7.26, 3333 (half of the head) 22.1 / 17.8
+// / 16.4 / 16.3, 8192 without the norm 50.2 / 32.7 / 32.9 / 31.3 (0.95 of the 6.79 TB/s copy rate).
+constexpr int64_t kRopePagedMany = 120;
 int rope_paged_plan(RopePagedParams* p, int32_t* threads, int64_t* blocks, int32_t sms) {
-  const int lanes = p->D <= 64 ? 4 : p->D <= 128 ? 8 : 16;
-  RopeSplit r = rope_split(p->NH, 32 / lanes, 1);
-  const int e = p->T * r.ipt > 3 * (int64_t)sms ? 1 : 0;
-  if (e) r = rope_split(p->NH, 32 / lanes, 3);
+  const int lanes = p->D <= 64 ? 4 : p->D <= 128 ? 8 : 16, groups = 32 / lanes;
+  RopeSplit r = rope_split(p->NH, groups, 1);
+  if (p->T * r.ipt > 3 * (int64_t)sms) r = rope_split(p->NH, groups, 3);
+  if (r.rpi > groups && p->T * r.ipt > kRopePagedMany * sms) r = rope_split(p->NH, groups, 4);
+  const int e = r.rpi / groups - 1;
   p->ipt = r.ipt;
   p->rpi = r.rpi;
   p->ipt_magic = r.magic;

@@ -572,7 +572,7 @@ struct Version {
   RopePlans rope_plans;         // vector RoPE: item splits of its entries
   RopeSplit rope_split[2];      // layer chain: item splits with one and kChainRopeRows rows
   CUfunction pw_fn[kPwEntries];  // elementwise: entries by layout and size (pointwise_plan)
-  CUfunction any_fn[2];            // RoPE versions of the generic kind: rope_any_kernel
+  CUfunction any_fn[4];            // RoPE versions of the generic kind: rope_any_kernel; rope_paged_kernel
   CUfunction attn_tile_fn;       // paged attention: the kernel of many rows
   CUfunction nm_fn[kNormEntries];  // norms: entries by layout and size (norm_plan)
   CUfunction step_fn;           // layer chain: several calls per launch (two blocks per token)
@@ -1665,7 +1665,7 @@ int32_t append_version(trident_scm_t* scm, const trident_spec_desc* desc, int32_
       for (int k = 0; k < kPwEntries; ++k)
         if (!resolve(v.ke.pw_fn[k], &v.pw_fn[k]))
           return fail(TRIDENT_ERR_CUDA, "cannot resolve the elementwise kernel entries");
-      for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < 4; ++k)
         if (!resolve(v.ke.any_fn[k], &v.any_fn[k]))
           return fail(TRIDENT_ERR_CUDA, "cannot resolve the RoPE kernel entries");
       for (int k = 0; k < kNormEntries; ++k)
