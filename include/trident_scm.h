@@ -165,8 +165,9 @@ typedef enum trident_dtype {
  *   from cu_q[B] on. Cache rows from kv_len on are never used (they may hold NaN); keys below kv_len
  *   have to be finite. Sums and the softmax's statistics are fp32; its numerators are rounded to act
  *   for the product with v.
- *   work: zeros before its first use, left ready for the next call; calls that may overlap on the
- *   GPU need a workspace each. cu_q that is not ascending from 0 within [0,T], a kv_len outside
+ *   work: zeros before its first use, left ready for the next call (after TRIDENT_DEVERR_TIMEOUT it
+ *   has to be zeroed again); calls that may overlap on the GPU need a workspace each. The result does
+ *   not depend on the order in which blocks finish. cu_q that is not ascending from 0 within [0,T], a kv_len outside
  *   [0, M * ps] or a page number outside [0,P) (read as page 0) sets TRIDENT_DEVERR_TABLE; the
  *   outputs of such a request are unspecified.
  */

@@ -255,6 +255,114 @@ def test_paged_attention(S, new, kv, Hq, Hkv, D, ps, order, tail, strided, dtype
     s.close()
 
 
+TILE_SHAPES = [  # enough rows and keys for the tile kernel; as above
+    ([128], [900], 8, 1, 256, 16, "head", 0, False),             # heads of 256
+    ([70, 90, 1], [1100, 800, 300], 16, 4, 256, 64, "token", 3, True),
+    ([120, 200], [1600, 1024], 7, 1, 64, 256, "pair", 0, False),  # seven heads per group, pages longer than a tile
+    ([500, 3, 64], [500, 2000, 3000], 8, 2, 128, 8, "padded", 1, False),
+    ([400, 1, 1, 0, 90], [390, 600, 31, 0, 2111], 12, 2, 128, 32, "head", 0, False),  # ten rows before the first key
+    ([129], [9000], 4, 1, 128, 16, "head", 0, False),            # one unit over all blocks: joined in groups
+    ([40] * 20, [2000 + 13 * k for k in range(20)], 8, 1, 128, 16, "head", 0, False),
+    ([1000], [1001], 64, 2, 64, 128, "head", 7, False),          # more units than blocks
+]
+
+
+@pytest.mark.parametrize("new,kv,Hq,Hkv,D,ps,order,tail,strided", TILE_SHAPES)
+@pytest.mark.parametrize("dtype", ["BF16", "FP16"])
+def test_paged_attention_many_rows(S, new, kv, Hq, Hkv, D, ps, order, tail, strided, dtype):
+    test_paged_attention(S, new, kv, Hq, Hkv, D, ps, order, tail, strided, dtype, "AUTO")
+
+
+def test_paged_attention_many_requests(S):
+    """More requests than a block has threads, in both kernels."""
+    g = np.random.default_rng(12)
+    new, kv = [1] * 300, [int(x) for x in g.integers(0, 200, 300)]
+    test_paged_attention(S, new, kv, 4, 1, 64, 16, "head", 0, False, "BF16", "AUTO")
+    new = [30 if k % 3 else 1 for k in range(420)]
+    test_paged_attention(S, new, [460 + k % 7 for k in range(420)], 8, 1, 128, 16, "head", 0, False, "FP16", "AUTO")
+
+
+def test_paged_attention_without_requests_or_pages(S):
+    Hq, Hkv, D, ps = 8, 2, 128, 16
+    s, index, work = attn_scm(S, S.BF16, Hq, Hkv, D, ps, S.VARIANT_AUTO)
+    g = np.random.default_rng(0)
+    kc, vc = R.pool(g, 2, Hkv, ps, D, S.BF16, "head")
+    q = torch.randn(400, Hq, D, device="cuda").bfloat16()
+    for B, M in ((0, 4), (3, 0)):
+        out, lse = torch.full_like(q, float("nan")), torch.zeros(400, Hq, device="cuda")
+        cu = i32([0] * (B + 1) if B == 0 else [0, 100, 300, 400])
+        args = S.make_args(S.OP_PAGED_ATTN, [q, kc, vc, torch.zeros(B, M, dtype=torch.int32, device="cuda"), cu,
+                                             torch.zeros(B, dtype=torch.int32, device="cuda"), work, out, lse], scalar=1.0)
+        assert s.invoke(args, stream()) == (S.OK, index), S.trident_scm_last_error()
+        assert S.trident_scm_device_status(s.h, stream())[1] == 0
+        assert (out == 0).all() and (lse == -float("inf")).all()
+    s.close()
+
+
+def test_paged_attention_workspace_is_checked(S):
+    s, index, work = attn_scm(S, S.BF16, 8, 2, 128, 16, S.VARIANT_AUTO)
+    b = R.batch(np.random.default_rng(0), [1], [40], 8, 2, 128, 16, S.BF16)
+    ts = [b["q"], b["kc"], b["vc"], b["table"], b["cu"], b["kv"], work[:-1], b["out"], b["lse"]]
+    assert s.invoke(S.make_args(S.OP_PAGED_ATTN, ts, scalar=1.0), stream())[0] == S.ERR_INVALID
+    s.close()
+
+
+def test_paged_attention_both_kernels_in_a_graph_and_on_two_streams(S):
+    """A call that launches both kernels, captured and replayed; and two calls at once with a workspace each."""
+    Hq, Hkv, D, ps = 16, 4, 128, 16
+    s, index, work = attn_scm(S, S.BF16, Hq, Hkv, D, ps, S.VARIANT_AUTO)
+    b = [R.batch(np.random.default_rng(k), [1, 300, 1, 4], [700, 900, 33, 1200], Hq, Hkv, D, ps, S.BF16) for k in range(2)]
+    works = [work, torch.zeros_like(work)]
+    refs = [R.attention(x["q"].cpu(), x["kc"].cpu(), x["vc"].cpu(), x["table"].cpu(), x["cu"].tolist(), x["kv"].tolist(), ps,
+                        0.09) for x in b]
+    args = [S.make_args(S.OP_PAGED_ATTN, [x["q"], x["kc"], x["vc"], x["table"], x["cu"], x["kv"], w, x["out"], x["lse"]],
+                        scalar=0.09) for x, w in zip(b, works)]
+
+    def check():
+        torch.cuda.synchronize()
+        assert S.trident_scm_device_status(s.h, stream())[1] == 0
+        for x, (out, lse, wgt) in zip(b, refs):
+            assert ((x["out"].cpu().double() - out).abs() <= R.attn_tolerance(out, wgt, S.BF16, 1200, 5.0)).all()
+            x["out"].fill_(float("nan"))
+        torch.cuda.synchronize()
+
+    side = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for a, st in zip(args, side):
+            assert s.invoke(a, st.cuda_stream) == (S.OK, index)
+    check()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side[0]):
+        for _ in range(3):
+            for a in args:
+                assert s.invoke(a, torch.cuda.current_stream().cuda_stream) == (S.OK, index)
+    for _ in range(2):
+        graph.replay()
+        check()
+    s.close()
+
+
+def test_paged_attention_reports_a_wait_that_ran_out(S):
+    """The tile kernel's first wait for scores gives up at once: status bit, nothing written; with the workspace
+    zeroed again the next call is right."""
+    Hq, Hkv, D, ps = 8, 2, 128, 16
+    b = R.batch(np.random.default_rng(6), [300], [2000], Hq, Hkv, D, ps, S.BF16)
+    s = S.Scm(flags=S.OPT_TEST_WAIT_TIMEOUT)
+    index = s.register(S.make_spec(S.OP_PAGED_ATTN, S.BF16, [Hq, Hkv, D, ps], 1, 1 << 20))
+    work = torch.zeros(s.workspace(index), device="cuda")
+    args = S.make_args(S.OP_PAGED_ATTN, [b["q"], b["kc"], b["vc"], b["table"], b["cu"], b["kv"], work, b["out"], b["lse"]],
+                       scalar=0.1)
+    assert s.invoke(args, stream()) == (S.OK, index)
+    assert S.trident_scm_device_status(s.h, stream())[1] == S.DEVERR_TIMEOUT
+    assert torch.isnan(b["out"]).all() and torch.isnan(b["lse"]).all()
+    s.close()
+    s, index, _ = attn_scm(S, S.BF16, Hq, Hkv, D, ps, S.VARIANT_AUTO)
+    work.zero_()
+    check_attn(S, b, Hq, Hkv, D, ps, S.BF16, 0.1, 0, s, index, work)
+    s.close()
+
+
 @pytest.mark.parametrize("D", [8, 40, 96, 512])
 @pytest.mark.parametrize("dtype", ["BF16", "FP16"])
 def test_paged_attention_other_head_sizes(S, D, dtype):
