@@ -568,8 +568,7 @@ struct RowsKernel {
 template <int DT, int D>
 __global__ void __launch_bounds__(kRowsThreads, RowsGeom<D>::PER_SM) attn_rows_kernel(const PagedAttnParams p) {
   extern __shared__ __align__(128) char smem[];
-  pdl_wait();
-  pdl_trigger();  // after the wait: the tile kernel of the same call, which may start now, need not wait
+  pdl_prologue();
   using K = RowsKernel<DT, D>;
   K::run(p, *reinterpret_cast<typename K::Smem*>(smem));
 }

@@ -811,11 +811,7 @@ struct Tile {
       __syncwarp();
       tc_before();
     }
-    // After the kernel of few rows of the same call, which has waited for everything before it when it lets
-    // this launch start, nothing has to be waited for: the two write different rows. This grid then must not be
-    // over before that one, so the wait comes last.
-    if (!p.beside) pdl_wait();
-    pdl_trigger();
+    pdl_prologue();
     __syncthreads();
     tc_after();
     const uint32_t tmem = s.tmem;
@@ -858,7 +854,6 @@ struct Tile {
     tc_before();
     __syncthreads();
     tc_after();
-    if (p.beside) pdl_wait();
     if (threadIdx.x == 0 && s.abort) atomicOr(p.err, kErrTimeout);
     if (warp == MMA_WARP)
       asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");

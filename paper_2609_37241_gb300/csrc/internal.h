@@ -224,7 +224,6 @@ struct PagedAttnParams {
   int64_t reread;                 // ... the bound between them (attn_takes)
   int64_t min_tiles;              // a block's run of key tiles is at least this long
   int64_t join_tiles;             // what a cut unit costs, in tiles' time (0: units are always cut to even runs)
-  int32_t beside;                 // tile kernel: launched after the kernel of few rows of the same call
   int32_t tokens;                 // tile kernel: tokens of a row tile
   uint32_t polls, first_polls;    // tile kernel: bounds of its waits, of a warp's first for scores
 };

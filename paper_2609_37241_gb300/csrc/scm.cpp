@@ -1068,7 +1068,7 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
     cfg.sharedMemBytes = (unsigned)rows.smem;
     const int32_t st = launch_on(scm, &cfg, v.fn, kp);
     if (st != TRIDENT_OK || !pl.tile) return st;
-    // the tile kernel starts beside it (see there)
+    // the tile kernel's launch overlaps it; the kernel waits for it before its first access
     attr.id = CU_LAUNCH_ATTRIBUTE_PROGRAMMATIC_STREAM_SERIALIZATION;
     attr.value.programmaticStreamSerializationAllowed = 1;
     cfg.numAttrs = 1;
@@ -1081,7 +1081,6 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
   p.min_tiles = kTileRun;
   p.join_tiles = kTileJoin;
   p.tokens = tile.rows / p.G;
-  p.beside = pl.rows ? 1 : 0;
   void* tp[3] = {&p, &mk, &mv};
   cfg.blockDimX = (unsigned)tile.threads;
   cfg.gridDimX = (unsigned)attn_blocks(tile, scm->sm_count);

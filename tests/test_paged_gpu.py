@@ -494,3 +494,13 @@ def test_a_step_through_one_call_and_a_graph(S):
         ctx.copy_(kv)
         head.copy_(head_out)
     s.close()
+
+
+def test_the_serving_example_runs(S):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, os.path.join(root, "examples", "paged_serving.py"), "3"], capture_output=True, text=True,
+                       timeout=300)
+    assert r.returncode == 0 and r.stdout.count("device status 0") == 4, r.stdout + r.stderr
