@@ -95,6 +95,7 @@ __device__ __forceinline__ bool attn_takes(const PagedAttnParams& p, const Reque
 struct AttnShare {
   int64_t per, lo, hi, total;
   bool whole;
+  bool others;  // ATTN_FEW: some requests are the other kernel's
 };
 
 // Cost::of(p, r): the key tiles of all of request r's units, at least one per unit so that a unit
@@ -114,10 +115,14 @@ struct AttnSplit {
     bool ok = true;
     long long sum = 0, units = 0;
     int32_t longest = 0;
+    bool others = false;
     Request r{0, 0, 0};
     for (int64_t b = threadIdx.x; b < p.B; b += NT) {
       r = attn_request(p, b, &ok);
-      if (!attn_takes(p, r)) continue;
+      if (!attn_takes(p, r)) {
+        others |= r.n > 0;
+        continue;
+      }
       sum += Cost::of(p, r);
       if (p.join_tiles > 0) {
         units += Cost::units(p, r);
@@ -140,7 +145,7 @@ struct AttnSplit {
       s.units[threadIdx.x >> 5] = units;
       s.longest[threadIdx.x >> 5] = longest;
     }
-    __syncthreads();
+    const int any_others = p.part == ATTN_FEW ? __syncthreads_or(others) : (__syncthreads(), 0);
     sum = units = 0;
 #pragma unroll
     for (int w = 0; w < NT / 32; ++w) {
@@ -152,6 +157,7 @@ struct AttnSplit {
                                              : (int64_t)(((uint32_t)sum + gridDim.x - 1) / gridDim.x);
     AttnShare a;
     a.whole = p.join_tiles > 0 && units <= gridDim.x && longest <= even + p.join_tiles;
+    a.others = any_others != 0;
     a.total = a.whole ? units : sum;
     a.per = a.whole ? 1 : (even > p.min_tiles ? even : p.min_tiles);
     a.lo = min(a.total, (int64_t)blockIdx.x * a.per);
@@ -217,6 +223,37 @@ struct AttnCuts {
   __device__ __forceinline__ bool whole() const { return first == last; }
   __device__ __forceinline__ int64_t slot(int64_t block) const { return block == first ? 2 * block + 1 : 2 * block; }
 };
+
+// Where both kernels run, the one of few rows comes first and the tile kernel's blocks start as its blocks
+// leave the SMs, not when all of it is done: the two write different rows and use different parts of the
+// workspace, so the tile kernel only needs what came before both. The first one's block 0 has waited for
+// that (griddepcontrol.wait) and looked the requests over when it stores the word p.start (release), and no
+// block of the second starts before block 0 has let it (the trigger comes after the store); the second
+// acquires the word and goes on, with its later loads behind that -- its TMA loads by a proxy fence -- or, if
+// it should read 0, waits for the whole first kernel. The word is 0 again when the second ends, which is not
+// before the first has (it waits for it last).
+enum : uint32_t { ATTN_START_NONE = 1, ATTN_START_SOME = 2 };  // no request is left to the tile kernel, or some
+
+__device__ __forceinline__ void attn_lets_start(const PagedAttnParams& p, bool others) {
+  if (blockIdx.x == 0 && threadIdx.x == 0)
+    asm volatile("st.release.gpu.global.u32 [%0], %1;" :: "l"(p.start), "r"(others ? ATTN_START_SOME : ATTN_START_NONE) : "memory");
+  __syncthreads();
+  pdl_trigger();
+}
+__device__ __forceinline__ bool attn_starts(const PagedAttnParams& p) {
+  uint32_t word = 0;
+  if (threadIdx.x == 0) asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(word) : "l"(p.start) : "memory");
+  if (!__syncthreads_or(word != 0)) {
+    pdl_wait();
+    word = __ldcg(p.start);
+  }
+  asm volatile("fence.proxy.async.global;" ::: "memory");
+  return __syncthreads_or(word == ATTN_START_SOME) != 0;
+}
+__device__ __forceinline__ void attn_ends(const PagedAttnParams& p) {
+  pdl_wait();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.start = 0u;
+}
 
 // Counts a finished part; true in every thread of the NT that call it (named barrier BAR) for the block
 // that completes `total` of them, which also puts the counter back to zero. What the parts' blocks

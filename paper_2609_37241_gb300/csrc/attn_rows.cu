@@ -95,14 +95,12 @@ template <int DT, int D>
 struct RowsKernel {
   using G = RowsGeom<D>;
   using Split = AttnSplit<kRowsThreads, RowsCost>;
-  static constexpr int kSlots = kFanIn > kJoinGroups ? kFanIn : kJoinGroups;  // slots of a join at most
   struct Smem {
     alignas(128) char ring[G::RING];
     alignas(128) char q[2][G::QBUF];
     alignas(16) float part[4][G::PASS][G::LDO];
     typename Split::Smem split;
     float m[4][16], l[4][16];
-    float sm[kSlots][16], sl[kSlots][16];  // m and l of the slots of a join
     int last;
   };
 
@@ -317,41 +315,42 @@ struct RowsKernel {
     }
   }
 
-  // m and l of the slots at(i), i < n, i != own, into shared memory: one round of loads.
+  // Four elements of a row over slots at(i), i < n, in their order, eight at a time whose m, l and elements
+  // come in one round of loads; slot `own` is the part (a0, l0, m0) itself, as if it had gone through it.
   template <class At>
-  static __device__ __forceinline__ void slot_stats(Smem& s, const Unit& u, int n, int own, At at) {
-    for (int e = threadIdx.x; e < n * 16; e += kRowsThreads) {
-      const int i = e / 16, row = e % 16;
-      if (i == own || row >= u.rows) continue;
-      s.sm[i][row] = __ldcg(at(i) + row);
-      s.sl[i][row] = __ldcg(at(i) + kRowsTile + row);
-    }
-  }
-  static __device__ __forceinline__ float slot_max(const Smem& s, int row, int n, int own) {
-    float m = -INFINITY;
-    for (int i = 0; i < n; ++i)
-      if (i != own) m = fmaxf(m, s.sm[i][row]);
-    return m;
-  }
-  // The slots in their order, scaled to `base`; in the place of slot `own` the part (a0, l0, m0), which is the
-  // same as if it had gone through its slot.
-  template <class At>
-  static __device__ __forceinline__ void add_slots(const Smem& s, float4& a, float& l, float base, int row, int d, int n,
-                                                   At at, int own, const float4& a0, float l0, float m0) {
+  static __device__ __forceinline__ void add_slots(float4& a, float& l, float& m, int row, int d, int n, At at, int own,
+                                                   const float4& a0, float l0, float m0) {
+    a = make_float4(0.f, 0.f, 0.f, 0.f);
+    l = 0.f;
+    m = -INFINITY;
     for (int i0 = 0; i0 < n; i0 += 8) {
       float4 v[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {  // eight loads in flight
-        const int i = min(i0 + e, n - 1);
-        v[e] = a0;
-        if (i != own) v[e] = __ldcg(reinterpret_cast<const float4*>(at(i) + 2 * kRowsTile + row * D + d));
-      }
+      float ms[8], ls[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int i = i0 + e;
-        if (i >= n) continue;
-        const float f = fast_exp2((i == own ? m0 : s.sm[i][row]) - base);
-        l = fmaf(f, i == own ? l0 : s.sl[i][row], l);
+        const int i = min(i0 + e, n - 1);
+        const float* z = at(i);
+        v[e] = a0;
+        ms[e] = m0;
+        ls[e] = l0;
+        if (i != own) {
+          ms[e] = __ldcg(z + row);
+          ls[e] = __ldcg(z + kRowsTile + row);
+          v[e] = __ldcg(reinterpret_cast<const float4*>(z + 2 * kRowsTile + row * D + d));
+        }
+      }
+      float m2 = m;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) m2 = fmaxf(m2, ms[e]);
+      const float base = m2 == -INFINITY ? 0.f : m2, old = fast_exp2(m - base);
+      m = m2;
+      l *= old;
+      a.x *= old; a.y *= old; a.z *= old; a.w *= old;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (i0 + e >= n) continue;
+        const float f = fast_exp2(ms[e] - base);
+        l = fmaf(f, ls[e], l);
         a.x = fmaf(f, v[e].x, a.x); a.y = fmaf(f, v[e].y, a.y); a.z = fmaf(f, v[e].z, a.z); a.w = fmaf(f, v[e].w, a.w);
       }
     }
@@ -369,7 +368,6 @@ struct RowsKernel {
         s.m[w][g + 8 * k] = m[k];
         s.l[w][g + 8 * k] = l[k];
       }
-    slot_stats(s, u, n, own, at);
     for (int p0 = 0; p0 < u.rows; p0 += G::PASS) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -398,10 +396,7 @@ struct RowsKernel {
         if (n > 0) {
           const float4 a0 = a;
           const float l0 = ll, m0 = mm;
-          mm = fmaxf(mm, slot_max(s, row, n, own));
-          a = make_float4(0.f, 0.f, 0.f, 0.f);
-          ll = 0.f;
-          add_slots(s, a, ll, mm == -INFINITY ? 0.f : mm, row, d, n, at, own, a0, l0, m0);
+          add_slots(a, ll, mm, row, d, n, at, own, a0, l0, m0);
         }
         if (slot) {
           *reinterpret_cast<float4*>(slot + 2 * kRowsTile + row * D + d) = a;
@@ -435,15 +430,15 @@ struct RowsKernel {
   template <class At>
   static __device__ __forceinline__ void join_slots(const PagedAttnParams& p, Smem& s, const Unit& u, int n, At at,
                                                     float* dst) {
-    slot_stats(s, u, n, -1, at);
-    __syncthreads();
-    for (int e = threadIdx.x; e < u.rows * (D / 4); e += kRowsThreads) {
-      const int row = e / (D / 4), d = e % (D / 4) * 4;
-      const float m = slot_max(s, row, n, -1);
-      float l = 0.f;
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-      add_slots(s, a, l, m == -INFINITY ? 0.f : m, row, d, n, at, -1, a, 0.f, 0.f);
-      if (dst) {  // its m and l have been read by all, and its elements d .. d + 3 by this thread alone
+    for (int e0 = 0; e0 < u.rows * (D / 4); e0 += kRowsThreads) {  // whole rounds: see the barrier below
+      const int e = e0 + threadIdx.x, row = min(e / (D / 4), u.rows - 1), d = e % (D / 4) * 4;
+      const bool live = e < u.rows * (D / 4);
+      float m, l;
+      float4 a;
+      add_slots(a, l, m, row, d, n, at, -1, make_float4(0.f, 0.f, 0.f, 0.f), 0.f, 0.f);
+      if (dst) __syncthreads();  // dst is one of the slots: its m and l are read by all threads of the row first
+      if (!live) continue;
+      if (dst) {
         *reinterpret_cast<float4*>(dst + 2 * kRowsTile + row * D + d) = a;
         if (d == 0) {
           dst[row] = m;
@@ -492,7 +487,7 @@ struct RowsKernel {
 
   static __device__ __forceinline__ void run(const PagedAttnParams& p, Smem& s) {
     const AttnShare a = Split::share(p, s.split);
-    attn_fill_tail<kRowsThreads>(p);
+    if (p.part == ATTN_FEW) attn_lets_start(p, a.others);
     bool bad = false;
     int64_t run = 0, x = a.lo;
     for (int64_t b0 = 0; b0 < p.B && x < a.hi; b0 += kRowsThreads) {
@@ -561,6 +556,7 @@ struct RowsKernel {
       }
       x = max(x, end);  // a last unit of which only the beginning's tiles were this block's
     }
+    attn_fill_tail<kRowsThreads>(p);
     if (bad) atomicOr(p.err, kErrTable);
   }
 };
@@ -568,7 +564,8 @@ struct RowsKernel {
 template <int DT, int D>
 __global__ void __launch_bounds__(kRowsThreads, RowsGeom<D>::PER_SM) attn_rows_kernel(const PagedAttnParams p) {
   extern __shared__ __align__(128) char smem[];
-  pdl_prologue();
+  if (p.part == ATTN_ALL) pdl_trigger();
+  pdl_wait();
   using K = RowsKernel<DT, D>;
   K::run(p, *reinterpret_cast<typename K::Smem*>(smem));
 }

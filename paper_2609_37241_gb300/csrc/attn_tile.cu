@@ -811,12 +811,15 @@ struct Tile {
       __syncwarp();
       tc_before();
     }
-    pdl_prologue();
+    pdl_trigger();
+    bool work = true;
+    if (p.part == ATTN_ALL) pdl_wait();
+    else work = attn_starts(p);
     __syncthreads();
     tc_after();
     const uint32_t tmem = s.tmem;
-    const AttnShare a = Split::share(p, s.split);
-    attn_fill_tail<THREADS>(p);
+    AttnShare a{};
+    if (work) a = Split::share(p, s.split);
     uint32_t* counters = reinterpret_cast<uint32_t*>(p.work);
     float* slots = p.work + attn_counters(gridDim.x);
     Load ld;
@@ -837,6 +840,8 @@ struct Tile {
         else if (warp < LOAD_WARP) ok = mma(p, s, tmem, f, warp - MMA_WARP, mm, one);
       });
     }
+    if (p.part == ATTN_ALL) attn_fill_tail<THREADS>(p);
+    else attn_ends(p);
     // the way out: every copy and product of the block has to be done before its memory is given back
     if (warp >= LOAD_WARP && warp < LOAD_WARP + 2) {
       for (uint32_t i = ld.tiles > KS ? ld.tiles - KS : 0; i < ld.tiles; ++i) {

@@ -222,6 +222,7 @@ struct PagedAttnParams {
   FastDiv page, group;  // by ps; by G = Hq / Hkv
   int32_t part;                   // AttnPart: which requests this launch takes
   int64_t reread;                 // ... the bound between them (attn_takes)
+  uint32_t* start;                // where both kernels run: the word with which the first lets the second start
   int64_t min_tiles;              // a block's run of key tiles is at least this long
   int64_t join_tiles;             // what a cut unit costs, in tiles' time (0: units are always cut to even runs)
   int32_t tokens;                 // tile kernel: tokens of a row tile
@@ -372,6 +373,7 @@ struct AttnPlan {
   int64_t reread;
 };
 AttnPlan attn_plan(const AttnEntry& tile, int64_t T, int64_t B, int64_t G, int64_t D, int64_t ps, int64_t keys);
+constexpr int64_t kAttnWords = 32;  // of the workspace, for PagedAttnParams::start
 constexpr int kFanIn = 16, kJoinGroups = 20;  // slots joined in one round; groups of them at most
 constexpr int32_t kMaxAttnBlocks = kFanIn * kJoinGroups;
 int32_t attn_blocks(const AttnEntry& e, int32_t sms);

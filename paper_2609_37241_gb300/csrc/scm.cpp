@@ -1053,8 +1053,10 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
   }
   const AttnEntry &rows = v.ke.attn_rows, &tile = v.ke.attn_tile;
   const int64_t rows_work = attn_work_floats(rows, scm->sm_count);
-  if (a->t[6].shape[0] < rows_work + attn_work_floats(tile, scm->sm_count))
+  const int64_t tile_work = attn_work_floats(tile, scm->sm_count);
+  if (a->t[6].shape[0] < rows_work + tile_work + kAttnWords)
     return fail(TRIDENT_ERR_INVALID, "the workspace is smaller than trident_scm_workspace says");
+  p.start = reinterpret_cast<uint32_t*>(p.work + rows_work + tile_work);
   p.polls = kBulkWaitPolls;
   p.first_polls = (scm->opt.flags & TRIDENT_OPT_TEST_WAIT_TIMEOUT) ? 0u : kBulkWaitPolls;
   const AttnPlan pl = attn_plan(tile, s.T, p.B, p.G, p.D, p.page.d, p.M * p.page.d);
@@ -1068,7 +1070,7 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
     cfg.sharedMemBytes = (unsigned)rows.smem;
     const int32_t st = launch_on(scm, &cfg, v.fn, kp);
     if (st != TRIDENT_OK || !pl.tile) return st;
-    // the tile kernel's launch overlaps it; the kernel waits for it before its first access
+    // the tile kernel starts beside it (attn_starts)
     attr.id = CU_LAUNCH_ATTRIBUTE_PROGRAMMATIC_STREAM_SERIALIZATION;
     attr.value.programmaticStreamSerializationAllowed = 1;
     cfg.numAttrs = 1;
@@ -1769,7 +1771,8 @@ TRIDENT_API int32_t trident_scm_workspace(const trident_scm_t* scm, int32_t inde
     return fail(TRIDENT_ERR_INVALID, "no version %d", index);
   if (scm->dry) return fail(TRIDENT_ERR_STATE, "a dry-run SCM has no device to size a workspace for");
   const KernelEntry& ke = scm->versions[index].ke;
-  *out = attn_work_floats(ke.attn_rows, scm->sm_count) + attn_work_floats(ke.attn_tile, scm->sm_count);
+  if (ke.kind == KK_PAGED_ATTN && ke.vec > 1)
+    *out = attn_work_floats(ke.attn_rows, scm->sm_count) + attn_work_floats(ke.attn_tile, scm->sm_count) + kAttnWords;
   return TRIDENT_OK;
 }
 
