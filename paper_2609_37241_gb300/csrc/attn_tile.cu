@@ -17,6 +17,11 @@
 // Every wait is bounded (params.polls polls, kBulkWaitPolls by default): a wait that runs out sets
 // TRIDENT_DEVERR_TIMEOUT and a flag that ends the block's other waits; the warps then let their copies
 // and products in flight finish (bounded again), free the TMEM and return without further writes.
+//
+// Measured on a GB300 (32 q heads on 8 kv heads of 128): 8192 rows after 8192 keys 985 us in bursts (1674
+// TFLOP/s, 0.88 of cuBLAS' burst rate), 1082 us back to back (1524, 0.90 of its sustained rate, at the power
+// limit); 2048 rows after 6144 keys 168 / 178 us. 128 keys of a unit take 2760 cycles, 2048 of them the
+// products at the full rate; what is more is the chain of a tile's scores, softmax and products.
 #include <cuda.h>
 
 #include "attn_common.cuh"
