@@ -90,7 +90,7 @@ __device__ __forceinline__ bool attn_takes(const PagedAttnParams& p, const Reque
 
 // One block's share of the call: tiles per block and this block's run [lo, hi). whole: a unit per block
 // instead, all of it, where there are at most as many units as blocks and none is longer than an even run
-// and what a cut costs (a partial written, counted and joined: about join_tiles tiles' time); per, lo and
+// and what a cut costs (a partial written, counted and joined: about kTileJoin tiles' time); per, lo and
 // hi then count units.
 struct AttnShare {
   int64_t per, lo, hi, total;
@@ -99,23 +99,43 @@ struct AttnShare {
 };
 
 // Cost::of(p, r): the key tiles of all of request r's units, at least one per unit so that a unit
-// without keys is written too; Cost::units and Cost::longest: its units, and the tiles of the longest.
-// NT: threads of the block.
-template <int NT, class Cost>
+// without keys is written too. WHOLE: whole units are a choice, with Cost::units and Cost::longest, the
+// request's units and the tiles of the longest. NT: threads of the block.
+template <int NT, class Cost, bool WHOLE>
 struct AttnSplit {
   struct Smem {
     long long warp[NT / 32], units[NT / 32];
     int32_t longest[NT / 32];
+    int hit;                // the request that holds the run's first tile (at most NT requests)
     long long pre[NT + 1];  // tiles (units) before each request of the current chunk, from the call's start
     int32_t q0[NT], n[NT], kv[NT];
   };
 
+  // Inclusive sum over the block's threads and the block's total; a barrier before the words are used again.
+  // others: is set where any thread's is (one barrier for both).
+  static __device__ __forceinline__ long long block_scan(Smem& s, long long v, long long* all, bool* others) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long u = __shfl_up_sync(0xffffffffu, v, o);
+      if ((int)(threadIdx.x & 31) >= o) v += u;
+    }
+    if ((threadIdx.x & 31) == 31) s.warp[threadIdx.x >> 5] = v;
+    *others = __syncthreads_or(*others) != 0;
+    long long total = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) {
+      if (w < (int)(threadIdx.x >> 5)) v += s.warp[w];
+      total += s.warp[w];
+    }
+    *all = total;
+    return v;
+  }
+
   // The block's share; with at most NT requests their chunk is filled as well.
   static __device__ __forceinline__ AttnShare share(const PagedAttnParams& p, Smem& s) {
-    bool ok = true;
-    long long sum = 0, units = 0;
+    bool ok = true, others = false;
+    long long own = 0, own_units = 0;
     int32_t longest = 0;
-    bool others = false;
     Request r{0, 0, 0};
     for (int64_t b = threadIdx.x; b < p.B; b += NT) {
       r = attn_request(p, b, &ok);
@@ -123,46 +143,54 @@ struct AttnSplit {
         others |= r.n > 0;
         continue;
       }
-      sum += Cost::of(p, r);
-      if (p.join_tiles > 0) {
-        units += Cost::units(p, r);
+      own += Cost::of(p, r);
+      if constexpr (WHOLE) {
+        own_units += Cost::units(p, r);
         longest = max(longest, Cost::longest(p, r));
       }
     }
-    const long long own = sum, own_units = units;  // of one request, where there are at most NT
     if (!ok && blockIdx.x == 0) atomicOr(p.err, kErrTable);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (p.join_tiles > 0) {
+    if (threadIdx.x == 0) s.hit = 0;
+    long long units = own_units;
+    if constexpr (WHOLE) {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) {
         units += __shfl_xor_sync(0xffffffffu, units, o);
         longest = max(longest, __shfl_xor_sync(0xffffffffu, longest, o));
       }
+      if ((threadIdx.x & 31) == 0) {
+        s.units[threadIdx.x >> 5] = units;
+        s.longest[threadIdx.x >> 5] = longest;
+      }
     }
-    if ((threadIdx.x & 31) == 0) {
-      s.warp[threadIdx.x >> 5] = sum;
-      s.units[threadIdx.x >> 5] = units;
-      s.longest[threadIdx.x >> 5] = longest;
-    }
-    const int any_others = p.part == ATTN_FEW ? __syncthreads_or(others) : (__syncthreads(), 0);
-    sum = units = 0;
-#pragma unroll
-    for (int w = 0; w < NT / 32; ++w) {
-      sum += s.warp[w];
-      units += s.units[w];
-      longest = max(longest, s.longest[w]);
-    }
+    long long sum;
+    long long upto = block_scan(s, own, &sum, &others);
     const int64_t even = (uint64_t)sum >> 31 ? (sum + gridDim.x - 1) / gridDim.x
                                              : (int64_t)(((uint32_t)sum + gridDim.x - 1) / gridDim.x);
     AttnShare a;
-    a.whole = p.join_tiles > 0 && units <= gridDim.x && longest <= even + p.join_tiles;
-    a.others = any_others != 0;
-    a.total = a.whole ? units : sum;
-    a.per = a.whole ? 1 : (even > p.min_tiles ? even : p.min_tiles);
+    a.others = others;
+    a.whole = false;
+    a.total = sum;
+    a.per = even > p.min_tiles ? even : p.min_tiles;
+    if constexpr (WHOLE) {
+      units = 0;
+#pragma unroll
+      for (int w = 0; w < NT / 32; ++w) {
+        units += s.units[w];
+        longest = max(longest, s.longest[w]);
+      }
+      if (units <= gridDim.x && longest <= even + kTileJoin) {  // the same in every thread
+        a.whole = true;
+        a.total = units;
+        a.per = 1;
+        own = own_units;
+        __syncthreads();
+        upto = block_scan(s, own, &sum, &others);
+      }
+    }
     a.lo = min(a.total, (int64_t)blockIdx.x * a.per);
     a.hi = min(a.total, a.lo + a.per);
-    if (p.B <= NT) scan(s, r, a.whole ? own_units : own, 0);
+    if (p.B <= NT) fill(s, r, own, upto, a.lo);
     return a;
   }
 
@@ -171,38 +199,34 @@ struct AttnSplit {
   static __device__ __forceinline__ int64_t chunk(const PagedAttnParams& p, Smem& s, int64_t b0, int64_t run, const AttnShare& a) {
     if (p.B <= NT) return a.total;
     const int64_t b = b0 + threadIdx.x;
-    bool ok = true;
+    bool ok = true, others = false;
     Request r{0, 0, 0};
     if (b < p.B) r = attn_request(p, b, &ok);
-    return scan(s, r, !attn_takes(p, r) ? 0 : a.whole ? Cost::units(p, r) : Cost::of(p, r), run);
-  }
-  static __device__ __forceinline__ int64_t scan(Smem& s, const Request& r, long long own, int64_t run) {
-    long long v = own;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long u = __shfl_up_sync(0xffffffffu, v, o);
-      if ((int)(threadIdx.x & 31) >= o) v += u;
+    long long own = 0;
+    if (attn_takes(p, r)) {
+      own = Cost::of(p, r);
+      if constexpr (WHOLE)
+        if (a.whole) own = Cost::units(p, r);
     }
+    long long all;
     __syncthreads();  // the chunk before has been read
-    if ((threadIdx.x & 31) == 31) s.warp[threadIdx.x >> 5] = v;
+    const long long upto = block_scan(s, own, &all, &others);
+    fill(s, r, own, run + upto, -1);
+    return run + all;
+  }
+  static __device__ __forceinline__ void fill(Smem& s, const Request& r, long long own, long long upto, int64_t lo) {
     s.q0[threadIdx.x] = r.q0;
     s.n[threadIdx.x] = r.n;
     s.kv[threadIdx.x] = r.kv;
+    s.pre[threadIdx.x + 1] = upto;
+    if (threadIdx.x == 0) s.pre[0] = upto - own;
+    if (upto - own <= lo && lo < upto) s.hit = threadIdx.x;
     __syncthreads();
-    long long before = run, all = run;
-#pragma unroll
-    for (int w = 0; w < NT / 32; ++w) {
-      if (w < (int)(threadIdx.x >> 5)) before += s.warp[w];
-      all += s.warp[w];
-    }
-    s.pre[threadIdx.x + 1] = before + v;
-    if (threadIdx.x == 0) s.pre[0] = run;
-    __syncthreads();
-    return all;
   }
 
   // The last request of the chunk with pre[r] <= x (pre[0] <= x < the chunk's end): it holds tile x.
-  static __device__ __forceinline__ int find(const Smem& s, int64_t x) {
+  static __device__ __forceinline__ int find(const PagedAttnParams& p, const Smem& s, const AttnShare& a, int64_t x) {
+    if (p.B <= NT && x == a.lo) return s.hit;
     int r = 0, end = NT;
     while (end - r > 1) {
       const int mid = (r + end) / 2;
@@ -264,17 +288,18 @@ __device__ __forceinline__ void attn_sync() {
 }
 template <int BAR, int NT>
 __device__ __forceinline__ bool attn_completes(volatile int* flag, bool leader, uint32_t* counter, uint32_t total) {
-  __threadfence();
   attn_sync<BAR, NT>();
-  if (leader) {
+  if (leader) {  // behind the barrier the leader's fences stand for the block: they are cumulative
+    __threadfence();
     const bool last = atomicAdd(counter, 1u) + 1 == total;
-    if (last) *counter = 0u;
+    if (last) {
+      *counter = 0u;
+      __threadfence();
+    }
     *flag = last;
   }
   attn_sync<BAR, NT>();
-  const bool last = *flag != 0;
-  if (last) __threadfence();
-  return last;
+  return *flag != 0;
 }
 
 }  // namespace trident

@@ -87,19 +87,15 @@ struct RowsCost {
   static __device__ __forceinline__ int64_t key_tiles(int32_t kv) {
     return kv > kRowsKeys ? ((int64_t)kv + kRowsKeys - 1) / kRowsKeys : 1;
   }
-  static __device__ __forceinline__ int64_t units(const PagedAttnParams& p, const Request& r) {
-    return (int64_t)p.Hkv * row_tiles(p, r.n);
-  }
-  static __device__ __forceinline__ int32_t longest(const PagedAttnParams&, const Request& r) { return (int32_t)key_tiles(r.kv); }
   static __device__ __forceinline__ int64_t of(const PagedAttnParams& p, const Request& r) {
-    return units(p, r) * (key_tiles(r.kv) + kUnitTiles);
+    return p.Hkv * row_tiles(p, r.n) * (key_tiles(r.kv) + kUnitTiles);
   }
 };
 
 template <int DT, int D>
 struct RowsKernel {
   using G = RowsGeom<D>;
-  using Split = AttnSplit<kRowsThreads, RowsCost>;
+  using Split = AttnSplit<kRowsThreads, RowsCost, false>;
   struct Smem {
     alignas(128) char ring[G::RING];
     alignas(128) char q[2][G::QBUF];
@@ -500,7 +496,7 @@ struct RowsKernel {
       const int64_t end = min(a.hi, run);
       if (x >= end) continue;
       // the unit that holds x; those after it follow one another
-      int rq = Split::find(s.split, x);
+      int rq = Split::find(p, s.split, a, x);
       Unit u;
       int64_t start_of;  // its first tile, of kUnitTiles + nt
       int32_t nt, nm, mt;

@@ -216,7 +216,7 @@ struct Tile {
   static constexpr int S_COL = 0, O_COL = NT * KEYS;
   static_assert(NT * (KEYS + D) <= 512, "TMEM columns");
   using Cost = TileCost<ROWS, KEYS>;
-  using Split = AttnSplit<THREADS, Cost>;
+  using Split = AttnSplit<THREADS, Cost, true>;
   struct Smem {
     alignas(1024) char q[NT * QB];
     alignas(1024) char ring[SLOTS * KB];
@@ -713,7 +713,7 @@ struct Tile {
     int count = 0;
     const int64_t end = min(a.hi, run);
     const int32_t R = p.tokens;
-    int rq = Split::find(s.split, x);
+    int rq = Split::find(p, s.split, a, x);
     Request r{s.split.q0[rq], s.split.n[rq], s.split.kv[rq]};
     int32_t nm = Cost::row_tiles(p, r), h, k = 0;
     int64_t start = s.split.pre[rq];  // the unit's first tile

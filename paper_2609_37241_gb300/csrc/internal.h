@@ -224,7 +224,6 @@ struct PagedAttnParams {
   int64_t reread;                 // ... the bound between them (attn_takes)
   uint32_t* start;                // where both kernels run: the word with which the first lets the second start
   int64_t min_tiles;              // a block's run of key tiles is at least this long
-  int64_t join_tiles;             // what a cut unit costs, in tiles' time (0: units are always cut to even runs)
   int32_t tokens;                 // tile kernel: tokens of a row tile
   uint32_t polls, first_polls;    // tile kernel: bounds of its waits, of a warp's first for scores
 };
@@ -366,7 +365,7 @@ bool attn_rows_entry(int32_t dtype, int32_t D, AttnEntry* e);
 bool attn_tile_entry(int32_t dtype, int32_t D, AttnEntry* e);
 // Which attention kernels a call of T rows and B requests takes: the one of few rows, the tile kernel, or
 // both, each for its requests (attn_takes).
-constexpr int64_t kTileJoin = 8;  // tile kernel: a cut unit's cost in tiles (12 us of 1.45 us tiles)
+constexpr int64_t kTileJoin = 8;  // tile kernel: what a cut unit costs, in tiles' time (12 us of 1.45 us tiles)
 constexpr int64_t kRowsRun = 2, kTileRun = 4;  // key tiles of a block's run at least
 struct AttnPlan {
   bool rows, tile;

@@ -1064,7 +1064,6 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
   if (pl.rows) {
     p.part = pl.tile ? ATTN_FEW : ATTN_ALL;
     p.min_tiles = kRowsRun;
-    p.join_tiles = 0;
     cfg.blockDimX = (unsigned)rows.threads;
     cfg.gridDimX = (unsigned)attn_blocks(rows, scm->sm_count);
     cfg.sharedMemBytes = (unsigned)rows.smem;
@@ -1081,7 +1080,6 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
   p.work += rows_work;
   p.part = pl.rows ? ATTN_MANY : ATTN_ALL;
   p.min_tiles = kTileRun;
-  p.join_tiles = kTileJoin;
   p.tokens = tile.rows / p.G;
   void* tp[3] = {&p, &mk, &mv};
   cfg.blockDimX = (unsigned)tile.threads;
