@@ -363,6 +363,67 @@ def test_paged_attention_reports_a_wait_that_ran_out(S):
     s.close()
 
 
+def far_pool(P, Hkv, ps, D):
+    """k and v of one buffer whose pages start 2^28 elements apart, v's 2^27 behind k's."""
+    base = torch.empty(P << 28, dtype=torch.bfloat16, device="cuda")
+    return tuple(base.as_strided((P, Hkv, ps, D), (1 << 28, ps * D, D, 1), at) for at in (0, 1 << 27))
+
+
+@pytest.mark.parametrize("variant", ["AUTO", "GENERIC"])
+@pytest.mark.parametrize("new,kv,ps,row", [([1, 4], [700, 330], 64, 1 << 29), ([38], [21000], 2048, 1 << 26)])
+def test_offsets_past_32_bits(S, new, kv, ps, row, variant):
+    """Pages and rows of q beyond 2^31 elements: the same bits as from dense tensors, which are
+    checked against the formula."""
+    g = np.random.default_rng(77)
+    Hq, Hkv, D, dt = 32, 2, 128, S.BF16
+    s, index, work = attn_scm(S, dt, Hq, Hkv, D, ps, getattr(S, "VARIANT_" + variant))
+    b = R.batch(g, new, kv, Hq, Hkv, D, ps, dt, spare=7)
+    P, T = b["kc"].shape[0], b["q"].shape[0]
+    dense = check_attn(S, b, Hq, Hkv, D, ps, dt, 1.0 / D ** 0.5, 0, s, index, work)
+    far = dict(b, out=torch.full_like(b["out"], float("nan")))
+    far["kc"], far["vc"] = far_pool(P, Hkv, ps, D)
+    far["kc"].copy_(b["kc"])
+    far["vc"].copy_(b["vc"])
+    far["q"] = torch.empty(T * row, dtype=torch.bfloat16, device="cuda").as_strided((T, Hq, D), (row, D, 1))
+    far["q"].copy_(b["q"])
+    used = b["table"][b["table"] < P].max().item()
+    assert used << 28 >= 1 << 31 and (T - 1) * row >= 1 << 31
+    assert torch.equal(check_attn(S, far, Hq, Hkv, D, ps, dt, 1.0 / D ** 0.5, 0, s, index, work), dense)
+    s.close()
+
+
+@pytest.mark.parametrize("variant", ["AUTO", "GENERIC"])
+def test_rope_paged_offsets_past_32_bits(S, variant):
+    g = np.random.default_rng(78)
+    T, Hq, Hkv, D, ps, P = 35, 4, 2, 128, 16, 18
+    s = S.Scm()
+    s.register(S.make_spec(S.OP_ROPE_PAGED_KV, S.BF16, [Hq, Hkv, D, D, ps], 1, 64, layout=S.LAYOUT_ANY,
+                           variant=getattr(S, "VARIANT_" + variant)))
+    q, k, v = (torch.from_numpy(g.standard_normal((T, h, D), dtype=np.float32)).bfloat16().cuda() for h in (Hq, Hkv, Hkv))
+    far_q = torch.empty(T << 26, dtype=torch.bfloat16, device="cuda").as_strided((T, Hq, D), (1 << 26, D, 1))
+    far_q.copy_(q)
+    slots = g.permutation(P * ps)[:T]
+    slots[0] = P * ps - 1  # the last row of the last page
+    assert len(set(slots.tolist())) == T
+    pos, freqs = i32(g.integers(0, 9000, T)), S.rope_freqs(10000.0, D)
+    got = []
+    for x, (kc, vc) in ((q, R.pool(g, P, Hkv, ps, D, S.BF16, "head")), (far_q, far_pool(P, Hkv, ps, D))):
+        kc.fill_(0.0)
+        vc.fill_(0.0)
+        q_out = torch.full_like(q, float("nan"))
+        args = S.make_args(S.OP_ROPE_PAGED_KV, [x, k, v, pos, i32(slots), freqs, q_out, kc, vc], scalar=1.0)
+        assert s.invoke(args, stream()) == (S.OK, 0), S.trident_scm_last_error()
+        assert S.trident_scm_device_status(s.h, stream())[1] == 0
+        got.append((q_out.cpu(), kc.cpu(), vc.cpu()))
+    want = R.rotate(k.cpu().double(), pos.cpu(), freqs.cpu().double().sum(1), 1.0, False)
+    page, at = slots // ps, slots % ps
+    tol = 2.0 ** -8 * want.abs() * 1.01 + 8e-6 * want.abs().amax(-1, keepdim=True) * 2 ** 0.5 + 2.0 ** -25
+    assert ((got[0][1][page, :, at].double() - want).abs() <= tol).all()
+    for near, far in zip(*got):
+        assert torch.equal(near, far)
+    s.close()
+
+
 @pytest.mark.parametrize("D", [8, 40, 96, 512])
 @pytest.mark.parametrize("dtype", ["BF16", "FP16"])
 def test_paged_attention_other_head_sizes(S, D, dtype):
