@@ -3,9 +3,9 @@
 // Bound: HBM. A unit's 16 rows (of mma.m16n8k16; a decode step of G = 4 fills four) read every key once,
 // 4 flops per byte and used row, so the legacy tensor instructions suffice and their padding rows cost
 // nothing that the memory does not wait for. What matters is bytes in flight, so every warp is a stream
-// of its own: it takes 16 keys of each 64-key tile, keeps a ring of NS stages (16 rows of k and of v)
-// filled by cp.async and never waits for another warp until the fragment's end, where the four warps'
-// (m, l, out) are joined in shared memory. Any page size and any strides: cp.async copies 16 bytes to
+// of its own: it takes a fourth of each tile's keys (16 of 64; heads of 64: 32 of 128), keeps a ring of NS
+// stages of them filled by cp.async and never waits for another warp until the fragment's end, where the four
+// warps' (m, l, out) are joined in shared memory. Any page size and any strides: cp.async copies 16 bytes to
 // where the swizzle puts them (chunk ^ row mod 8: ldmatrix reads eight rows from eight bank groups).
 // Rows past the unit's last visible key are filled with zeros, not read.
 //
@@ -15,7 +15,7 @@
 //
 // Measured on a GB300 (32 q heads on 8 kv heads of 128 where nothing else is said; of the 6.79 TB/s copy
 // rate): 64 requests of 1000 to 8000 keys 177 us (0.99), 3 of 131071 keys 237 us (1.00), 64 of 4000 keys with
-// 4 kv heads of 256 164 us (0.94); one request of 1000 keys 9.0 us, four dependent rounds of loads and the
+// 4 kv heads of 256 164 us (0.94); one request of 1000 keys 8.5 us, four dependent rounds of loads and the
 // join of its parts.
 #include "attn_common.cuh"
 
@@ -24,15 +24,19 @@ namespace {
 
 constexpr int kRowsThreads = 128;
 constexpr int kRowsTile = 16;   // rows of a unit
-constexpr int kRowsKeys = 64;   // keys of a tile, 16 per warp
 constexpr float kLazy = 8.f;
 
 template <int D>
 struct RowsGeom {
   static constexpr int CH = D / 8;              // 16-byte chunks per row
-  static constexpr int HALF = 16 * D * 2;       // bytes of a stage's k (and of its v)
+  // 16-key groups that a warp takes at a time. Heads of 64: two, since the fixed part of a step (waits, the
+  // maximum's exchange, page numbers) and its chain of dependent instructions bound it before the memory does:
+  // 48 requests of about 3 rows 37.5 -> 30.8 us, 200 decode steps of 1700 keys 125 -> 113 us.
+  static constexpr int KG = D == 64 ? 2 : 1;
+  static constexpr int KEYS = 64 * KG;          // keys of a tile, a fourth of them per warp
+  static constexpr int HALF = 16 * KG * D * 2;  // bytes of a stage's k (and of its v)
   static constexpr int STAGE = 2 * HALF;
-  static constexpr int NS = D == 64 ? 6 : 3;    // stages per warp: 24 KB in flight, D 256 48 KB
+  static constexpr int NS = 3;                  // stages per warp: 24 KB, D 256 48 KB
   static constexpr int RING = 4 * NS * STAGE;
   static constexpr int PER_SM = D == 256 ? 1 : 2;
   static constexpr int PASS = 512 / D;          // rows that the warps join at a time: a float4 per thread
@@ -78,14 +82,16 @@ struct Unit {
 // Every row tile counted with all of the request's keys: exact for decode steps, a little unequal where a
 // long chunk comes this way; and with kUnitTiles for its beginning and end, which take a block as long as
 // that many tiles do (a block of many short units would otherwise be the last: 48 requests of about 3 rows of
-// D 64, the slowest block 38.9 us, the median one 28.7). A cut in these tiles moves to the unit's beginning.
+// D 64, the slowest block 38.9 us, the median one 28.7; with tiles of 128 keys 3 is still the best of 1 to 3).
+// A cut in these tiles moves to the unit's beginning.
 constexpr int kUnitTiles = 3;
+template <int KEYS>
 struct RowsCost {
   static __device__ __forceinline__ int64_t row_tiles(const PagedAttnParams& p, int32_t n) {
     return ((int64_t)n * p.G + kRowsTile - 1) / kRowsTile;
   }
   static __device__ __forceinline__ int64_t key_tiles(int32_t kv) {
-    return kv > kRowsKeys ? ((int64_t)kv + kRowsKeys - 1) / kRowsKeys : 1;
+    return kv > KEYS ? ((int64_t)kv + KEYS - 1) / KEYS : 1;
   }
   static __device__ __forceinline__ int64_t of(const PagedAttnParams& p, const Request& r) {
     return p.Hkv * row_tiles(p, r.n) * (key_tiles(r.kv) + kUnitTiles);
@@ -95,7 +101,9 @@ struct RowsCost {
 template <int DT, int D>
 struct RowsKernel {
   using G = RowsGeom<D>;
-  using Split = AttnSplit<kRowsThreads, RowsCost, false>;
+  static constexpr int KG = G::KG, KEYS = G::KEYS, WARP = 16 * KG;  // WARP: keys of a tile that are one warp's
+  using Cost = RowsCost<KEYS>;
+  using Split = AttnSplit<kRowsThreads, Cost, false>;
   struct Smem {
     alignas(128) char ring[G::RING];
     alignas(128) char q[2][G::QBUF];
@@ -105,44 +113,48 @@ struct RowsKernel {
     int last;
   };
 
-  // The table's entry for the lane's row (lane mod 16) of the 16 keys from j0 on. It is asked for a stage
+  // The table's entry for the lane's row (lane mod WARP) of the keys from j0 on. It is asked for a stage
   // before its copies are issued, so that they do not wait for it.
   static __device__ __forceinline__ int32_t entry(const PagedAttnParams& p, const Unit& u, int32_t j0) {
-    const uint32_t j = (uint32_t)min(j0 + (int32_t)(threadIdx.x & 15), u.limit - 1);
+    const uint32_t j = (uint32_t)min(j0 + (int32_t)(threadIdx.x & (WARP - 1)), u.limit - 1);
     return p.table[u.b * p.table_rs + fast_div(j, p.page.magic, p.page.shift)];
   }
 
-  // Issues the copies of 16 keys from j0 on into a stage; page: what entry() gave for them.
+  // Issues the copies of WARP keys from j0 on into a stage; page: what entry() gave for them.
   static __device__ __forceinline__ void load(const PagedAttnParams& p, const Unit& u, const char* kb, const char* vb,
                                               int32_t j0, int32_t page, uint32_t stage, bool* bad) {
     const int lane = threadIdx.x & 31;
     constexpr int RPI = 32 / G::CH > 0 ? 32 / G::CH : 1;  // rows per instruction (D 256: one)
-    constexpr int ITER = 16 / RPI;
+    constexpr int ITER = 16 / RPI;  // for 16 rows
     const int c = lane % G::CH, rr = lane / G::CH;
     if (page < 0 || page >= p.P) {
       *bad = true;
       page = 0;
     }
-    const uint32_t j = (uint32_t)min(j0 + (lane & 15), u.limit - 1);
+    const uint32_t j = (uint32_t)min(j0 + (lane & (WARP - 1)), u.limit - 1);
     const int32_t at = (int32_t)(j - fast_div(j, p.page.magic, p.page.shift) * (uint32_t)p.page.d);
-    if (p.page.d % 16 == 0) {  // one page for all 16 rows
-      const int32_t at0 = __shfl_sync(0xffffffffu, at, 0);
-      const char* ks = kb + ((int64_t)page * p.kc.page + (int64_t)(at0 + rr) * p.kc.row + c * 8) * 2;
-      const char* vs = vb + ((int64_t)page * p.vc.page + (int64_t)(at0 + rr) * p.vc.row + c * 8) * 2;
+    if (p.page.d % 16 == 0) {  // one page for 16 rows
       const int64_t kstep = RPI * p.kc.row * 2, vstep = RPI * p.vc.row * 2;
 #pragma unroll
-      for (int i = 0; i < ITER; ++i) {
-        const int r = rr + i * RPI;
-        const bool live = j0 + r < u.limit;
-        const uint32_t dst = stage + r * (D * 2) + ((c ^ (r & 7)) << 4);
-        cp16(dst, live ? ks + i * kstep : kb, live);
-        cp16(dst + G::HALF, live ? vs + i * vstep : vb, live);
+      for (int h = 0; h < KG; ++h) {
+        const int32_t at0 = __shfl_sync(0xffffffffu, at, 16 * h);
+        const int32_t pg = KG == 1 ? page : __shfl_sync(0xffffffffu, page, 16 * h);
+        const char* ks = kb + ((int64_t)pg * p.kc.page + (int64_t)(at0 + rr) * p.kc.row + c * 8) * 2;
+        const char* vs = vb + ((int64_t)pg * p.vc.page + (int64_t)(at0 + rr) * p.vc.row + c * 8) * 2;
+#pragma unroll
+        for (int i = 0; i < ITER; ++i) {
+          const int r = 16 * h + rr + i * RPI;
+          const bool live = j0 + r < u.limit;
+          const uint32_t dst = stage + r * (D * 2) + ((c ^ (r & 7)) << 4);
+          cp16(dst, live ? ks + i * kstep : kb, live);
+          cp16(dst + G::HALF, live ? vs + i * vstep : vb, live);
+        }
       }
     } else {  // each row's place from the lane that looked it up
       const int64_t ko = ((int64_t)page * p.kc.page + (int64_t)at * p.kc.row) * 2;
       const int64_t vo = ((int64_t)page * p.vc.page + (int64_t)at * p.vc.row) * 2;
 #pragma unroll
-      for (int i = 0; i < ITER; ++i) {
+      for (int i = 0; i < KG * ITER; ++i) {
         const int r = rr + i * RPI;
         const bool live = j0 + r < u.limit;
         const int64_t kr = __shfl_sync(0xffffffffu, ko, r), vr = __shfl_sync(0xffffffffu, vo, r);
@@ -156,7 +168,7 @@ struct RowsKernel {
   // What a warp holds of a fragment between its first loads and its last product.
   struct State {
     const char *kb, *vb;
-    int32_t first, groups;  // its 16-key groups: keys first + 64 x, x < groups
+    int32_t first, groups;  // its groups of WARP keys: from first + KEYS x on, x < groups
     int32_t page;           // entry() of the next group to copy
     int32_t see[2];         // keys that rows g and g + 8 see
     uint32_t q[G::QREG][4];
@@ -197,15 +209,15 @@ struct RowsKernel {
     st.kb = reinterpret_cast<const char*>(p.kc.base) + (int64_t)u.h * p.kc.head * 2;
     st.vb = reinterpret_cast<const char*>(p.vc.base) + (int64_t)u.h * p.vc.head * 2;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s.ring) + w * (G::NS * G::STAGE);
-    st.first = u.t0 * kRowsKeys + 16 * w;
-    const int32_t upto = (int32_t)min((int64_t)u.limit, (int64_t)u.t1 * kRowsKeys);
-    st.groups = st.first < upto ? (upto - st.first + kRowsKeys - 1) / kRowsKeys : 0;
+    st.first = u.t0 * KEYS + WARP * w;
+    const int32_t upto = (int32_t)min((int64_t)u.limit, (int64_t)u.t1 * KEYS);
+    st.groups = st.first < upto ? (upto - st.first + KEYS - 1) / KEYS : 0;
     int32_t page[G::NS];
 #pragma unroll
-    for (int i = 0; i < G::NS; ++i) page[i] = i < st.groups ? entry(p, u, st.first + i * kRowsKeys) : 0;
+    for (int i = 0; i < G::NS; ++i) page[i] = i < st.groups ? entry(p, u, st.first + i * KEYS) : 0;
 #pragma unroll
     for (int i = 0; i < G::NS - 1; ++i) {
-      if (i < st.groups) load(p, u, st.kb, st.vb, st.first + i * kRowsKeys, page[i], ring + i * G::STAGE, bad);
+      if (i < st.groups) load(p, u, st.kb, st.vb, st.first + i * KEYS, page[i], ring + i * G::STAGE, bad);
       cp_commit();
     }
     st.page = page[G::NS - 1];
@@ -232,18 +244,15 @@ struct RowsKernel {
         const int y = x + G::NS - 1;
         if (y < st.groups) {
           const int32_t page = st.page;
-          if (y + 1 < st.groups) st.page = entry(p, u, st.first + (y + 1) * kRowsKeys);
-          load(p, u, st.kb, st.vb, st.first + y * kRowsKeys, page, ring + (y % G::NS) * G::STAGE, bad);
+          if (y + 1 < st.groups) st.page = entry(p, u, st.first + (y + 1) * KEYS);
+          load(p, u, st.kb, st.vb, st.first + y * KEYS, page, ring + (y % G::NS) * G::STAGE, bad);
         }
         cp_commit();
       }
       const uint32_t at = ring + (x % G::NS) * G::STAGE;
-      float sc[2][4] = {}, odd[2][4] = {};  // two chains of products, half as long
+      float sc[2 * KG][4] = {}, odd[2 * KG][4] = {};  // two chains of products, half as long
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
-        uint32_t kf[4];
-        const int key = (mi >> 1) * 8 + mr, ch = kk * 2 + (mi & 1);
-        ldsm4(kf, at + key * (D * 2) + ((ch ^ (key & 7)) << 4));
         uint32_t qf[4];
         if constexpr (G::QS) {
           const int row = (mi & 1) * 8 + mr, qch = kk * 2 + (mi >> 1);
@@ -252,24 +261,32 @@ struct RowsKernel {
 #pragma unroll
           for (int e = 0; e < 4; ++e) qf[e] = st.q[kk][e];
         }
-        mma16816<DT>(kk & 1 ? odd[0] : sc[0], qf, kf[0], kf[1]);
-        mma16816<DT>(kk & 1 ? odd[1] : sc[1], qf, kf[2], kf[3]);
+#pragma unroll
+        for (int h = 0; h < KG; ++h) {
+          uint32_t kf[4];
+          const int key = 16 * h + (mi >> 1) * 8 + mr, ch = kk * 2 + (mi & 1);
+          ldsm4(kf, at + key * (D * 2) + ((ch ^ (key & 7)) << 4));
+          mma16816<DT>(kk & 1 ? odd[2 * h] : sc[2 * h], qf, kf[0], kf[1]);
+          mma16816<DT>(kk & 1 ? odd[2 * h + 1] : sc[2 * h + 1], qf, kf[2], kf[3]);
+        }
       }
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
+      for (int nt = 0; nt < 2 * KG; ++nt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) sc[nt][e] += odd[nt][e];
-      const int32_t j0 = st.first + x * kRowsKeys;
-      if (j0 + 16 > min(st.see[0], st.see[1]))  // some key is hidden from a row
+      const int32_t j0 = st.first + x * KEYS;
+      if (j0 + WARP > min(st.see[0], st.see[1]))  // some key is hidden from a row
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
+        for (int nt = 0; nt < 2 * KG; ++nt)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (j0 + nt * 8 + 2 * t + (e & 1) >= st.see[e >> 1]) sc[nt][e] = -INFINITY;
       float top[2];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        top[k] = fmaxf(fmaxf(sc[0][2 * k], sc[0][2 * k + 1]), fmaxf(sc[1][2 * k], sc[1][2 * k + 1]));
+        top[k] = fmaxf(sc[0][2 * k], sc[0][2 * k + 1]);
+#pragma unroll
+        for (int nt = 1; nt < 2 * KG; ++nt) top[k] = fmaxf(top[k], fmaxf(sc[nt][2 * k], sc[nt][2 * k + 1]));
         top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 1));
         top[k] = c * fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], 2));
       }
@@ -287,25 +304,27 @@ struct RowsKernel {
           }
         }
       }
-      uint32_t pf[4];
+      uint32_t pf[KG][4];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const float base = m[k] == -INFINITY ? 0.f : m[k];
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
+        for (int nt = 0; nt < 2 * KG; ++nt) {
           const float e0 = fast_exp2(fmaf(sc[nt][2 * k], c, -base)), e1 = fast_exp2(fmaf(sc[nt][2 * k + 1], c, -base));
           l[k] += e0 + e1;
-          pf[2 * nt + k] = ActType<DT>::pack2(e0, e1);
+          pf[nt / 2][2 * (nt & 1) + k] = ActType<DT>::pack2(e0, e1);
         }
       }
 #pragma unroll
-      for (int dd = 0; dd < D / 16; ++dd) {
-        uint32_t vf[4];
-        const int key = (mi & 1) * 8 + mr, ch = dd * 2 + (mi >> 1);
-        ldsm4t(vf, at + G::HALF + key * (D * 2) + ((ch ^ (key & 7)) << 4));
-        mma16816<DT>(o[2 * dd], pf, vf[0], vf[1]);
-        mma16816<DT>(o[2 * dd + 1], pf, vf[2], vf[3]);
-      }
+      for (int h = 0; h < KG; ++h)
+#pragma unroll
+        for (int dd = 0; dd < D / 16; ++dd) {
+          uint32_t vf[4];
+          const int key = 16 * h + (mi & 1) * 8 + mr, ch = dd * 2 + (mi >> 1);
+          ldsm4t(vf, at + G::HALF + key * (D * 2) + ((ch ^ (key & 7)) << 4));
+          mma16816<DT>(o[2 * dd], pf[h], vf[0], vf[1]);
+          mma16816<DT>(o[2 * dd + 1], pf[h], vf[2], vf[3]);
+        }
     }
     cp_wait<0>();
     __syncwarp();  // the ring has been read by all lanes
@@ -505,8 +524,8 @@ struct RowsKernel {
         u.q0 = s.split.q0[rq];
         u.n = s.split.n[rq];
         u.kv = s.split.kv[rq];
-        nt = (int32_t)RowsCost::key_tiles(u.kv);
-        nm = (int32_t)RowsCost::row_tiles(p, u.n);
+        nt = (int32_t)Cost::key_tiles(u.kv);
+        nm = (int32_t)Cost::row_tiles(p, u.n);
       };
       request_of();
       {
