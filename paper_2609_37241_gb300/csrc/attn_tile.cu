@@ -435,7 +435,10 @@ struct Tile {
       if (turns) turn_wait(x);
       F2 sum[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
       F2 cc = f2_pack(c, c), mm = cc;
-      // numerators of half the tile's keys, to the columns of its scores
+      auto pass = [&]() {
+        if (turns && (x == 0 || t + 1 < t1)) turn_pass(x);
+      };
+      // numerators of half the tile's keys, to the columns of its scores; the turn ends inside the second half
       auto half = [&](int h) {
         uint32_t w[KEYS / 4];
 #pragma unroll
@@ -447,9 +450,10 @@ struct Tile {
           v = fast_exp2(v);
           sum[i & 1] = f2_add(sum[i & 1], f2_pack(u, v));
           w[i] = ActType<DT>::pack2(u, v);
+          if (h == 1 && i == KEYS / 16 - 1) pass();
         }
-        if constexpr (KEYS == 128) tc_st32(sc + h * 32, w);
-        else tc_st16(sc + h * 16, w);
+#pragma unroll
+        for (int k = 0; k < KEYS / 64; ++k) tc_st16(sc + h * (KEYS / 4) + k * 16, w + k * 16);
         tc_wait_st();
         tc_before();
         mb_arrive(smem_at(h == 0 ? &s.p_half[x] : &s.p_full[x]));
@@ -492,13 +496,12 @@ struct Tile {
         const float base = m == -INFINITY ? 0.f : m;
         mm = f2_pack(-base, -base);
         half(0);  // its products start while the second half's numerators are made
-      }
-      if (turns && (x == 0 || t + 1 < t1)) turn_pass(x);
-      if (ok) {
         half(1);
         float s0, s1;
         f2_unpack(f2_add(sum[0], sum[1]), &s0, &s1);
         l += s0 + s1;
+      } else {
+        pass();
       }
     }
     *m_out = m;
