@@ -420,9 +420,10 @@ struct Tile {
                                                  Soft& st, bool ok, float* m_out, float* l_out) {
     const uint32_t lanes = tmem + (((threadIdx.x >> 5) & 3) << 21);  // TMEM lane 32 * (warp mod 4)
     const uint32_t sc = lanes + S_COL + x * KEYS, oc = lanes + O_COL + x * D;
-    const int r = x * 128 + (threadIdx.x & 127);
-    const int32_t k = (int32_t)fast_div((uint32_t)r, p.group.magic, p.group.shift);
-    const int32_t see = r < f.rows ? f.kv - f.n + f.tok0 + k + 1 : 0;
+    // Rows past the unit's (their q is zeros, their results go nowhere) see what its last one does: a row that
+    // sees less has every tile's scores masked, and the turn waits for that (1.75 us per tile instead of 1.25).
+    const int r = min(x * 128 + (int)(threadIdx.x & 127), f.rows - 1);
+    const int32_t see = f.kv - f.n + f.tok0 + (int32_t)fast_div((uint32_t)r, p.group.magic, p.group.shift) + 1;
     const float c = p.scale * kLog2e;
     const bool turns = NT == 2 && f.rows > 128;
     const int32_t t0 = f.t0, t1 = f.t1;
