@@ -82,11 +82,14 @@ __global__ void __launch_bounds__(kThreads) attn_generic_kernel(const PagedAttnP
 
 // The kernel of few rows takes 16 of them (tokens x heads of a group) to a unit and reads the keys again for
 // every further 16; the tile kernel reads them once, but its units cost more to begin and to end. Measured,
-// few rows / tile kernel: 32 requests of 32 rows over 8000 keys of D 128 314 / 203 us, of 20 rows over 1000
-// keys 52.7 / 54.5; 16 of 128 rows over 2000 123 / 41; 4 of 24 over 500 15.7 / 18.0; 48 of 7 to 35 rows over
-// 400 to 3000 of D 64 36.5 / 49.5, of 35 rows over 3000 79 / 65; 8 of 32 over 4000 of D 256 100 / 57. So the
-// bound is by elements read again: kReread.
-constexpr int64_t kReread = 6000 * 128;
+// few rows / tile kernel (us, D 128, 4 heads to a group, where nothing else is said): 32 requests of 32 rows
+// over 8000 keys 311 / 184, of 20 rows over 1000 47 / 50; 16 of 128 over 2000 126 / 43, of 32 over 4000
+// 73 / 61; 8 of 64 over 1500 34 / 29, of 32 over 3000 35 / 42; 4 of 24 over 500 14 / 17; D 64, 48 of 7 to 35
+// rows over 400 to 3000 28 / 44, 16 of 64 over 3000 53 / 40; D 256, 8 of 32 over 4000 57 / 56. So the bound is
+// by a request's elements read again: kReread. A single request does not fill the memory's rate with them:
+// 96 rows over 1000 keys 14.6 / 18.5, over 2000 17.8 / 19.8, 256 over 1000 20.7 / 22.8, 400 over 1000
+// 24.7 / 22.9; D 64, 210 over 2000 12.5 / 17.7; so there it is kRereadOne.
+constexpr int64_t kReread = 4000 * 128, kRereadOne = 20000 * 128;
 
 // The lengths are on the device, so the choice goes by what T, B and the table's width (keys) leave
 // possible: both kernels, unless no request can pass the bound, or there is one request only. Pages that do
@@ -96,7 +99,7 @@ AttnPlan attn_plan(const AttnEntry& tile, int64_t T, int64_t B, int64_t G, int64
   const bool fits = tile.fn && G <= 128 && ps % 8 == 0 && (tile.keys % ps == 0 || ps % tile.keys == 0);
   const int64_t most = T > B ? T - B + 1 : 1;  // rows of a request, if every one has some
   AttnPlan pl;
-  pl.reread = (kReread + D - 1) / D;
+  pl.reread = ((B == 1 ? kRereadOne : kReread) + D - 1) / D;
   pl.tile = fits && ((most * G + 15) / 16 - 1) * keys >= pl.reread;
   pl.rows = !pl.tile || B > 1;
   return pl;

@@ -365,7 +365,7 @@ bool attn_rows_entry(int32_t dtype, int32_t D, AttnEntry* e);
 bool attn_tile_entry(int32_t dtype, int32_t D, AttnEntry* e);
 // Which attention kernels a call of T rows and B requests takes: the one of few rows, the tile kernel, or
 // both, each for its requests (attn_takes).
-constexpr int64_t kTileJoin = 8;  // tile kernel: what a cut unit costs, in tiles' time (12 us of 1.45 us tiles)
+constexpr int64_t kTileJoin = 10;  // tile kernel: what a cut unit costs, in tiles' time (12 us, a tile 1.25)
 constexpr int64_t kRowsRun = 1, kTileRun = 4;  // key tiles of a block's run at least
 struct AttnPlan {
   bool rows, tile;
