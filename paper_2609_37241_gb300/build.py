@@ -18,7 +18,7 @@ LIB = os.path.join(LIBDIR, "libtrident_scm.so")
 SOURCES = ["scm.cpp", "tree.cpp", "norm.cu", "rope.cu", "pointwise.cu", "chain.cu",
            "noalloc.cu", "page_map.cu", "rope_paged.cu", "attn.cu",
            "attn_rows.cu", "attn_tile.cu"]
-HEADERS = ["internal.h", "device_common.cuh", "tree.h", "measure.h", "attn_common.cuh"]
+HEADERS = ["internal.h", "device_common.cuh", "tree.h", "measure.h", "attn_common.cuh", "attn_count.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-fvisibility=hidden",
          "-I", INC, "-I", CSRC]

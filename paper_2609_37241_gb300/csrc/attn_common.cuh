@@ -14,6 +14,7 @@
 // fragment order, so that the result does not depend on which one that is; above kFanIn fragments in two
 // levels, since one block reading hundreds would take longer than the attention itself.
 #pragma once
+#include "attn_count.h"
 #include "device_common.cuh"
 
 namespace trident {
@@ -279,27 +280,22 @@ __device__ __forceinline__ void attn_ends(const PagedAttnParams& p) {
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.start = 0u;
 }
 
-// Counts a finished part; true in every thread of the NT that call it (named barrier BAR) for the block
-// that completes `total` of them, which also puts the counter back to zero. What the parts' blocks
-// wrote before is visible to it. flag: a shared word.
+// The block as attn_count.h sees it: NT threads at named barrier BAR, their words in shared memory.
 template <int BAR, int NT>
 __device__ __forceinline__ void attn_sync() {
   asm volatile("bar.sync %0, %1;" :: "n"(BAR), "n"(NT) : "memory");
 }
 template <int BAR, int NT>
-__device__ __forceinline__ bool attn_completes(volatile int* flag, bool leader, uint32_t* counter, uint32_t total) {
-  attn_sync<BAR, NT>();
-  if (leader) {  // behind the barrier the leader's fences stand for the block: they are cumulative
-    __threadfence();
-    const bool last = atomicAdd(counter, 1u) + 1 == total;
-    if (last) {
-      *counter = 0u;
-      __threadfence();
-    }
-    *flag = last;
-  }
-  attn_sync<BAR, NT>();
-  return *flag != 0;
-}
+struct AttnBlock {
+  volatile int* words;  // kAttnAnswers of them
+  __device__ __forceinline__ void sync() const { attn_sync<BAR, NT>(); }
+  __device__ __forceinline__ bool leader() const { return threadIdx.x == 0; }
+  __device__ __forceinline__ void fence() const { __threadfence(); }
+  __device__ __forceinline__ uint32_t look(uint32_t* c) const { return *reinterpret_cast<volatile uint32_t*>(c); }
+  __device__ __forceinline__ uint32_t add(uint32_t* c) const { return atomicAdd(c, 1u); }
+  __device__ __forceinline__ void zero(uint32_t* c) const { *c = 0u; }
+  __device__ __forceinline__ void tell(AttnWord w, bool x) const { words[w] = x; }
+  __device__ __forceinline__ bool told(AttnWord w) const { return words[w] != 0; }
+};
 
 }  // namespace trident

@@ -1,0 +1,56 @@
+// attn_count.h -- how the blocks that share a unit of paged attention agree on which one joins its parts.
+//
+// The steps are templates over what a block can do, so that a host program can run them under every order of
+// its threads (tests/count_probe.cpp). Block has
+//   sync()            a barrier of all its threads
+//   leader()          is this thread the one that counts?
+//   fence()           this thread's writes before, and its reads after, in order for the whole GPU
+//   look(c), add(c)   the unit's counter: read, and read and raised by one; zero(c): put back to zero
+//   tell(w, x), told(w)   one of the words (AttnWord) that the block's threads share
+// A word is told by the leader and read behind the next barrier. Each question has a word of its own: between
+// its last read and its next writing there is then always another barrier, and a thread that is late to read
+// an answer cannot find the next one in its place.
+#pragma once
+#include <cstdint>
+
+#ifdef __CUDACC__
+#define TRIDENT_HD __host__ __device__ __forceinline__
+#else
+#define TRIDENT_HD inline
+#endif
+
+namespace trident {
+
+enum AttnWord : int { ATTN_LAST, ATTN_DONE, kAttnAnswers };
+
+// Have all other parts of the unit been counted, so that this one need not be written out? True in every
+// thread; the block then joins them and zeroes the counter. Asked of a unit that goes on past the block's run,
+// so at most once by a block.
+template <class Block, class Counter>
+TRIDENT_HD bool attn_is_last(Block& b, Counter counter, uint32_t total) {
+  if (b.leader()) b.tell(ATTN_LAST, b.look(counter) + 1 == total);
+  b.sync();
+  const bool last = b.told(ATTN_LAST);
+  if (last) b.fence();
+  return last;
+}
+
+// Counts a part that has been written out; true in every thread of the block that completes `total` of them,
+// which also puts the counter back to zero. What the parts' blocks wrote before is visible to it.
+template <class Block, class Counter>
+TRIDENT_HD bool attn_completes(Block& b, Counter counter, uint32_t total) {
+  b.sync();
+  if (b.leader()) {  // behind the barrier the leader's fences stand for the block: they are cumulative
+    b.fence();
+    const bool last = b.add(counter) + 1 == total;
+    if (last) {
+      b.zero(counter);
+      b.fence();
+    }
+    b.tell(ATTN_DONE, last);
+  }
+  b.sync();
+  return b.told(ATTN_DONE);
+}
+
+}  // namespace trident

@@ -110,7 +110,7 @@ struct RowsKernel {
     alignas(16) float part[4][G::PASS][G::LDO];
     typename Split::Smem split;
     float m[4][16], l[4][16];
-    int last;
+    volatile int words[kAttnAnswers];
   };
 
   // The table's entry for the lane's row (lane mod WARP) of the keys from j0 on. It is asked for a stage
@@ -486,21 +486,15 @@ struct RowsKernel {
     auto in_group = [&](int i) { return slot(g0 + i); };
     // A unit that goes on past this block's run: the blocks after this one began with it, so they mostly are
     // done, and this part is joined with theirs without a turn through the workspace.
-    bool last = false;
-    if (u.last > blockIdx.x && groups == 1) {
-      if (threadIdx.x == 0) s.last = *reinterpret_cast<volatile uint32_t*>(counter) + 1 == (uint32_t)size;
-      __syncthreads();
-      last = s.last != 0;
-      if (last) __threadfence();
-    }
+    const AttnBlock<0, kRowsThreads> block{s.words};
+    const bool last = u.last > blockIdx.x && groups == 1 && attn_is_last(block, counter, (uint32_t)size);
     const bool done = cut.whole() || last;
     join_warps(p, s, u, m, l, o, done ? nullptr : slot(blockIdx.x), last ? size : 0, f, in_group);
-    if (last && threadIdx.x == 0) *counter = 0u;
+    if (last && block.leader()) block.zero(counter);
     if (done) return;
-    if (attn_completes<0, kRowsThreads>(&s.last, threadIdx.x == 0, counter, size)) {
+    if (attn_completes(block, counter, (uint32_t)size)) {
       join_slots(p, s, u, size, in_group, groups > 1 ? slot(g0) : nullptr);
-      if (groups > 1 && attn_completes<0, kRowsThreads>(&s.last, threadIdx.x == 0,
-                                                        counters + 2 * gridDim.x + cut.slot(cut.first), groups))
+      if (groups > 1 && attn_completes(block, counters + 2 * gridDim.x + cut.slot(cut.first), (uint32_t)groups))
         join_slots(p, s, u, groups, [&](int i) { return slot(cut.first + (int64_t)i * kFanIn); }, nullptr);
     }
   }

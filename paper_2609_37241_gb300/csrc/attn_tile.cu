@@ -224,7 +224,7 @@ struct Tile {
     alignas(1024) char ring[SLOTS * KB];
     alignas(8) uint64_t full[SLOTS], empty[SLOTS], raw, q_full[NT], s_full[NT], p_half[NT], p_full[NT], o_full[NT], drain;
     uint32_t tmem;
-    volatile int abort, flag;
+    volatile int abort, words[kAttnAnswers];
     int count;
     long long x;
     Frag frag[kFrags];
@@ -674,7 +674,7 @@ struct Tile {
     auto slot = [&](int64_t block) { return slots + cut.slot(block) * SLOT; };
     auto in_group = [&](int i) { return slot(g0 + i); };
     uint32_t* counter = counters + cut.slot(g0);
-    const bool leader = threadIdx.x == 0, used = x == 0 || f.rows > 128;
+    const bool used = x == 0 || f.rows > 128;
     float m = -INFINITY, l = 0.f;
     if (used) {
       if (ok && !st.q_ready) load_q(p, s, f, x);
@@ -685,27 +685,19 @@ struct Tile {
     }
     // A unit that goes on past this block's run: the blocks after this one began with it, so they mostly are
     // done. Then this one's part is the last and is joined from TMEM without a turn through the workspace.
-    if (f.last > blockIdx.x && groups == 1) {
-      if (leader) s.flag = !s.abort && *reinterpret_cast<volatile uint32_t*>(counter) + 1 == (uint32_t)size;
-      attn_sync<1, SOFT>();
-      const bool last = s.flag != 0;
-      attn_sync<1, SOFT>();
-      if (last) {
-        __threadfence();
-        if (used && ok) join<true>(p, tmem, f, x, size, in_group, nullptr, i0, m, l);
-        if (leader) *counter = 0u;
-        return ok;
-      }
+    // With a block that failed the count is never met, so nobody joins the unit.
+    const AttnBlock<1, SOFT> block{s.words};
+    auto total = [&](int n) { return s.abort ? 0xffffffffu : (uint32_t)n; };
+    if (f.last > blockIdx.x && groups == 1 && attn_is_last(block, counter, total(size))) {
+      if (used && ok) join<true>(p, tmem, f, x, size, in_group, nullptr, i0, m, l);
+      if (block.leader()) block.zero(counter);
+      return ok;
     }
     if (used && ok) finish(p, tmem, f, x, m, l, mine);
     if (cut.whole()) return ok;
-    // with a block that failed the count is never met, so nobody joins the unit
-    auto done = [&](uint32_t* counter, uint32_t total) {
-      return attn_completes<1, SOFT>(&s.flag, leader, counter, s.abort ? 0xffffffffu : total);
-    };
-    if (done(counter, size)) {
+    if (attn_completes(block, counter, total(size))) {
       if (used) join<false>(p, tmem, f, x, size, in_group, groups > 1 ? slot(g0) : nullptr, -1, 0.f, 0.f);
-      if (groups > 1 && done(counters + 2 * gridDim.x + cut.slot(cut.first), groups) && used)
+      if (groups > 1 && attn_completes(block, counters + 2 * gridDim.x + cut.slot(cut.first), total(groups)) && used)
         join<false>(p, tmem, f, x, groups, [&](int i) { return slot(cut.first + (int64_t)i * kFanIn); }, nullptr, -1, 0.f, 0.f);
     }
     return ok;

@@ -1,0 +1,249 @@
+// count_probe.cpp -- runs the steps of csrc/attn_count.h on the host, under random orders of the threads.
+//
+//   count_probe NAME RUNS    prints "ok" or what went wrong first, with its run
+//
+// Threads are contexts of one process. Each gives way before every step that another thread can see, and the
+// next one to go on is drawn. Values are seen at once; what a thread may rely on of another block's data is
+// tracked apart from that, as a set of (block, thread) whose writes are known to come before:
+//   fence     what the thread's earlier reads of a counter brought becomes known; its later counts bring what
+//             it knows now
+//   sync      the block's threads know what any of them knew
+// NAME "rows" and "tile": units that cuts go through, the parts written, counted and joined as the kernels of
+// few and of many rows do (of few rows: with block barriers between a part's end and its join).
+// "rows-one-word", "tile-one-word": both answers in one shared word, to show that the orders drawn here find it.
+#include <ucontext.h>
+
+#include <cstdint>
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+#include <functional>
+#include <random>
+#include <string>
+#include <vector>
+
+#include "attn_count.h"
+
+namespace {
+
+constexpr int kBlocks = 4, kThreads = 3;
+
+struct Thread;
+struct World {
+  std::mt19937 rng;
+  ucontext_t home;
+  std::vector<Thread*> threads;
+  std::string fault;
+  void fail(const std::string& what) {
+    if (fault.empty()) fault = what;
+  }
+};
+
+using Set = uint64_t;  // bit unit * 16 + block * kThreads + thread
+inline Set bit(int unit, int block, int thread) { return 1ull << (unit * 16 + block * kThreads + thread); }
+inline Set bits_of(int unit, int block) {
+  Set s = 0;
+  for (int t = 0; t < kThreads; ++t) s |= bit(unit, block, t);
+  return s;
+}
+
+struct Counter {
+  uint32_t value = 0;
+  Set brings = 0;
+};
+
+struct Group {  // a block: its barrier and its shared words
+  int arrived = 0, round = 0;
+  Set known = 0;
+  int words[trident::kAttnAnswers] = {};
+};
+
+struct Thread {
+  World* w;
+  ucontext_t at;
+  std::vector<char> stack;
+  Group* group = nullptr;
+  int block = 0, index = 0;
+  bool ended = false;
+  int waits = -1;  // the barrier round that it waits for, or -1
+  Set seen = 0, known = 0, fenced = 0;
+  std::function<void(Thread&)> body;
+  std::vector<int> answers;
+
+  void give_way() { swapcontext(&at, &w->home); }
+  bool runs() const { return !ended && (waits < 0 || group->round > waits); }
+};
+
+Thread* g_current;
+void enter() {
+  Thread* t = g_current;
+  t->body(*t);
+  t->ended = true;
+  swapcontext(&t->at, &t->w->home);
+}
+
+// What attn_count.h asks of a block. kOneWord: both answers in one word.
+template <bool kOneWord>
+struct Block {
+  Thread& t;
+  void sync() {
+    t.give_way();
+    Group& g = *t.group;
+    g.known |= t.known;
+    if (++g.arrived == kThreads) {
+      g.arrived = 0;
+      ++g.round;
+      for (Thread* o : t.w->threads)
+        if (o->group == &g) o->known |= g.known;
+    } else {
+      t.waits = g.round;
+      t.give_way();
+      t.waits = -1;
+    }
+  }
+  bool leader() const { return t.index == 0; }
+  void fence() {
+    t.give_way();
+    t.known |= t.seen;
+    t.fenced = t.known;
+  }
+  uint32_t look(Counter* c) {
+    t.give_way();
+    t.seen |= c->brings;
+    return c->value;
+  }
+  uint32_t add(Counter* c) {
+    t.give_way();
+    c->brings |= t.fenced;
+    t.seen |= c->brings;
+    return c->value++;
+  }
+  void zero(Counter* c) {
+    t.give_way();
+    c->value = 0;
+  }
+  void tell(trident::AttnWord w, bool x) {
+    t.give_way();
+    t.group->words[kOneWord ? 0 : w] = x;
+  }
+  bool told(trident::AttnWord w) {
+    t.give_way();
+    const bool x = t.group->words[kOneWord ? 0 : w] != 0;
+    t.answers.push_back(2 * w + x);
+    return x;
+  }
+};
+
+struct Unit {
+  Counter counter;
+  int total = 0, joins = 0;
+  Set parts = 0;  // of all blocks
+};
+
+// One part of a unit, as the kernels end it.
+template <class B>
+void part(B& b, Unit& u, int unit, bool goes_on, bool rows) {
+  Thread& t = b.t;
+  auto join = [&](Set others) {
+    if ((t.known & others) != others) t.w->fail("a part is read that is not known to be written");
+    if (b.leader()) ++u.joins;
+  };
+  const Set own = bits_of(unit, t.block);
+  const bool last = goes_on && trident::attn_is_last(b, &u.counter, (uint32_t)u.total);
+  if (rows) {  // the warps' join
+    b.sync();
+    b.sync();
+  }
+  if (!last) t.known |= bit(unit, t.block, t.index);  // written
+  if (last) {
+    join(u.parts & ~own);
+    if (b.leader()) b.zero(&u.counter);
+    return;
+  }
+  if (trident::attn_completes(b, &u.counter, (uint32_t)u.total)) join(u.parts);
+}
+
+std::string run(World& w, std::vector<Thread>& threads) {
+  for (Thread& t : threads) {
+    t.w = &w;
+    t.stack.resize(64 << 10);
+    getcontext(&t.at);
+    t.at.uc_stack.ss_sp = t.stack.data();
+    t.at.uc_stack.ss_size = t.stack.size();
+    t.at.uc_link = &w.home;
+    makecontext(&t.at, enter, 0);
+    w.threads.push_back(&t);
+  }
+  while (w.fault.empty()) {
+    std::vector<Thread*> can;
+    bool all = true;
+    for (Thread& t : threads) {
+      all &= t.ended;
+      if (t.runs()) can.push_back(&t);
+    }
+    if (all) break;
+    if (can.empty()) {
+      w.fail("threads of a block wait at different barriers");
+      break;
+    }
+    // a few steps of one thread in a row are as likely as turns: late threads are what matters
+    Thread* t = can[w.rng() % can.size()];
+    const int steps = 1 + (int)(w.rng() % 6);
+    for (int i = 0; i < steps && t->runs() && w.fault.empty(); ++i) {
+      g_current = t;
+      swapcontext(&w.home, &t->at);
+    }
+  }
+  for (Thread& t : threads)
+    for (Thread& o : threads)
+      if (w.fault.empty() && t.group == o.group && t.answers != o.answers) w.fail("threads of a block differ in an answer");
+  return w.fault;
+}
+
+// Block b's run goes from within unit b - 1 to within unit b (the first and the last run: one unit only).
+template <bool kOneWord>
+std::string parts(uint32_t seed, bool rows) {
+  World w;
+  w.rng.seed(seed);
+  std::vector<Group> groups(kBlocks);
+  Unit units[kBlocks - 1];
+  for (int u = 0; u + 1 < kBlocks; ++u) {
+    units[u].total = 2;
+    units[u].parts = bits_of(u, u) | bits_of(u, u + 1);
+  }
+  std::vector<Thread> threads(kBlocks * kThreads);
+  for (int i = 0; i < kBlocks * kThreads; ++i) {
+    Thread& t = threads[i];
+    t.block = i / kThreads;
+    t.index = i % kThreads;
+    t.group = &groups[t.block];
+    t.body = [&units, rows](Thread& t) {
+      Block<kOneWord> b{t};
+      if (t.block > 0) part(b, units[t.block - 1], t.block - 1, false, rows);
+      if (t.block + 1 < kBlocks) part(b, units[t.block], t.block, true, rows);
+    };
+  }
+  std::string fault = run(w, threads);
+  for (Unit& u : units)
+    if (fault.empty() && (u.joins != 1 || u.counter.value != 0)) fault = "a unit is not joined once, or its counter not zero after";
+  return fault;
+}
+
+}  // namespace
+
+int main(int argc, char** argv) {
+  if (argc != 3) return 2;
+  const std::string name = argv[1];
+  for (int i = 0; i < std::atoi(argv[2]); ++i) {
+    std::string fault;
+    if (name == "rows" || name == "tile") fault = parts<false>(i, name == "rows");
+    else if (name == "rows-one-word" || name == "tile-one-word") fault = parts<true>(i, name == "rows-one-word");
+    else return 2;
+    if (!fault.empty()) {
+      std::printf("run %d: %s\n", i, fault.c_str());
+      return 0;
+    }
+  }
+  std::puts("ok");
+  return 0;
+}
