@@ -28,11 +28,13 @@ enum AttnWord : int { ATTN_LAST, ATTN_DONE, kAttnAnswers };
 // so at most once by a block.
 template <class Block, class Counter>
 TRIDENT_HD bool attn_is_last(Block& b, Counter counter, uint32_t total) {
-  if (b.leader()) b.tell(ATTN_LAST, b.look(counter) + 1 == total);
+  if (b.leader()) {  // its fence stands for the block, behind the barrier: the others have not read the counter
+    const bool last = b.look(counter) + 1 == total;
+    if (last) b.fence();
+    b.tell(ATTN_LAST, last);
+  }
   b.sync();
-  const bool last = b.told(ATTN_LAST);
-  if (last) b.fence();
-  return last;
+  return b.told(ATTN_LAST);
 }
 
 // Counts a part that has been written out; true in every thread of the block that completes `total` of them,

@@ -24,6 +24,11 @@ def test_parts_of_few_rows_are_joined_once(probe):
     assert probe("rows") == "ok"
 
 
+def test_parts_of_many_rows_are_joined_once(probe):
+    """Without block barriers before the join: what the other blocks wrote has to be known by then."""
+    assert probe("tile") == "ok"
+
+
 def test_one_word_for_two_answers_is_found(probe):
     """A thread that reads the first answer late finds the second one in its place."""
     assert probe("rows-one-word") != "ok"
