@@ -249,36 +249,23 @@ struct AttnCuts {
   __device__ __forceinline__ int64_t slot(int64_t block) const { return block == first ? 2 * block + 1 : 2 * block; }
 };
 
-// Where both kernels run, the one of few rows comes first and the tile kernel's blocks start as its blocks
-// leave the SMs, not when all of it is done: the two write different rows and use different parts of the
-// workspace, so the tile kernel only needs what came before both. The first one's block 0 has waited for
-// that (griddepcontrol.wait) and looked the requests over when it stores the word p.start (release), and no
-// block of the second starts before block 0 has let it (the trigger comes after the store); the second
-// acquires the word and goes on, with its later loads behind that -- its TMA loads by a proxy fence -- or, if
-// it should read 0, waits for the whole first kernel. The word is 0 again when the second ends, which is not
-// before the first has (it waits for it last).
-enum : uint32_t { ATTN_START_NONE = 1, ATTN_START_SOME = 2 };  // no request is left to the tile kernel, or some
-
-__device__ __forceinline__ void attn_lets_start(const PagedAttnParams& p, bool others) {
-  if (blockIdx.x == 0 && threadIdx.x == 0)
-    asm volatile("st.release.gpu.global.u32 [%0], %1;" :: "l"(p.start), "r"(others ? ATTN_START_SOME : ATTN_START_NONE) : "memory");
-  __syncthreads();
-  pdl_trigger();
-}
-__device__ __forceinline__ bool attn_starts(const PagedAttnParams& p) {
-  uint32_t word = 0;
-  if (threadIdx.x == 0) asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(word) : "l"(p.start) : "memory");
-  if (!__syncthreads_or(word != 0)) {
-    pdl_wait();
-    word = __ldcg(p.start);
+// A block of either kernel as attn_count.h's start word sees it.
+struct AttnStartBlock {
+  uint32_t* word;
+  __device__ __forceinline__ void sync() const { __syncthreads(); }
+  __device__ __forceinline__ bool any(bool x) const { return __syncthreads_or(x) != 0; }
+  __device__ __forceinline__ bool leader() const { return threadIdx.x == 0; }
+  __device__ __forceinline__ bool first() const { return blockIdx.x == 0; }
+  __device__ __forceinline__ void wait_before() const { pdl_wait(); }
+  __device__ __forceinline__ uint32_t start_word() const {
+    uint32_t x;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(x) : "l"(word) : "memory");
+    return x;
   }
-  asm volatile("fence.proxy.async.global;" ::: "memory");
-  return __syncthreads_or(word == ATTN_START_SOME) != 0;
-}
-__device__ __forceinline__ void attn_ends(const PagedAttnParams& p) {
-  pdl_wait();
-  if (blockIdx.x == 0 && threadIdx.x == 0) *p.start = 0u;
-}
+  __device__ __forceinline__ void set_start_word(uint32_t x) const {
+    asm volatile("st.release.gpu.global.u32 [%0], %1;" :: "l"(word), "r"(x) : "memory");
+  }
+};
 
 // The block as attn_count.h sees it: NT threads at named barrier BAR, their words in shared memory.
 template <int BAR, int NT>

@@ -501,7 +501,11 @@ struct RowsKernel {
 
   static __device__ __forceinline__ void run(const PagedAttnParams& p, Smem& s) {
     const AttnShare a = Split::share(p, s.split);
-    if (p.part == ATTN_FEW) attn_lets_start(p, a.others);
+    if (p.part == ATTN_FEW) {
+      const AttnStartBlock block{p.start};
+      attn_sets_start(block, a.others);
+      pdl_trigger();
+    }
     bool bad = false;
     int64_t run = 0, x = a.lo;
     for (int64_t b0 = 0; b0 < p.B && x < a.hi; b0 += kRowsThreads) {

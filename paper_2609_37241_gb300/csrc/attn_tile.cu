@@ -816,8 +816,13 @@ struct Tile {
     }
     pdl_trigger();
     bool work = true;
-    if (p.part == ATTN_ALL) pdl_wait();
-    else work = attn_starts(p);
+    const AttnStartBlock start{p.start};
+    if (p.part == ATTN_ALL) {
+      pdl_wait();
+    } else {
+      work = attn_starts(start);
+      asm volatile("fence.proxy.async.global;" ::: "memory");  // the TMA loads, behind what the word or the wait brought
+    }
     __syncthreads();
     tc_after();
     const uint32_t tmem = s.tmem;
@@ -844,7 +849,7 @@ struct Tile {
       });
     }
     if (p.part == ATTN_ALL) attn_fill_tail<THREADS>(p);
-    else attn_ends(p);
+    else attn_ends(start);
     // the way out: every copy and product of the block has to be done before its memory is given back
     if (warp >= LOAD_WARP && warp < LOAD_WARP + 2) {
       for (uint32_t i = ld.tiles > KS ? ld.tiles - KS : 0; i < ld.tiles; ++i) {

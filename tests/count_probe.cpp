@@ -11,6 +11,8 @@
 // NAME "rows" and "tile": units that cuts go through, the parts written, counted and joined as the kernels of
 // few and of many rows do (of few rows: with block barriers between a part's end and its join).
 // "rows-one-word", "tile-one-word": both answers in one shared word, to show that the orders drawn here find it.
+// "start": a first kernel's blocks and a second one's, which may start at any time after all of the first have
+// let them. "start-reads-again": a block that finds the word unset reads it again after its wait, and goes by that.
 #include <ucontext.h>
 
 #include <cstdint>
@@ -56,6 +58,7 @@ struct Group {  // a block: its barrier and its shared words
   int arrived = 0, round = 0;
   Set known = 0;
   int words[trident::kAttnAnswers] = {};
+  bool ors[8] = {};  // any(), by the round
 };
 
 struct Thread {
@@ -66,12 +69,13 @@ struct Thread {
   int block = 0, index = 0;
   bool ended = false;
   int waits = -1;  // the barrier round that it waits for, or -1
+  std::function<bool()> gate;  // what else it waits for
   Set seen = 0, known = 0, fenced = 0;
   std::function<void(Thread&)> body;
   std::vector<int> answers;
 
   void give_way() { swapcontext(&at, &w->home); }
-  bool runs() const { return !ended && (waits < 0 || group->round > waits); }
+  bool runs() const { return !ended && (waits < 0 || group->round > waits) && (!gate || gate()); }
 };
 
 Thread* g_current;
@@ -229,6 +233,95 @@ std::string parts(uint32_t seed, bool rows) {
   return fault;
 }
 
+constexpr Set kBefore = 1ull << 63;  // what the launches before both kernels wrote
+
+// One thread of a block of either kernel; kernel 0 runs first.
+struct Kernels {
+  uint32_t word = 0;
+  bool word_brings = false;  // the word was stored by a thread that knew what came before
+  int let = 0, ended[2] = {};
+};
+struct StartBlock {
+  Thread& t;
+  Kernels& k;
+  int kernel;
+  void sync() { any(false); }
+  bool any(bool x) {
+    bool& of_round = t.group->ors[t.group->round];
+    of_round |= x;
+    Block<false>{t}.sync();
+    return of_round;
+  }
+  bool leader() const { return t.index == 0; }
+  bool first() const { return t.block == 0; }
+  void wait_before() {
+    if (kernel == 1) {
+      t.gate = [this] { return k.ended[0] == kBlocks * kThreads; };
+      t.give_way();
+      t.gate = nullptr;
+    }
+    t.known |= kBefore;
+  }
+  uint32_t start_word() {
+    t.give_way();
+    if (k.word_brings) t.known |= kBefore;
+    return k.word;
+  }
+  void set_start_word(uint32_t x) {
+    t.give_way();
+    k.word = x;
+    k.word_brings = (t.known & kBefore) != 0;
+  }
+};
+
+// As it was: the word again after the wait.
+bool starts_reads_again(StartBlock& b) {
+  uint32_t word = b.leader() ? b.start_word() : 0u;
+  if (!b.any(word != 0)) {
+    b.wait_before();
+    word = b.start_word();
+  }
+  return b.any(word == trident::ATTN_START_SOME);
+}
+
+std::string start(uint32_t seed, bool reads_again) {
+  World w;
+  w.rng.seed(seed);
+  const bool some = w.rng() % 2 != 0;
+  std::vector<Group> groups(2 * kBlocks);
+  std::vector<Thread> threads(2 * kBlocks * kThreads);
+  Kernels k;
+  int works = 0;
+  for (int i = 0; i < 2 * kBlocks * kThreads; ++i) {
+    Thread& t = threads[i];
+    const int kernel = i / (kBlocks * kThreads);
+    t.block = i / kThreads % kBlocks;
+    t.index = i % kThreads;
+    t.group = &groups[i / kThreads];
+    if (kernel == 1) t.gate = [&k] { return k.let == kBlocks * kThreads; };
+    t.body = [&, kernel](Thread& t) {
+      StartBlock b{t, k, kernel};
+      if (kernel == 0) {
+        b.wait_before();
+        trident::attn_sets_start(b, some);
+        ++k.let;
+      } else {
+        t.gate = nullptr;
+        const bool work = reads_again ? starts_reads_again(b) : trident::attn_starts(b);
+        t.answers.push_back(work);
+        works += work;
+        if (some && !work) t.w->fail("a block of the second kernel skips its share");
+        if (work && !(t.known & kBefore)) t.w->fail("a block goes on without what came before");
+        trident::attn_ends(b);
+      }
+      ++k.ended[kernel];
+    };
+  }
+  std::string fault = run(w, threads);
+  if (fault.empty() && k.word != 0) fault = "the word is not 0 after";
+  return fault;
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
@@ -238,6 +331,7 @@ int main(int argc, char** argv) {
     std::string fault;
     if (name == "rows" || name == "tile") fault = parts<false>(i, name == "rows");
     else if (name == "rows-one-word" || name == "tile-one-word") fault = parts<true>(i, name == "rows-one-word");
+    else if (name == "start" || name == "start-reads-again") fault = start(i, name != "start");
     else return 2;
     if (!fault.empty()) {
       std::printf("run %d: %s\n", i, fault.c_str());

@@ -32,3 +32,9 @@ def test_parts_of_many_rows_are_joined_once(probe):
 def test_one_word_for_two_answers_is_found(probe):
     """A thread that reads the first answer late finds the second one in its place."""
     assert probe("rows-one-word") != "ok"
+
+
+def test_a_block_that_starts_late_takes_its_share(probe):
+    """The second kernel's blocks, started before and after its block 0 has put the start word back."""
+    assert probe("start") == "ok"
+    assert probe("start-reads-again") != "ok"  # the form that goes by the word it reads after the wait

@@ -75,3 +75,41 @@ def test_cut_units_many_times(S, new, kv, Hq, Hkv, D):
     assert differ.item() == 0
     assert S.trident_scm_device_status(s.h, stream())[1] == 0
     s.close()
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_both_kernels_while_another_stream_holds_the_sms(S, D):
+    """A call that launches both kernels, the tile kernel's work cut over every block, beside long chunks of a
+    second stream, at several distances in time: the second kernel's blocks start when those leave the SMs,
+    some after the others have ended. Then the same call alone on the same workspace."""
+    ps, Hq, Hkv, scale = 16, 32, 8, 1.0 / D ** 0.5
+    s = S.Scm(flags=S.OPT_PDL)
+    index = s.register(S.make_spec(S.OP_PAGED_ATTN, S.BF16, [Hq, Hkv, D, ps], 1, 1 << 20, layout=S.LAYOUT_ANY))
+    new, kv = [1, 64, 1, 64, 1], [700, 9728, 3000, 9728, 33]
+    g = np.random.default_rng(9)
+    b = R.batch(g, new, kv, Hq, Hkv, D, ps, S.BF16)
+    long = R.batch(g, [2048], [8192], Hq, Hkv, D, ps, S.BF16)
+    work, long_work = (torch.zeros(s.workspace(index), device="cuda") for _ in range(2))
+    call(S, s, index, b, work, scale)
+    check(b, reference(b, Hq, Hkv, ps, scale), S.BF16, max(kv))
+    call(S, s, index, long, long_work, scale)
+    alone, long_alone = (b["out"].clone(), b["lse"].clone()), long["out"].clone()
+    side, main = torch.cuda.Stream(), torch.cuda.current_stream()
+    for trial in range(48):
+        for x in (b["out"], b["lse"], long["out"]):
+            x.fill_(float("nan"))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(6):
+                call(S, s, index, long, long_work, scale)
+        torch.cuda._sleep(1 + trial * 30000)  # one thread, up to 0.7 ms
+        for _ in range(3):
+            call(S, s, index, b, work, scale)
+        torch.cuda.synchronize()
+        assert torch.equal(b["out"], alone[0]) and torch.equal(b["lse"], alone[1]), trial
+        assert torch.equal(long["out"], long_alone), trial
+        b["out"].fill_(float("nan"))
+        call(S, s, index, b, work, scale)
+        assert torch.equal(b["out"], alone[0]), trial
+        assert S.trident_scm_device_status(s.h, main.cuda_stream)[1] == 0
+    s.close()
