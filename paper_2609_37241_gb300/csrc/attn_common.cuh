@@ -274,13 +274,15 @@ __device__ __forceinline__ void attn_sync() {
 }
 template <int BAR, int NT>
 struct AttnBlock {
-  volatile int* words;  // kAttnAnswers of them
+  volatile int* words;          // kAttnAnswers of them
+  const volatile int* abort;    // set where a wait ran out; NULL: a kernel that waits for nothing
   __device__ __forceinline__ void sync() const { attn_sync<BAR, NT>(); }
   __device__ __forceinline__ bool leader() const { return threadIdx.x == 0; }
   __device__ __forceinline__ void fence() const { __threadfence(); }
   __device__ __forceinline__ uint32_t look(uint32_t* c) const { return *reinterpret_cast<volatile uint32_t*>(c); }
   __device__ __forceinline__ uint32_t add(uint32_t* c) const { return atomicAdd(c, 1u); }
   __device__ __forceinline__ void zero(uint32_t* c) const { *c = 0u; }
+  __device__ __forceinline__ bool failed() const { return abort && *abort != 0; }
   __device__ __forceinline__ void tell(AttnWord w, bool x) const { words[w] = x; }
   __device__ __forceinline__ bool told(AttnWord w) const { return words[w] != 0; }
 };

@@ -7,6 +7,7 @@
 //   leader()          is this thread the one that counts?
 //   fence()           this thread's writes before, and its reads after, in order for the whole GPU
 //   look(c), add(c)   the unit's counter: read, and read and raised by one; zero(c): put back to zero
+//   failed()          has a wait of this block run out? A thread says so before its next barrier
 //   tell(w, x), told(w)   one of the words (AttnWord) that the block's threads share
 // A word is told by the leader and read behind the next barrier. Each question has a word of its own: between
 // its last read and its next writing there is then always another barrier, and a thread that is late to read
@@ -30,7 +31,7 @@ enum AttnWord : int { ATTN_LAST, ATTN_DONE, kAttnAnswers };
 template <class Block, class Counter>
 TRIDENT_HD bool attn_is_last(Block& b, Counter counter, uint32_t total) {
   if (b.leader()) {  // its fence stands for the block, behind the barrier: the others have not read the counter
-    const bool last = b.look(counter) + 1 == total;
+    const bool last = b.look(counter) + 1 == total && !b.failed();
     if (last) b.fence();
     b.tell(ATTN_LAST, last);
   }
@@ -39,16 +40,20 @@ TRIDENT_HD bool attn_is_last(Block& b, Counter counter, uint32_t total) {
 }
 
 // Counts a part that has been written out; true in every thread of the block that completes `total` of them,
-// which also puts the counter back to zero. What the parts' blocks wrote before is visible to it.
+// which also puts the counter back to zero. What the parts' blocks wrote before is visible to it. A block that
+// failed, whose part may be missing, does not count, so that nobody joins the unit.
 template <class Block, class Counter>
 TRIDENT_HD bool attn_completes(Block& b, Counter counter, uint32_t total) {
   b.sync();
   if (b.leader()) {  // behind the barrier the leader's fences stand for the block: they are cumulative
-    b.fence();
-    const bool last = b.add(counter) + 1 == total;
-    if (last) {
-      b.zero(counter);
+    bool last = false;
+    if (!b.failed()) {
       b.fence();
+      last = b.add(counter) + 1 == total;
+      if (last) {
+        b.zero(counter);
+        b.fence();
+      }
     }
     b.tell(ATTN_DONE, last);
   }

@@ -486,7 +486,7 @@ struct RowsKernel {
     auto in_group = [&](int i) { return slot(g0 + i); };
     // A unit that goes on past this block's run: the blocks after this one began with it, so they mostly are
     // done, and this part is joined with theirs without a turn through the workspace.
-    const AttnBlock<0, kRowsThreads> block{s.words};
+    const AttnBlock<0, kRowsThreads> block{s.words, nullptr};
     const bool last = u.last > blockIdx.x && groups == 1 && attn_is_last(block, counter, (uint32_t)size);
     const bool done = cut.whole() || last;
     join_warps(p, s, u, m, l, o, done ? nullptr : slot(blockIdx.x), last ? size : 0, f, in_group);

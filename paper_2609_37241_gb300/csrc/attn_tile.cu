@@ -685,19 +685,17 @@ struct Tile {
     }
     // A unit that goes on past this block's run: the blocks after this one began with it, so they mostly are
     // done. Then this one's part is the last and is joined from TMEM without a turn through the workspace.
-    // With a block that failed the count is never met, so nobody joins the unit.
-    const AttnBlock<1, SOFT> block{s.words};
-    auto total = [&](int n) { return s.abort ? 0xffffffffu : (uint32_t)n; };
-    if (f.last > blockIdx.x && groups == 1 && attn_is_last(block, counter, total(size))) {
+    const AttnBlock<1, SOFT> block{s.words, &s.abort};
+    if (f.last > blockIdx.x && groups == 1 && attn_is_last(block, counter, (uint32_t)size)) {
       if (used && ok) join<true>(p, tmem, f, x, size, in_group, nullptr, i0, m, l);
       if (block.leader()) block.zero(counter);
       return ok;
     }
     if (used && ok) finish(p, tmem, f, x, m, l, mine);
     if (cut.whole()) return ok;
-    if (attn_completes(block, counter, total(size))) {
+    if (attn_completes(block, counter, (uint32_t)size)) {
       if (used) join<false>(p, tmem, f, x, size, in_group, groups > 1 ? slot(g0) : nullptr, -1, 0.f, 0.f);
-      if (groups > 1 && attn_completes(block, counters + 2 * gridDim.x + cut.slot(cut.first), total(groups)) && used)
+      if (groups > 1 && attn_completes(block, counters + 2 * gridDim.x + cut.slot(cut.first), (uint32_t)groups) && used)
         join<false>(p, tmem, f, x, groups, [&](int i) { return slot(cut.first + (int64_t)i * kFanIn); }, nullptr, -1, 0.f, 0.f);
     }
     return ok;

@@ -11,6 +11,8 @@
 // NAME "rows" and "tile": units that cuts go through, the parts written, counted and joined as the kernels of
 // few and of many rows do (of few rows: with block barriers between a part's end and its join).
 // "rows-one-word", "tile-one-word": both answers in one shared word, to show that the orders drawn here find it.
+// "tile-failed": as "tile"; a thread of one block fails and does not write its part. "tile-failed-counts": the
+// block counts all the same, without completing the count itself.
 // "start": a first kernel's blocks and a second one's, which may start at any time after all of the first have
 // let them. "start-reads-again": a block that finds the word unset reads it again after its wait, and goes by that.
 #include <ucontext.h>
@@ -58,6 +60,7 @@ struct Group {  // a block: its barrier and its shared words
   int arrived = 0, round = 0;
   Set known = 0;
   int words[trident::kAttnAnswers] = {};
+  bool failed = false;
   bool ors[8] = {};  // any(), by the round
 };
 
@@ -67,6 +70,7 @@ struct Thread {
   std::vector<char> stack;
   Group* group = nullptr;
   int block = 0, index = 0;
+  int fails = -1;  // the unit whose part it does not write
   bool ended = false;
   int waits = -1;  // the barrier round that it waits for, or -1
   std::function<bool()> gate;  // what else it waits for
@@ -126,6 +130,10 @@ struct Block {
     t.give_way();
     c->value = 0;
   }
+  bool failed() {
+    t.give_way();
+    return t.group->failed;
+  }
   void tell(trident::AttnWord w, bool x) {
     t.give_way();
     t.group->words[kOneWord ? 0 : w] = x;
@@ -141,14 +149,17 @@ struct Block {
 struct Unit {
   Counter counter;
   int total = 0, joins = 0;
-  Set parts = 0;  // of all blocks
+  Set parts = 0;  // of all blocks' threads
 };
 
 // One part of a unit, as the kernels end it.
-template <class B>
+template <bool kCountsFailed, class B>
 void part(B& b, Unit& u, int unit, bool goes_on, bool rows) {
   Thread& t = b.t;
+  const bool ok = t.fails < 0 || unit < t.fails;
+  if (t.fails == unit) t.group->failed = true;
   auto join = [&](Set others) {
+    if (!ok) return;
     if ((t.known & others) != others) t.w->fail("a part is read that is not known to be written");
     if (b.leader()) ++u.joins;
   };
@@ -158,10 +169,16 @@ void part(B& b, Unit& u, int unit, bool goes_on, bool rows) {
     b.sync();
     b.sync();
   }
-  if (!last) t.known |= bit(unit, t.block, t.index);  // written
+  if (!last && ok) t.known |= bit(unit, t.block, t.index);  // written
   if (last) {
     join(u.parts & ~own);
     if (b.leader()) b.zero(&u.counter);
+    return;
+  }
+  if (kCountsFailed) {  // as it was: the leader looks before the barrier, and counts
+    const uint32_t total = b.failed() ? 0xffffffffu : (uint32_t)u.total;
+    t.group->failed = false;
+    if (trident::attn_completes(b, &u.counter, total)) join(u.parts);
     return;
   }
   if (trident::attn_completes(b, &u.counter, (uint32_t)u.total)) join(u.parts);
@@ -205,8 +222,8 @@ std::string run(World& w, std::vector<Thread>& threads) {
 }
 
 // Block b's run goes from within unit b - 1 to within unit b (the first and the last run: one unit only).
-template <bool kOneWord>
-std::string parts(uint32_t seed, bool rows) {
+template <bool kOneWord, bool kCountsFailed = false>
+std::string parts(uint32_t seed, bool rows, bool fails = false) {
   World w;
   w.rng.seed(seed);
   std::vector<Group> groups(kBlocks);
@@ -223,11 +240,16 @@ std::string parts(uint32_t seed, bool rows) {
     t.group = &groups[t.block];
     t.body = [&units, rows](Thread& t) {
       Block<kOneWord> b{t};
-      if (t.block > 0) part(b, units[t.block - 1], t.block - 1, false, rows);
-      if (t.block + 1 < kBlocks) part(b, units[t.block], t.block, true, rows);
+      if (t.block > 0) part<kCountsFailed>(b, units[t.block - 1], t.block - 1, false, rows);
+      if (t.block + 1 < kBlocks) part<kCountsFailed>(b, units[t.block], t.block, true, rows);
     };
   }
+  if (fails) {
+    Thread& t = threads[w.rng() % threads.size()];
+    t.fails = t.block == 0 || (t.block + 1 < kBlocks && w.rng() % 2) ? t.block : t.block - 1;
+  }
   std::string fault = run(w, threads);
+  if (fails) return fault;
   for (Unit& u : units)
     if (fault.empty() && (u.joins != 1 || u.counter.value != 0)) fault = "a unit is not joined once, or its counter not zero after";
   return fault;
@@ -331,6 +353,8 @@ int main(int argc, char** argv) {
     std::string fault;
     if (name == "rows" || name == "tile") fault = parts<false>(i, name == "rows");
     else if (name == "rows-one-word" || name == "tile-one-word") fault = parts<true>(i, name == "rows-one-word");
+    else if (name == "tile-failed") fault = parts<false>(i, false, true);
+    else if (name == "tile-failed-counts") fault = parts<false, true>(i, false, true);
     else if (name == "start" || name == "start-reads-again") fault = start(i, name != "start");
     else return 2;
     if (!fault.empty()) {

@@ -38,3 +38,9 @@ def test_a_block_that_starts_late_takes_its_share(probe):
     """The second kernel's blocks, started before and after its block 0 has put the start word back."""
     assert probe("start") == "ok"
     assert probe("start-reads-again") != "ok"  # the form that goes by the word it reads after the wait
+
+
+def test_a_part_that_failed_is_not_joined(probe):
+    """A wait that runs out in one thread of a block: nobody reads the part that it did not write."""
+    assert probe("tile-failed") == "ok"
+    assert probe("tile-failed-counts") != "ok"  # the form whose failed block counts, and is completed by another
