@@ -163,8 +163,8 @@ typedef enum trident_dtype {
  *   reads kv head h / (Hq / Hkv). s_j = scalar * (q . k_j); out = round(sum_j softmax(s)_j v_j);
  *   lse = log(sum_j exp(s_j)). A row that sees no key gets out 0 and lse -inf, and so do the rows
  *   from cu_q[B] on. Cache rows from kv_len on are never used (they may hold NaN); keys below kv_len
- *   have to be finite. Sums and the softmax's statistics are fp32; its numerators are rounded to act
- *   for the product with v.
+ *   have to be finite. A row of q with a score that is NaN or +inf gets NaN in out and lse. Sums and the
+ *   softmax's statistics are fp32; its numerators are rounded to act for the product with v.
  *   work: zeros before its first use, left ready for the next call (after TRIDENT_DEVERR_TIMEOUT it
  *   has to be zeroed again); calls that may overlap on the GPU need a workspace each. The result does
  *   not depend on the order in which blocks finish. cu_q that is not ascending from 0 within [0,T], a kv_len outside

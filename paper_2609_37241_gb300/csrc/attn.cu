@@ -69,12 +69,12 @@ __global__ void __launch_bounds__(kThreads) attn_generic_kernel(const PagedAttnP
         if (lane + 32 * x < p.D) acc[x] = fmaf(pk, load_elem<DT>(p.vc.base, at + lane + 32 * x), acc[x]);
     }
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float inv = attn_inverse(l);
   char* out = row_ptr(p.out, t, p.o_rs, 2) + (int64_t)h * p.D * 2;
 #pragma unroll
   for (int x = 0; x < 16; ++x)
     if (lane + 32 * x < p.D) store_elem<DT>(out, lane + 32 * x, acc[x] * inv);
-  if (lane == 0) p.lse[t * p.Hq + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+  if (lane == 0) p.lse[t * p.Hq + h] = attn_lse(m, l);
   if (!ok) atomicOr(p.err, kErrTable);
 }
 

@@ -69,6 +69,11 @@ __device__ __forceinline__ float fast_exp2(float x) {
   return y;
 }
 
+// What a row's sum l of numerators and its maximum make of it; l is 0 where the row sees no key, and NaN where a
+// score was NaN or +inf: then so are out and lse.
+__device__ __forceinline__ float attn_inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
+__device__ __forceinline__ float attn_lse(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2; }
+
 // Rows past the last request: out 0, lse -inf.
 template <int NT>
 __device__ __forceinline__ void attn_fill_tail(const PagedAttnParams& p) {

@@ -438,12 +438,12 @@ struct RowsKernel {
     const int32_t r = u.r0 + row, i = (int32_t)fast_div((uint32_t)r, p.group.magic, p.group.shift);
     const int64_t t = u.q0 + i;
     const int h = u.h * p.G + (r - i * p.G);
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = attn_inverse(l);
     uint2 v;
     v.x = ActType<DT>::pack2(a.x * inv, a.y * inv);
     v.y = ActType<DT>::pack2(a.z * inv, a.w * inv);
     *reinterpret_cast<uint2*>(row_ptr(p.out, t, p.o_rs, 2) + ((int64_t)h * D + d) * 2) = v;
-    if (d == 0) p.lse[t * p.Hq + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+    if (d == 0) p.lse[t * p.Hq + h] = attn_lse(m, l);
   }
 
   // Joins n workspace slots, `at(i)` the i-th, into out and lse or into dst, the first of them.

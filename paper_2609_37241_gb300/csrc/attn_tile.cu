@@ -524,7 +524,7 @@ struct Tile {
     return row_ptr(p.out, t, p.o_rs, 2) + (int64_t)h * D * 2;
   }
   static __device__ __forceinline__ void put_lse(const PagedAttnParams& p, int64_t at, float m, float l) {
-    p.lse[at] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+    p.lse[at] = attn_lse(m, l);
   }
 
   // The finished accumulator to out, or unnormalised to a workspace slot: m[ROWS], l[ROWS], then for every
@@ -534,7 +534,7 @@ struct Tile {
     const uint32_t oc = tmem + (((threadIdx.x >> 5) & 3) << 21) + O_COL + x * D;
     const int r = x * 128 + (threadIdx.x & 127);
     const bool live = r < f.rows;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = attn_inverse(l);
     int64_t at = 0;
     char* out = live ? out_row(p, f, r, &at) : nullptr;
 #pragma unroll 1
@@ -634,7 +634,7 @@ struct Tile {
           *reinterpret_cast<float4*>(dst + 2 * ROWS + ((c / 4 + e) * ROWS + r) * 4) =
               make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
       } else {
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = attn_inverse(l);
 #pragma unroll
         for (int e = 0; e < 64; ++e) v[e] *= inv;
 #pragma unroll
