@@ -166,10 +166,11 @@ typedef enum trident_dtype {
  *   have to be finite. A row of q with a score that is NaN or +inf gets NaN in out and lse. Sums and the
  *   softmax's statistics are fp32; its numerators are rounded to act for the product with v.
  *   work: zeros before its first use, left ready for the next call (after TRIDENT_DEVERR_TIMEOUT it
- *   has to be zeroed again); calls that may overlap on the GPU need a workspace each. The result does
- *   not depend on the order in which blocks finish. cu_q that is not ascending from 0 within [0,T], a kv_len outside
- *   [0, M * ps] or a page number outside [0,P) (read as page 0) sets TRIDENT_DEVERR_TABLE; the
- *   outputs of such a request are unspecified.
+ *   has to be zeroed again); calls that may overlap on the GPU need a workspace each; calls in
+ *   order may share one, also of versions of different sizes where it is large enough for each. The
+ *   result does not depend on the order in which blocks finish. cu_q that is not ascending from 0 within
+ *   [0,T], a kv_len outside [0, M * ps] or a page number outside [0,P) (read as page 0) sets
+ *   TRIDENT_DEVERR_TABLE; the outputs of such a request are unspecified.
  */
 typedef enum trident_op {
   TRIDENT_OP_ADD_RMSNORM = 1,

@@ -110,9 +110,8 @@ int32_t attn_blocks(const AttnEntry& e, int32_t sms) {
   return sms * e.per_sm < kMaxAttnBlocks ? sms * e.per_sm : kMaxAttnBlocks;
 }
 
-int64_t attn_work_floats(const AttnEntry& e, int32_t sms) {
-  const int64_t blocks = attn_blocks(e, sms);
-  return e.fn ? attn_counters(blocks) + 2 * blocks * e.slot_floats : 0;
+int64_t attn_slots_floats(const AttnEntry& e, int32_t sms) {
+  return e.fn ? 2 * (int64_t)attn_blocks(e, sms) * e.slot_floats : 0;
 }
 
 bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, KernelEntry* out, const char** why) {

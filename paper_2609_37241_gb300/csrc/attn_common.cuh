@@ -40,9 +40,10 @@ __device__ __forceinline__ Request attn_request(const PagedAttnParams& p, int64_
 }
 
 
-// Workspace: counters (zero between calls), then two slots of rows * (D + 2) floats per block: slot 2c
-// for the unit that a block's run starts within, 2c + 1 for the one that it ends within.
-__host__ __device__ constexpr int64_t attn_counters(int64_t blocks) { return (4 * blocks + 31) / 32 * 32; }
+// Workspace: the words that are zero between calls first, as many for every version (kAttnWords), so that any of
+// them can use a workspace after another: the counters of both kernels and the start word. Then, for each
+// kernel, two slots of rows * (D + 2) floats per block: slot 2c for the unit that a block's run starts within,
+// 2c + 1 for the one that it ends within.
 __host__ __device__ constexpr int64_t attn_slot_floats(int rows, int D) { return (int64_t)rows * (D + 2); }
 
 template <int DT> struct ActType;

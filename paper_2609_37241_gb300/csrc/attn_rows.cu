@@ -473,8 +473,8 @@ struct RowsKernel {
   // The end of a fragment whose keys are done.
   static __device__ __forceinline__ void finish(const PagedAttnParams& p, Smem& s, const Unit& u, const float* m,
                                                 const float* l, const float (*o)[4]) {
-    uint32_t* counters = reinterpret_cast<uint32_t*>(p.work);
-    float* slots = p.work + attn_counters(gridDim.x);
+    uint32_t* counters = p.counters;
+    float* slots = p.slots;
     constexpr int64_t SLOT = attn_slot_floats(kRowsTile, D);
     const AttnCuts cut{u.first, u.last};
     const int n = (int)(cut.last - cut.first + 1), f = (int)(blockIdx.x - cut.first);

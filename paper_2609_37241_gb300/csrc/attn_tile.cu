@@ -826,8 +826,8 @@ struct Tile {
     const uint32_t tmem = s.tmem;
     AttnShare a{};
     if (work) a = Split::share(p, s.split);
-    uint32_t* counters = reinterpret_cast<uint32_t*>(p.work);
-    float* slots = p.work + attn_counters(gridDim.x);
+    uint32_t* counters = p.counters;
+    float* slots = p.slots;
     Load ld;
     bool ok = true;
     if (warp < MMA_WARP) {

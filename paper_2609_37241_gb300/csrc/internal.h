@@ -212,7 +212,8 @@ struct PagedAttnParams {
   const int32_t* table;
   const int32_t* cu;
   const int32_t* kv;
-  float* work;
+  uint32_t* counters;  // of this launch's kernel, and its slots (attn_common.cuh)
+  float* slots;
   void* out;
   float* lse;
   uint32_t* err;
@@ -372,11 +373,12 @@ struct AttnPlan {
   int64_t reread;
 };
 AttnPlan attn_plan(const AttnEntry& tile, int64_t T, int64_t B, int64_t G, int64_t D, int64_t ps, int64_t keys);
-constexpr int64_t kAttnWords = 32;  // of the workspace, for PagedAttnParams::start
 constexpr int kFanIn = 16, kJoinGroups = 20;  // slots joined in one round; groups of them at most
 constexpr int32_t kMaxAttnBlocks = kFanIn * kJoinGroups;
+// Workspace words that are zero between calls: 4 counters per block for each kernel, then the start word.
+constexpr int64_t kAttnCounters = 4 * kMaxAttnBlocks, kAttnWords = 2 * kAttnCounters + 32;
 int32_t attn_blocks(const AttnEntry& e, int32_t sms);
-int64_t attn_work_floats(const AttnEntry& e, int32_t sms);
+int64_t attn_slots_floats(const AttnEntry& e, int32_t sms);
 bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, KernelEntry* out, const char** why);
 const void* empty_kernel_entry();  // the latency-floor probe's kernel (does nothing)
 

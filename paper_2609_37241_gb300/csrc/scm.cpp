@@ -986,7 +986,7 @@ void pack_paged_attn(const trident_args* a, const Sig& s, uint32_t* err, PagedAt
   p->q = t[0].data;
   p->kc = paged_cache(t[1]); p->vc = paged_cache(t[2]);
   p->table = (const int32_t*)t[3].data; p->cu = (const int32_t*)t[4].data; p->kv = (const int32_t*)t[5].data;
-  p->work = (float*)t[6].data; p->out = t[7].data; p->lse = (float*)t[8].data;
+  p->out = t[7].data; p->lse = (float*)t[8].data;
   p->err = err;
   p->T = s.T; p->B = t[3].shape[0]; p->M = t[3].shape[1]; p->P = t[1].shape[0];
   p->table_rs = t[3].stride[0]; p->q_rs = t[0].stride[0]; p->o_rs = t[7].stride[0];
@@ -1052,11 +1052,14 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
     return launch_on(scm, &cfg, v.fn, kp);
   }
   const AttnEntry &rows = v.ke.attn_rows, &tile = v.ke.attn_tile;
-  const int64_t rows_work = attn_work_floats(rows, scm->sm_count);
-  const int64_t tile_work = attn_work_floats(tile, scm->sm_count);
-  if (a->t[6].shape[0] < rows_work + tile_work + kAttnWords)
+  const int64_t rows_slots = attn_slots_floats(rows, scm->sm_count);
+  const int64_t tile_slots = attn_slots_floats(tile, scm->sm_count);
+  if (a->t[6].shape[0] < kAttnWords + rows_slots + tile_slots)
     return fail(TRIDENT_ERR_INVALID, "the workspace is smaller than trident_scm_workspace says");
-  p.start = reinterpret_cast<uint32_t*>(p.work + rows_work + tile_work);
+  float* work = (float*)a->t[6].data;
+  p.counters = reinterpret_cast<uint32_t*>(work);
+  p.start = p.counters + 2 * kAttnCounters;
+  p.slots = work + kAttnWords;
   p.polls = kBulkWaitPolls;
   p.first_polls = (scm->opt.flags & TRIDENT_OPT_TEST_WAIT_TIMEOUT) ? 0u : kBulkWaitPolls;
   const AttnPlan pl = attn_plan(tile, s.T, p.B, p.G, p.D, p.page.d, p.M * p.page.d);
@@ -1077,7 +1080,8 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
   CUtensorMap mk, mv;
   if (!tile_map(&mk, a->t[1], v.d.dtype, tile.keys) || !tile_map(&mv, a->t[2], v.d.dtype, tile.keys))
     return fail(TRIDENT_ERR_CUDA, "cuTensorMapEncodeTiled failed");
-  p.work += rows_work;
+  p.counters += kAttnCounters;
+  p.slots += rows_slots;
   p.part = pl.rows ? ATTN_MANY : ATTN_ALL;
   p.min_tiles = kTileRun;
   p.tokens = tile.rows / p.G;
@@ -1770,7 +1774,7 @@ TRIDENT_API int32_t trident_scm_workspace(const trident_scm_t* scm, int32_t inde
   if (scm->dry) return fail(TRIDENT_ERR_STATE, "a dry-run SCM has no device to size a workspace for");
   const KernelEntry& ke = scm->versions[index].ke;
   if (ke.kind == KK_PAGED_ATTN && ke.vec > 1)
-    *out = attn_work_floats(ke.attn_rows, scm->sm_count) + attn_work_floats(ke.attn_tile, scm->sm_count) + kAttnWords;
+    *out = kAttnWords + attn_slots_floats(ke.attn_rows, scm->sm_count) + attn_slots_floats(ke.attn_tile, scm->sm_count);
   return TRIDENT_OK;
 }
 

@@ -113,3 +113,26 @@ def test_both_kernels_while_another_stream_holds_the_sms(S, D):
         assert torch.equal(b["out"], alone[0]), trial
         assert S.trident_scm_device_status(s.h, main.cuda_stream)[1] == 0
     s.close()
+
+
+def test_versions_of_different_head_sizes_share_a_workspace(S):
+    """Heads of 128, 64 and 256 in turn on one workspace, each call with cut units of both kernels: each
+    leaves partial results where it may, and what the next one counts with at zero."""
+    Hq, Hkv, ps = 32, 8, 16
+    s = S.Scm(flags=S.OPT_PDL)
+    heads = (128, 64, 256)
+    index = {D: s.register(S.make_spec(S.OP_PAGED_ATTN, S.BF16, [Hq, Hkv, D, ps], 1, 1 << 20, layout=S.LAYOUT_ANY))
+             for D in heads}
+    work = torch.zeros(max(s.workspace(i) for i in index.values()), device="cuda")
+    cases = {}
+    for D in heads:
+        b = R.batch(np.random.default_rng(D + 1), [1, 64, 1, 64], [2700, 9728, 3000, 9728], Hq, Hkv, D, ps, S.BF16)
+        cases[D] = b, reference(b, Hq, Hkv, ps, 1.0 / D ** 0.5)
+    for D in heads + heads[::-1] + heads:
+        b, ref = cases[D]
+        b["out"].fill_(float("nan"))
+        b["lse"].fill_(float("nan"))
+        call(S, s, index[D], b, work, 1.0 / D ** 0.5)
+        check(b, ref, S.BF16, 9728)
+    assert S.trident_scm_device_status(s.h, stream())[1] == 0
+    s.close()
