@@ -46,8 +46,13 @@ __device__ __forceinline__ Request attn_request(const PagedAttnParams& p, int64_
 // 2c + 1 for the one that it ends within.
 __host__ __device__ constexpr int64_t attn_slot_floats(int rows, int D) { return (int64_t)rows * (D + 2); }
 
+// kUp: the numerators are taken against the running maximum less kUp, so that they reach 2^kUp, and with a maximum
+// that is 2^8 behind 2^(kUp + 8). fp16 holds nothing below 2^-25: with 7 a key counts in the product with v down to
+// 2^-32 of the largest, not 2^-25, while the sum counts every one; 2^15 is within its range. In bf16 it would
+// change nothing. m in what follows is that level, and lse = m + log2 l whatever it is.
 template <int DT> struct ActType;
 template <> struct ActType<DT_BF16> {
+  static constexpr float kUp = 0.f;
   static __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
     uint32_t w;
@@ -56,6 +61,7 @@ template <> struct ActType<DT_BF16> {
   }
 };
 template <> struct ActType<DT_FP16> {
+  static constexpr float kUp = 7.f;
   static __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     __half2 b = __floats2half2_rn(lo, hi);
     uint32_t w;
@@ -63,6 +69,13 @@ template <> struct ActType<DT_FP16> {
     return w;
   }
 };
+
+// The level of a largest score, c * score in units of log 2.
+template <int DT>
+__device__ __forceinline__ float attn_level(float c, float score) {
+  if constexpr (ActType<DT>::kUp == 0.f) return c * score;
+  else return fmaf(c, score, -ActType<DT>::kUp);
+}
 
 __device__ __forceinline__ float fast_exp2(float x) {
   float y;

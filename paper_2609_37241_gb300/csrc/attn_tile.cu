@@ -478,7 +478,7 @@ struct Tile {
 #pragma unroll
         for (int i = 8; i < KEYS; i += 2)
           top[i / 2 & 3] = fmaxf(fmaxf(top[i / 2 & 3], __uint_as_float(a[i])), __uint_as_float(a[i + 1]));
-        const float hi = c * fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        const float hi = attn_level<DT>(c, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
         if (__any_sync(0xffffffffu, hi > m + kLazy)) {
           const float m2 = fmaxf(m, hi);
           const float g = m2 == -INFINITY ? 1.f : fast_exp2(m - m2);
