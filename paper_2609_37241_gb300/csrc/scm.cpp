@@ -1064,6 +1064,9 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
   p.first_polls = (scm->opt.flags & TRIDENT_OPT_TEST_WAIT_TIMEOUT) ? 0u : kBulkWaitPolls;
   const AttnPlan pl = attn_plan(tile, s.T, p.B, p.G, p.D, p.page.d, p.M * p.page.d);
   p.reread = pl.reread;
+  CUtensorMap mk, mv;  // before the first launch: a call that fails has not begun
+  if (pl.tile && (!tile_map(&mk, a->t[1], v.d.dtype, tile.keys) || !tile_map(&mv, a->t[2], v.d.dtype, tile.keys)))
+    return fail(TRIDENT_ERR_CUDA, "cuTensorMapEncodeTiled failed");
   if (pl.rows) {
     p.part = pl.tile ? ATTN_FEW : ATTN_ALL;
     p.min_tiles = kRowsRun;
@@ -1077,9 +1080,6 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
     attr.value.programmaticStreamSerializationAllowed = 1;
     cfg.numAttrs = 1;
   }
-  CUtensorMap mk, mv;
-  if (!tile_map(&mk, a->t[1], v.d.dtype, tile.keys) || !tile_map(&mv, a->t[2], v.d.dtype, tile.keys))
-    return fail(TRIDENT_ERR_CUDA, "cuTensorMapEncodeTiled failed");
   p.counters += kAttnCounters;
   p.slots += rows_slots;
   p.part = pl.rows ? ATTN_MANY : ATTN_ALL;
