@@ -168,7 +168,8 @@ typedef enum trident_dtype {
  *   work: zeros before its first use, left ready for the next call (after TRIDENT_DEVERR_TIMEOUT it
  *   has to be zeroed again); calls that may overlap on the GPU need a workspace each; calls in
  *   order may share one, also of versions of different sizes where it is large enough for each. The
- *   result does not depend on the order in which blocks finish. cu_q that is not ascending from 0 within
+ *   result does not depend on the order in which blocks finish. Sizes: T * Hq, B and P below 2^31, M * ps
+ *   below 2^31 - 4097 (ERR_INVALID at the launch). cu_q that is not ascending from 0 within
  *   [0,T], a kv_len outside [0, M * ps] or a page number outside [0,P) (read as page 0) sets
  *   TRIDENT_DEVERR_TABLE; the outputs of such a request are unspecified.
  */

@@ -1044,7 +1044,9 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
   }
   PagedAttnParams p;
   pack_paged_attn(a, s, scm->d_err, &p);
-  if (s.T * p.Hq >= kMost || p.B >= kMost || p.M * (int64_t)p.page.d >= kMost || p.P > kMost)
+  // the kernels look up to a tile (of 128 keys, by 32 lanes) past a request's last key before they stop at it
+  constexpr int64_t kPast = 4096;
+  if (s.T * p.Hq >= kMost || p.B >= kMost || p.M * (int64_t)p.page.d >= kMost - kPast || p.P > kMost)
     return fail(TRIDENT_ERR_INVALID, "paged attention call too large for 32-bit counts");
   void* kp[1] = {&p};
   if (v.ke.vec == 1) {

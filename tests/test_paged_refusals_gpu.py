@@ -54,3 +54,30 @@ def test_a_tensor_map_that_cannot_be_made(S):
         return ts
 
     refused_then_right(S, S.ERR_CUDA, change, S.OPT_NO_ALIAS_CHECK)
+
+
+def wide_table(b, width):
+    t = torch.zeros(b["table"].shape[0], width, dtype=torch.int32, device="cuda")
+    t[:, :b["table"].shape[1]] = b["table"]
+    return t
+
+
+def test_a_table_of_nearly_2_to_the_31_keys(S):
+    """Key numbers are 32-bit; the kernels look a little past the last one."""
+    refused_then_right(S, S.ERR_INVALID, lambda ts, b: ts[:3] + [desc(S, wide_table(b, (1 << 20) - 1))] + ts[4:])
+
+
+def test_a_table_just_below(S):
+    stream = torch.cuda.current_stream().cuda_stream
+    s = S.Scm()
+    index = s.register(S.make_spec(S.OP_PAGED_ATTN, S.BF16, [HQ, HKV, D, PS], 1, 1 << 20, layout=S.LAYOUT_ANY))
+    work = torch.zeros(s.workspace(index), device="cuda")
+    b = R.batch(np.random.default_rng(32), [1, 300], [700, 2000], HQ, HKV, D, PS, S.BF16, spare=0)
+    out, lse, wgt = R.attention(b["q"].cpu(), b["kc"].cpu(), b["vc"].cpu(), b["table"].cpu(), b["cu"].tolist(), [700, 2000], PS,
+                                0.1)
+    table = wide_table(b, (1 << 20) - 3)
+    ts = [b["q"], b["kc"], b["vc"], table, b["cu"], b["kv"], work, b["out"], b["lse"]]
+    assert s.invoke(S.make_args(S.OP_PAGED_ATTN, ts, scalar=0.1), stream) == (S.OK, index)
+    assert S.trident_scm_device_status(s.h, stream)[1] == 0
+    assert ((b["out"].cpu().double() - out).abs() <= R.attn_tolerance(out, wgt, S.BF16, 2000, 5.0)).all()
+    s.close()
