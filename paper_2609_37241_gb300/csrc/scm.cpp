@@ -698,6 +698,41 @@ bool same_desc(const trident_tensor& x, const trident_tensor& y) {
   return true;
 }
 
+// Do two paged caches of the same shape and strides (k and v of one buffer) share an element? d elements apart, they
+// do where d = sum e_k stride_k with |e_k| < shape_k. By stride, largest first: each stride is past the span of the
+// smaller ones (paged_layout_ok), so at most two e_k leave a rest within their span.
+bool paged_share(const trident_tensor& x, const trident_tensor& y) {
+  int d[4] = {0, 1, 2, 3};
+  std::sort(d, d + 4, [&](int a, int b) { return x.stride[a] > x.stride[b]; });
+  int64_t n[4], s[4], span[5] = {0, 0, 0, 0, 0};  // span[i]: what dimensions i .. reach
+  int m = 0;
+  for (int k : d)
+    if (x.shape[k] > 1) {
+      n[m] = x.shape[k];
+      s[m++] = x.stride[k];
+    }
+  for (int i = m - 1; i >= 0; --i) span[i] = span[i + 1] + (n[i] - 1) * s[i];
+  int64_t rest[16], next[16];
+  int count = 1;
+  rest[0] = ((int64_t)reinterpret_cast<uintptr_t>(y.data) - (int64_t)reinterpret_cast<uintptr_t>(x.data)) / elem_size(x.dtype);
+  for (int i = 0; i < m; ++i) {
+    int more = 0;
+    for (int j = 0; j < count; ++j)
+      for (int64_t e = fdiv(rest[j], s[i]), last = e + 1; e <= last; ++e) {
+        const int64_t left = rest[j] - e * s[i];
+        if (e > -n[i] && e < n[i] && left >= -span[i + 1] && left <= span[i + 1]) next[more++] = left;
+      }
+    std::copy(next, next + more, rest);
+    count = more;
+  }
+  return count > 0 && std::find(rest, rest + count, 0) != rest + count;
+}
+bool same_paged(const trident_tensor& x, const trident_tensor& y) {
+  for (int d = 0; d < 4; ++d)
+    if (x.shape[d] != y.shape[d] || x.stride[d] != y.stride[d]) return false;
+  return x.dtype == y.dtype;
+}
+
 // Launch precondition (checked after a hit, before the launch): no output shares a byte
 // with another slot unless the two are the same tensor in one of the op's in-place groups.
 // Slots are sorted by the start of their byte extent and swept once, so only pairs whose
@@ -731,6 +766,7 @@ int32_t check_overlap(const trident_args* a, const OpInfo& oi) {
       if (!oi.out[i] && !oi.out[j]) continue;  // inputs may share bytes
       if (!rows_overlap(base[i], nr[i], w[i], rs[i], base[j], nr[j], w[j], rs[j])) continue;
       if (oi.group[i] != 0 && oi.group[i] == oi.group[j] && same_desc(a->t[i], a->t[j])) continue;
+      if (oi.kind[i] == K_PAGED && oi.kind[j] == K_PAGED && same_paged(a->t[i], a->t[j]) && !paged_share(a->t[i], a->t[j])) continue;
       const int o = oi.out[i] ? i : j;
       return fail(TRIDENT_ERR_INVALID, "output tensor %d overlaps tensor %d", o, o == i ? j : i);
     }
