@@ -143,8 +143,8 @@ typedef enum trident_dtype {
  *   7 k_cache [P,Hkv,ps,D] act (out)  8 v_cache [P,Hkv,ps,D] act (out)
  *   Rotates the first R elements of each q and k head (R even, <= D; the others pass through): pairs
  *   (i, i + R/2), i < R/2, angle a = pos * f_i, f_i = freqs[i,0] + freqs[i,1] (trident_rope_freqs
- *   fills such a table, also for positions rescaled to long contexts), scalar * cos a and
- *   scalar * sin a in the place of cos and sin. q_out = round(rope(q)) (in place: q_out = q);
+ *   fills such a table, also for positions rescaled to long contexts; cos a and sin a to 1e-6 up to angles of
+ *   2^26), scalar * cos a and scalar * sin a in the place of cos and sin. q_out = round(rope(q)) (in place: q_out = q);
  *   k_cache[slot / ps, h, slot % ps, :] = round(rope(k)); the same row of v_cache = v (bit copy).
  *   The caches may have any page, head and row strides (elements of a row packed) that give every
  *   element bytes of its own. A slot below 0 is padding: its token's k and v are dropped. A slot of
@@ -169,9 +169,11 @@ typedef enum trident_dtype {
  *   has to be zeroed again); calls that may overlap on the GPU need a workspace each; calls in
  *   order may share one, also of versions of different sizes where it is large enough for each. The
  *   result does not depend on the order in which blocks finish. Sizes: T * Hq, B and P below 2^31, M * ps
- *   below 2^31 - 4097 (ERR_INVALID at the launch). cu_q that is not ascending from 0 within
- *   [0,T], a kv_len outside [0, M * ps] or a page number outside [0,P) (read as page 0) sets
- *   TRIDENT_DEVERR_TABLE; the outputs of such a request are unspecified.
+ *   below 2^31 - 4097 (ERR_INVALID at the launch). cu_q that is not ascending from 0 within [0,T], a
+ *   kv_len outside [0, M * ps] or a page number outside [0,P) (read as page 0) sets
+ *   TRIDENT_DEVERR_TABLE; the outputs of such a request are unspecified, and where cu_q descends those of
+ *   all requests. A request may have no rows; but a call with T <= B is made for one row per request, and
+ *   a long chunk among idle requests takes several times longer there: leave those out.
  */
 typedef enum trident_op {
   TRIDENT_OP_ADD_RMSNORM = 1,
@@ -203,7 +205,9 @@ typedef enum trident_rope_scaling {
                                frequency stays, the lowest is divided by factor (R > 2)     */
   TRIDENT_ROPE_PARTS = 3    /* by the turns n_i = context * f_i / (2 pi) that pair i makes over
                                the trained context: k_i = clamp((n_i - slow) / (fast - slow),
-                               0, 1), f_i * (k_i + (1 - k_i) / factor)                      */
+                               0, 1), f_i * (k_i + (1 - k_i) / factor). The ramp is over turns;
+                               a model trained with a ramp over the pair index between two
+                               (rounded) bounds needs a table of its own                     */
 } trident_rope_scaling;
 
 /* Layout class of an argument tuple (guard field, §2.2.1 "shape-related metadata").

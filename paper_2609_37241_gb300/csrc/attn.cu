@@ -92,9 +92,12 @@ __global__ void __launch_bounds__(kThreads) attn_generic_kernel(const PagedAttnP
 constexpr int64_t kReread = 4000 * 128, kRereadOne = 20000 * 128;
 
 // The lengths are on the device, so the choice goes by what T, B and the table's width (keys) leave
-// possible: both kernels, unless no request can pass the bound, or there is one request only. Pages that do
-// not divide a tile's keys (or are no multiple of them), or hold fewer than the eight rows of a swizzle
-// atom, and groups of more than 128 heads stay with the kernel of few rows.
+// possible where every request has a row: both kernels, unless no request can then pass the bound, or there is
+// one request only. So a call of no more rows than requests is taken for a decode step, for which a second launch
+// that finds nothing would cost 4 us. A request of many rows beside empty ones (idle slots) is right there, but
+// slow: 400 rows over 8000 keys among 512 requests 276 us, with 200 rows of padding 60, in a call of two 56.
+// Pages that do not divide a tile's keys (or are no multiple of them), or hold fewer than the eight rows of a
+// swizzle atom, and groups of more than 128 heads stay with the kernel of few rows.
 AttnPlan attn_plan(const AttnEntry& tile, int64_t T, int64_t B, int64_t G, int64_t D, int64_t ps, int64_t keys) {
   const bool fits = tile.fn && G <= 128 && ps % 8 == 0 && (tile.keys % ps == 0 || ps % tile.keys == 0);
   const int64_t most = T > B ? T - B + 1 : 1;  // rows of a request, if every one has some

@@ -14,8 +14,8 @@
 // They are rounded to the activation type for the product with v, the sum is taken before that.
 //
 // Measured on a GB300 (32 q heads on 8 kv heads of 128 where nothing else is said; of the 6.79 TB/s copy
-// rate): 64 requests of 1000 to 8000 keys 177 us (0.99), 3 of 131071 keys 237 us (1.00), 64 of 4000 keys with
-// 4 kv heads of 256 164 us (0.94); one request of 1000 keys 8.5 us, four dependent rounds of loads and the
+// rate): 64 requests of 1000 to 8000 keys 178 us (0.99), 3 of 131071 keys 242 us (0.98), 64 of 4000 keys with
+// 4 kv heads of 256 161 us (0.96); one request of 1000 keys 8.5 us, four dependent rounds of loads and the
 // join of its parts.
 #include "attn_common.cuh"
 

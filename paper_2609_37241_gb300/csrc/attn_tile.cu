@@ -18,9 +18,10 @@
 // TRIDENT_DEVERR_TIMEOUT and a flag that ends the block's other waits; the warps then let their copies
 // and products in flight finish (bounded again), free the TMEM and return without further writes.
 //
-// Measured on a GB300 (32 q heads on 8 kv heads of 128): 8192 rows after 8192 keys 951 to 1001 us in bursts
-// (1735 to 1647 TFLOP/s, 0.92 to 0.87 of cuBLAS' burst rate), 1039 to 1066 us back to back (0.94 to 0.92 of its
-// sustained rate, at the power limit); 2048 rows after 6144 keys 153 / 166 us, 1000 after 3096 55 us. 128 keys
+// Measured on a GB300 (32 q heads on 8 kv heads of 128): 8192 rows after 8192 keys 1035 to 1066 us back to back
+// (1593 to 1547 TFLOP/s, 0.94 to 0.92 of cuBLAS' sustained rate, at the power limit); 2048 rows after 6144 keys
+// 155 us in a graph of 30 calls, 166 longer, 1000 after 3096 55 us; 2048 after 6144 with heads of 64 126 us, of 256
+// 456 us. 128 keys
 // of a unit take 1.26 us, about 2500 cycles, 2048 of them the products at the full rate; what is more is the
 // chain of a tile's scores, softmax and products. Before its first tile a block takes 6 us (lengths, its share,
 // q), a cut part 4 us to write and 2.5 us to count, the last one 8 us to join.

@@ -9,8 +9,9 @@
 // the launch before may have written: they are read after the launch wait, by plain loads.
 //
 // Angles: pos < 2^24 is exact in fp32 and rope_sincos' first reduction step, fma(-k, A, pos * f), is
-// exact for every such angle (k A and pos * f are multiples of 2^-9 where they pass 2^15, and their
-// difference is small), so what remains is the error of the hardware sine, about 1e-6.
+// exact for every such angle with f <= 1 (k A and pos * f are multiples of 2^-9 where they pass 2^15, and their
+// difference is small), so what remains is the error of the hardware sine, about 1e-6. Frequencies above 1
+// take it further: the reduced angle is within 1e-6 up to angles of 2^26, 1.3e-5 at 2^30 (checked on the CPU).
 #include "device_common.cuh"
 
 namespace trident {
