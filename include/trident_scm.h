@@ -59,7 +59,9 @@ typedef enum trident_dtype {
   TRIDENT_FP32 = 3,  /* 4 bytes */
   TRIDENT_I32 = 4,   /* 4 bytes */
   TRIDENT_I64 = 5,   /* 8 bytes */
-  TRIDENT_U8 = 6     /* 1 byte (masks: 0 false, non-zero true) */
+  TRIDENT_U8 = 6,    /* 1 byte (masks: 0 false, non-zero true) */
+  TRIDENT_E4M3 = 7,  /* 1 byte: cache codes (4 exponent bits, 3 of mantissa, no infinity, largest 448) */
+  TRIDENT_E8M0 = 8   /* 1 byte: cache scales (the byte b is 2^(b - 127)) */
 } trident_dtype;
 
 /* ---------------------------------------------------------------- operations
@@ -174,6 +176,43 @@ typedef enum trident_dtype {
  *   TRIDENT_DEVERR_TABLE; the outputs of such a request are unspecified, and where cu_q descends those of
  *   all requests. A request may have no rows; but a call with T <= B is made for one row per request, and
  *   a long chunk among idle requests takes several times longer there: leave those out.
+ *
+ * Caches held in 8 bits: codes [P,Hkv,ps,D] e4m3 and scales [P,Hkv,ps/bt] e8m0, one for each block of bt
+ * consecutive rows of a page and head (bt, a divisor of ps, is a fixed size of the version: bt = 1 is a scale per
+ * token, bt = ps one per page). An element is code * scale. Scales are 2^e with e in [-32, 32]; a byte outside
+ * that range counts as the nearer end. Codes may have any strides as the caches above, scales any strides
+ * that give every scale a byte of its own; k and v may be of one buffer, codes and scales too where a page's
+ * codes and its scales do not lie inside each other's span.
+ *
+ * TRIDENT_OP_ROPE_PAGED_KV8 (11 tensors; act = bf16 | fp16; scalar as ROPE_PAGED_KV)
+ *   slots 0-6 as ROPE_PAGED_KV  7 k_cache [P,Hkv,ps,D] e4m3 (in/out)  8 v_cache (in/out)
+ *   9 k_scale [P,Hkv,ps/bt] e8m0 (in/out)  10 v_scale (in/out)
+ *   q_out and the values of k and v as ROPE_PAGED_KV, k's not rounded to act before they are quantised. Of a
+ *   block in which the call writes rows, e = the smallest with (largest magnitude of these rows) <= 448 * 2^e,
+ *   at least -32 (and at most 32: beyond it values, infinities among them, become +-448 * 2^32). A call that writes
+ *   a block's first row begins it anew: its scale is 2^e, and rows that are not written are left as they were. A
+ *   call that goes on with a block takes the larger of 2^e and its scale; where that grows, the block's other
+ *   rows are rounded to the new scale. code = round(value / scale); a NaN becomes a NaN code and does not count for
+ *   e. Rows of one block written by one call must come from consecutive tokens with ascending consecutive slots, as
+ *   PAGE_MAP gives them (else that block's codes and scale are unspecified). pos and slot are checked as in
+ *   ROPE_PAGED_KV; a token skipped for its position leaves its row's code unspecified.
+ * TRIDENT_OP_ROPE_PAGED_KV8_INTERLEAVED, TRIDENT_OP_QKNORM_ROPE_PAGED_KV8 and
+ * TRIDENT_OP_QKNORM_ROPE_PAGED_KV8_INTERLEAVED (13 tensors: 11 gamma_q [D] fp32, 12 gamma_k [D] fp32): as those of
+ *   ROPE_PAGED_KV.
+ *
+ * TRIDENT_OP_PAGED_READ8 (9 tensors; act = bf16 | fp16, of the outputs)
+ *   0 k_cache [P,Hkv,ps,D] e4m3  1 v_cache  2 k_scale [P,Hkv,ps/bt] e8m0  3 v_scale
+ *   4 block_table [B,M] i32  5 cu [B+1] i32  6 first [B] i32  7 k_out [T,Hkv,D] act (out)  8 v_out (out)
+ *   Rows cu[b] .. cu[b+1]-1 of the outputs are request b's tokens from position first[b] on: round(code * scale).
+ *   Rows from cu[B] on are left as they were. Sizes: T, B and P below 2^31, M * ps below 2^31 - 1. A position
+ *   outside [0, M * ps) or a page outside [0,P) gives a row of zeros and sets TRIDENT_DEVERR_TABLE; cu must ascend
+ *   from 0 (a request's rows are unspecified where it does not).
+ *
+ * TRIDENT_OP_PAGED_ATTN8 (11 tensors; act = bf16 | fp16; scalar = the scale of the scores, > 0)
+ *   0 q [T,Hq,D] act  1 k_cache [P,Hkv,ps,D] e4m3  2 v_cache  3 k_scale [P,Hkv,ps/bt] e8m0  4 v_scale
+ *   5 block_table  6 cu_q  7 kv_len  8 work  9 out [T,Hq,D] act (out)  10 lse [T,Hq] fp32 (out)
+ *   PAGED_ATTN with k and v = code * scale, in all that is said there. Codes below kv_len must not be NaN; codes
+ *   and scales past it may be anything.
  */
 typedef enum trident_op {
   TRIDENT_OP_ADD_RMSNORM = 1,
@@ -193,7 +232,13 @@ typedef enum trident_op {
   TRIDENT_OP_ROPE_PAGED_KV_INTERLEAVED = 18,
   TRIDENT_OP_QKNORM_ROPE_PAGED_KV = 19,
   TRIDENT_OP_QKNORM_ROPE_PAGED_KV_INTERLEAVED = 20,
-  TRIDENT_OP_PAGED_ATTN = 21
+  TRIDENT_OP_PAGED_ATTN = 21,
+  TRIDENT_OP_ROPE_PAGED_KV8 = 22,
+  TRIDENT_OP_ROPE_PAGED_KV8_INTERLEAVED = 23,
+  TRIDENT_OP_QKNORM_ROPE_PAGED_KV8 = 24,
+  TRIDENT_OP_QKNORM_ROPE_PAGED_KV8_INTERLEAVED = 25,
+  TRIDENT_OP_PAGED_READ8 = 26,
+  TRIDENT_OP_PAGED_ATTN8 = 27
 } trident_op;
 
 /* How trident_rope_freqs rescales the frequencies f_i = theta^(-2i/R) for contexts longer than

@@ -1,13 +1,14 @@
 // attn.cu -- attention of each request's last rows over its cache pages, any alignment (the formulas
 // are in attn_common.cuh), and the choice of the kernels.
 #include "attn_common.cuh"
+#include "kv8.cuh"
 
 namespace trident {
 namespace {
 
 // Any alignment and head size up to 512: one warp per (row, head), a key per lane for the scores, then
-// the lanes split D for the product with v.
-template <int DT>
+// the lanes split D for the product with v. KV8: the caches are held in 8 bits.
+template <int DT, bool KV8>
 __global__ void __launch_bounds__(kThreads) attn_generic_kernel(const PagedAttnParams p) {
   pdl_prologue();
   const int lane = threadIdx.x & 31;
@@ -35,7 +36,7 @@ __global__ void __launch_bounds__(kThreads) attn_generic_kernel(const PagedAttnP
   for (int e = 0; e < 16; ++e) acc[e] = 0.f;
   for (int64_t j0 = 0; j0 < seen; j0 += 32) {
     const int64_t j = j0 + lane;
-    float s = -INFINITY;
+    float s = -INFINITY, vscale = 1.f;
     int64_t vat = 0;
     if (j < seen) {
       const uint32_t pg = fast_div((uint32_t)j, p.page.magic, p.page.shift);
@@ -48,8 +49,14 @@ __global__ void __launch_bounds__(kThreads) attn_generic_kernel(const PagedAttnP
       const int64_t kat = page * p.kc.page + hk * p.kc.head + at * p.kc.row;
       vat = page * p.vc.page + hk * p.vc.head + at * p.vc.row;
       float d = 0.f;
-      for (int e = 0; e < p.D; ++e) d = fmaf(load_elem<DT>(q, e), load_elem<DT>(p.kc.base, kat + e), d);
+      for (int e = 0; e < p.D; ++e)
+        d = fmaf(load_elem<DT>(q, e), KV8 ? code_value(p.kc.base, kat + e) : load_elem<DT>(p.kc.base, kat + e), d);
       s = d * (p.scale * kLog2e);
+      if constexpr (KV8) {
+        const int block = (int)fast_div((uint32_t)at, p.block.magic, p.block.shift);
+        s *= exp2_int(scale_exp(*scale_at(p.ks, page, hk, block)));
+        vscale = exp2_int(scale_exp(*scale_at(p.vs, page, hk, block)));
+      }
     }
     float top = s;
 #pragma unroll
@@ -62,11 +69,13 @@ __global__ void __launch_bounds__(kThreads) attn_generic_kernel(const PagedAttnP
     for (int x = 0; x < 16; ++x) acc[x] *= old;
     const int n = (int)min((int64_t)32, seen - j0);
     for (int k = 0; k < n; ++k) {
-      const float pk = __shfl_sync(0xffffffffu, e, k);
+      const float pk = __shfl_sync(0xffffffffu, KV8 ? e * vscale : e, k);
       const int64_t at = __shfl_sync(0xffffffffu, vat, k);
 #pragma unroll
       for (int x = 0; x < 16; ++x)
-        if (lane + 32 * x < p.D) acc[x] = fmaf(pk, load_elem<DT>(p.vc.base, at + lane + 32 * x), acc[x]);
+        if (lane + 32 * x < p.D)
+          acc[x] = fmaf(pk, KV8 ? code_value(p.vc.base, at + lane + 32 * x) : load_elem<DT>(p.vc.base, at + lane + 32 * x),
+                        acc[x]);
     }
   }
   const float inv = attn_inverse(l);
@@ -117,10 +126,14 @@ int64_t attn_slots_floats(const AttnEntry& e, int32_t sms) {
   return e.fn ? 2 * (int64_t)attn_blocks(e, sms) * e.slot_floats : 0;
 }
 
-bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, KernelEntry* out, const char** why) {
+bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, bool kv8, KernelEntry* out, const char** why) {
   if (dtype != DT_BF16 && dtype != DT_FP16) { *why = "paged attention supports bf16 and fp16"; return false; }
   out->kind = KK_PAGED_ATTN;
   if (variant != 1) {
+    if (kv8) {
+      *why = "no vector kernel yet";
+      return false;
+    }
     if (!attn_rows_entry(dtype, D, &out->attn_rows)) {
       *why = "vector paged attention supports D in {64, 128, 256}";
       return false;
@@ -131,7 +144,8 @@ bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, KernelEntry* o
     return true;
   }
   out->vec = 1;
-  out->fn = dtype == DT_BF16 ? (const void*)attn_generic_kernel<DT_BF16> : (const void*)attn_generic_kernel<DT_FP16>;
+  if (kv8) out->fn = dtype == DT_BF16 ? (const void*)attn_generic_kernel<DT_BF16, true> : (const void*)attn_generic_kernel<DT_FP16, true>;
+  else out->fn = dtype == DT_BF16 ? (const void*)attn_generic_kernel<DT_BF16, false> : (const void*)attn_generic_kernel<DT_FP16, false>;
   return true;
 }
 

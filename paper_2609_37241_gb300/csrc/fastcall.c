@@ -141,8 +141,8 @@ static PyObject* fc_invoke_tree(PyObject* self, PyObject* const* args, Py_ssize_
  * (data_ptr, shape, stride, dtype, get_device); nothing is copied. */
 typedef struct {
   PyObject* tensor_type;
-  PyObject* dtypes[7]; /* bfloat16, float16, float32, int32, int64, uint8, bool */
-  int32_t codes[7];
+  PyObject* dtypes[9]; /* bfloat16, float16, float32, int32, int64, uint8, bool, float8_e4m3fn, float8_e8m0fnu */
+  int32_t codes[9];
   PyObject *s_data_ptr, *s_shape, *s_stride, *s_dtype, *s_get_device;
   PyObject *m_data_ptr, *m_stride, *m_get_device; /* torch.Tensor's own methods */
 } TorchNames;
@@ -152,12 +152,13 @@ static int torch_names(void) {
   if (tn.tensor_type) return 0;
   PyObject* torch = PyImport_ImportModule("torch");
   if (!torch) return -1;
-  static const char* names[7] = {"bfloat16", "float16", "float32", "int32", "int64", "uint8", "bool"};
-  static const int32_t codes[7] = {TRIDENT_BF16, TRIDENT_FP16, TRIDENT_FP32, TRIDENT_I32, TRIDENT_I64,
-                                   TRIDENT_U8, TRIDENT_U8};
+  static const char* names[9] = {"bfloat16", "float16", "float32", "int32", "int64", "uint8", "bool",
+                                 "float8_e4m3fn", "float8_e8m0fnu"};
+  static const int32_t codes[9] = {TRIDENT_BF16, TRIDENT_FP16, TRIDENT_FP32, TRIDENT_I32, TRIDENT_I64,
+                                   TRIDENT_U8, TRIDENT_U8, TRIDENT_E4M3, TRIDENT_E8M0};
   PyObject* tt = PyObject_GetAttrString(torch, "Tensor");
   int ok = tt != NULL;
-  for (int k = 0; ok && k < 7; ++k) {
+  for (int k = 0; ok && k < 9; ++k) {
     tn.dtypes[k] = PyObject_GetAttrString(torch, names[k]);
     tn.codes[k] = codes[k];
     ok = tn.dtypes[k] != NULL;
@@ -204,7 +205,7 @@ static int fill_from_torch(PyObject* t, trident_node* nd) {
         nd->t.stride[k] = PyLong_AsLongLong(PyTuple_GET_ITEM(stride, k));
       }
       nd->t.dtype = 0;
-      for (int k = 0; k < 7; ++k)
+      for (int k = 0; k < 9; ++k)
         if (dt == tn.dtypes[k]) nd->t.dtype = tn.codes[k];
       const long d = PyLong_AsLong(dev);
       nd->t.device = d >= 0 ? (int32_t)d : -1;

@@ -181,6 +181,12 @@ struct PagedCache {
   int64_t page, head, row;
 };
 
+// The scales of a paged cache held in 8 bits, a byte per block of a page's rows and head: strides in bytes.
+struct PagedScale {
+  uint8_t* base;
+  int64_t page, head, block;
+};
+
 // Partial, rescaled and interleaved RoPE with the append to a paged cache.
 struct RopePagedParams {
   const void* q;
@@ -202,6 +208,28 @@ struct RopePagedParams {
   int32_t ipt, rpi;  // warp items per token, head-rows per item (RopeSplit)
   uint32_t ipt_magic;
   int32_t ipt_shift;
+};
+
+// The same with the append to a cache held in 8 bits.
+struct RopePaged8Params {
+  RopePagedParams r;
+  PagedScale ks, vs;
+  FastDiv block;  // by the rows of a scale's block
+};
+
+// Rows of a cache held in 8 bits, read back in the activation type.
+struct PagedRead8Params {
+  PagedCache kc, vc;
+  PagedScale ks, vs;
+  const int32_t* table;
+  const int32_t* cu;
+  const int32_t* first;
+  void* k_out;
+  void* v_out;
+  uint32_t* err;
+  int64_t T, B, M, P, table_rs, k_rs, v_rs;
+  int32_t Hkv, D;
+  FastDiv page, block;
 };
 
 // Attention of each request's last rows over its pages.
@@ -227,6 +255,8 @@ struct PagedAttnParams {
   int64_t min_tiles;              // a block's run of key tiles is at least this long
   int32_t tokens;                 // tile kernel: tokens of a row tile
   uint32_t polls, first_polls;    // tile kernel: bounds of its waits, of a warp's first for scores
+  PagedScale ks, vs;              // caches held in 8 bits: their scales
+  FastDiv block;                  // ... and the rows of a scale's block
 };
 
 // Elementwise entries (pointwise_plan): flat and rows kernels with one or two vectors per
@@ -295,7 +325,9 @@ enum KernelKind : int32_t {
   KK_CHAIN = 6,
   KK_PAGE_MAP = 7,
   KK_ROPE_PAGED = 8,   // vector: any_fn by rope_paged_plan; generic (vec 1): one warp per head-row
-  KK_PAGED_ATTN = 9
+  KK_PAGED_ATTN = 9,
+  KK_ROPE_PAGED8 = 10,
+  KK_PAGED_READ8 = 11
 };
 
 constexpr int kMapThreads = 256;  // PAGE_MAP: block size
@@ -379,7 +411,10 @@ constexpr int32_t kMaxAttnBlocks = kFanIn * kJoinGroups;
 constexpr int64_t kAttnCounters = 4 * kMaxAttnBlocks, kAttnWords = 2 * kAttnCounters + 32;
 int32_t attn_blocks(const AttnEntry& e, int32_t sms);
 int64_t attn_slots_floats(const AttnEntry& e, int32_t sms);
-bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, KernelEntry* out, const char** why);
+bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, bool kv8, KernelEntry* out, const char** why);
+bool rope_paged8_kernel(int32_t dtype, int32_t variant, int32_t D, int32_t R, bool qknorm, bool inter,
+                        KernelEntry* out, const char** why);
+bool paged_read8_kernel(int32_t dtype, int32_t variant, int32_t D, KernelEntry* out, const char** why);
 const void* empty_kernel_entry();  // the latency-floor probe's kernel (does nothing)
 
 // Validation, guard-equivalent checks (sizes, layouts, 16-byte alignment, overlap) and

@@ -1,0 +1,73 @@
+// paged_read8.cu -- rows of a paged cache held in 8 bits (kv8.cuh), read back in the activation type.
+#include "kv8.cuh"
+
+namespace trident {
+namespace {
+
+constexpr uint32_t kErrTable = 0x10u;  // TRIDENT_DEVERR_TABLE
+
+// Where token t of the call lies: its page and row there. false: past the last request, or *bad (no such place).
+struct Place { int64_t page; int32_t row; };
+__device__ __forceinline__ bool place_of(const PagedRead8Params& p, int64_t t, Place* at, bool* bad) {
+  *bad = false;
+  if (p.B == 0 || t >= p.cu[p.B]) return false;
+  int64_t b = 0, n = p.B;  // the last request that starts at or before t, by 32 lanes
+  while (n > 1) {
+    const int64_t step = (n + 31) / 32, mine = (int64_t)(threadIdx.x & 31) * step;
+    const unsigned le = __ballot_sync(0xffffffffu, mine < n && p.cu[b + mine] <= t);
+    const int last = le ? 31 - __clz(le) : 0;
+    b += last * step;
+    n = min(step, n - last * step);
+  }
+  const int64_t pos = (int64_t)p.first[b] + (t - p.cu[b]);
+  if (t < p.cu[b] || pos < 0 || pos >= p.M * (int64_t)p.page.d) {
+    *bad = true;
+    return false;
+  }
+  const uint32_t pg = fast_div((uint32_t)pos, p.page.magic, p.page.shift);
+  at->page = p.table[b * p.table_rs + pg];
+  at->row = (int32_t)((uint32_t)pos - pg * (uint32_t)p.page.d);
+  *bad = at->page < 0 || at->page >= p.P;
+  return !*bad;
+}
+
+// Any alignment: one warp per token, an element per lane at a time.
+template <int DT>
+__global__ void __launch_bounds__(kThreads) paged_read8_generic_kernel(const PagedRead8Params p) {
+  pdl_prologue();
+  const int lane = threadIdx.x & 31;
+  const int64_t nwarps = (int64_t)gridDim.x * (kThreads / 32);
+  for (int64_t t = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / 32; t < p.T; t += nwarps) {
+    Place at{0, 0};
+    bool bad = false;
+    const bool live = place_of(p, t, &at, &bad);
+    if (!live && !bad) continue;
+    if (bad && lane == 0) atomicOr(p.err, kErrTable);
+    const int block = (int)fast_div((uint32_t)at.row, p.block.magic, p.block.shift);
+    for (int x = 0; x < 2; ++x) {
+      const PagedCache& c = x ? p.vc : p.kc;
+      char* out = row_ptr(x ? p.v_out : p.k_out, t, x ? p.v_rs : p.k_rs, 2);
+      for (int h = 0; h < p.Hkv; ++h) {
+        const float f = live ? exp2_int(scale_exp(*scale_at(x ? p.vs : p.ks, at.page, h, block))) : 0.f;
+        const int64_t src = at.page * c.page + h * c.head + at.row * c.row;
+        for (int j = lane; j < p.D; j += 32) store_elem<DT>(out, (int64_t)h * p.D + j, live ? code_value(c.base, src + j) * f : 0.f);
+      }
+    }
+  }
+}
+
+}  // namespace
+
+bool paged_read8_kernel(int32_t dtype, int32_t variant, int32_t D, KernelEntry* out, const char** why) {
+  if (dtype != DT_BF16 && dtype != DT_FP16) { *why = "reading a cache back supports bf16 and fp16"; return false; }
+  out->kind = KK_PAGED_READ8;
+  if (variant != 1) {
+    *why = "no vector kernel yet";
+    return false;
+  }
+  out->vec = 1;
+  out->fn = dtype == DT_BF16 ? (const void*)paged_read8_generic_kernel<DT_BF16> : (const void*)paged_read8_generic_kernel<DT_FP16>;
+  return true;
+}
+
+}  // namespace trident

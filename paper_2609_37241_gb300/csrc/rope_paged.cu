@@ -12,26 +12,12 @@
 // exact for every such angle with f <= 1 (k A and pos * f are multiples of 2^-9 where they pass 2^15, and their
 // difference is small), so what remains is the error of the hardware sine, about 1e-6. Frequencies above 1
 // take it further: the reduced angle is within 1e-6 up to angles of 2^26, 1.3e-5 at 2^30 (checked on the CPU).
-#include "device_common.cuh"
+#include "rope_paged.cuh"
 
 namespace trident {
 namespace {
 
-constexpr uint32_t kErrSlot = 0x4u;  // TRIDENT_DEVERR_SLOT
 constexpr int kRopePagedThreads = 64;
-
-// Element offsets of lane l's two vectors in a head-row.
-template <bool INTER>
-__device__ __forceinline__ void lane_vectors(const RopePagedParams& p, int l, int* a, int* b) {
-  const int pairs = p.R / 16;  // lanes that rotate
-  if (l >= pairs || INTER) {
-    *a = 16 * l;
-    *b = 16 * l + 8;
-  } else {
-    *a = 8 * l;
-    *b = p.R / 2 + 8 * l;
-  }
-}
 
 // The row of a token in a paged cache (slot valid).
 __device__ __forceinline__ char* paged_row(const PagedCache& c, const FastDiv& page, int32_t slot, int h) {
@@ -46,44 +32,6 @@ __device__ __forceinline__ char* paged_dst(const RopePagedParams& p, int64_t t, 
   if (slot < 0) return nullptr;
   const bool is_v = hh >= p.Hq + p.Hkv;
   return paged_row(is_v ? p.vc : p.kc, p.page, slot, hh - p.Hq - (is_v ? p.Hkv : 0));
-}
-__device__ __forceinline__ const char* paged_src(const RopePagedParams& p, int64_t t, int hh) {
-  const int64_t rb = (int64_t)p.D * 2;
-  return hh < p.Hq ? row_ptr(p.q, t, p.q_rs, 2) + hh * rb
-       : hh < p.Hq + p.Hkv ? row_ptr(p.k, t, p.k_rs, 2) + (hh - p.Hq) * rb
-                           : row_ptr(p.v, t, p.v_rs, 2) + (hh - p.Hq - p.Hkv) * rb;
-}
-
-// Eight values of vectors x and y as the first and second members of the lane's pairs, and back.
-template <bool INTER>
-__device__ __forceinline__ void pairs_of(const float* x, const float* y, bool rot, F2* A, F2* B) {
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    if (INTER && rot) {
-      const float* s = q < 2 ? x + 4 * q : y + 4 * (q - 2);
-      A[q] = f2_pack(s[0], s[2]);
-      B[q] = f2_pack(s[1], s[3]);
-    } else {
-      A[q] = f2_pack(x[2 * q], x[2 * q + 1]);
-      B[q] = f2_pack(y[2 * q], y[2 * q + 1]);
-    }
-  }
-}
-template <bool INTER>
-__device__ __forceinline__ void pairs_back(const F2* A, const F2* B, bool rot, float* x, float* y) {
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    float a0, a1, b0, b1;
-    f2_unpack(A[q], &a0, &a1);
-    f2_unpack(B[q], &b0, &b1);
-    if (INTER && rot) {
-      float* s = q < 2 ? x + 4 * q : y + 4 * (q - 2);
-      s[0] = a0; s[1] = b0; s[2] = a1; s[3] = b1;
-    } else {
-      x[2 * q] = a0; x[2 * q + 1] = a1;
-      y[2 * q] = b0; y[2 * q + 1] = b1;
-    }
-  }
 }
 
 // R rows per lane group; every load they need is issued first.
@@ -112,10 +60,7 @@ __global__ void __launch_bounds__(kRopePagedThreads) rope_paged_kernel(const Rop
   int32_t slot = p.slot[t];
   const bool rot = lane < p.R / 16;
   float4 fq[4];
-#pragma unroll
-  for (int q = 0; q < 4; ++q)
-    fq[q] = rot ? *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.freqs) + 16 * lane + 4 * q)
-                : make_float4(0.f, 0.f, 0.f, 0.f);
+  paged_freqs(p, lane, rot, fq);
   if (pos < 0 || pos >= kPosLimit) {
     if ((threadIdx.x & 31) == 0) atomicOr(p.err, kErrPos);
     return;
@@ -125,16 +70,7 @@ __global__ void __launch_bounds__(kRopePagedThreads) rope_paged_kernel(const Rop
     slot = -1;
   }
   RopeAngles an;
-  rope_angles(pos, fq, &an);
-  {
-    const F2 m = f2_pack(p.mag, p.mag);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      an.sn[q] = f2_mul(an.sn[q], m);
-      an.ns[q] = f2_mul(an.ns[q], m);
-      an.cs[q] = f2_mul(an.cs[q], m);
-    }
-  }
+  paged_angles(p, pos, fq, &an);
 #pragma unroll
   for (int j = 0; j < R; ++j) {
     const int hh = hh0 + j * GW;
@@ -148,38 +84,7 @@ __global__ void __launch_bounds__(kRopePagedThreads) rope_paged_kernel(const Rop
       continue;
     }
     float x[8], y[8];
-    F2 A[4], B[4];
-    unpack<DT>(lo[j], x);
-    unpack<DT>(hi[j], y);
-    if (QKNORM) {
-      float ss = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], fmaf(y[e], y[e], ss));
-      if (!on) ss = 0.f;
-      const unsigned mask =
-          LPG == 32 ? 0xffffffffu : (((1u << LPG) - 1u) << ((threadIdx.x & 31) & ~(LPG - 1)));
-#pragma unroll
-      for (int o = LPG / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(mask, ss, o, LPG);
-      const float inv = rsqrtf(ss * p.inv_D + p.eps);
-      const float* gam = hh < p.Hq ? p.gamma_q : p.gamma_k;
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const float4 ga = *reinterpret_cast<const float4*>(gam + va + 4 * q);
-        const float4 gb = *reinterpret_cast<const float4*>(gam + vb + 4 * q);
-        x[4 * q] *= inv * ga.x; x[4 * q + 1] *= inv * ga.y; x[4 * q + 2] *= inv * ga.z; x[4 * q + 3] *= inv * ga.w;
-        y[4 * q] *= inv * gb.x; y[4 * q + 1] *= inv * gb.y; y[4 * q + 2] *= inv * gb.z; y[4 * q + 3] *= inv * gb.w;
-      }
-    }
-    pairs_of<INTER>(x, y, rot, A, B);
-    if (rot) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const F2 a = A[q], b = B[q];
-        A[q] = f2_fma(a, an.cs[q], f2_mul(b, an.ns[q]));
-        B[q] = f2_fma(b, an.cs[q], f2_mul(a, an.sn[q]));
-      }
-    }
-    pairs_back<INTER>(A, B, rot, x, y);
+    paged_row_math<DT, LPG, QKNORM, INTER>(p, lo[j], hi[j], hh < p.Hq ? p.gamma_q : p.gamma_k, an, on, rot, va, vb, x, y);
     if (live && dst) {
       st16(dst + va * 2, pack<DT>(x));
       st16(dst + vb * 2, pack<DT>(y));

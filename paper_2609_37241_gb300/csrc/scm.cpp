@@ -115,7 +115,9 @@ enum Kind : uint8_t { K_ACT_H, K_ACT_I, K_GAMMA_H, K_GAMMA_D, K_HEADS_Q, K_HEADS
                      K_MASK_H,
                      // paged ops: i32 vectors [B], [B+1], [1], of any length and [B,M]; a paged cache, the
                      // frequency table, per-row statistics and the workspace
-                     K_REQ, K_CU, K_ONE, K_LIST, K_TABLE, K_PAGED, K_FREQ, K_LSE, K_WORK };
+                     K_REQ, K_CU, K_ONE, K_LIST, K_TABLE, K_PAGED, K_FREQ, K_LSE, K_WORK,
+                     // a paged cache held in 8 bits and its scales
+                     K_PAGED8, K_SCALE };
 
 struct OpInfo {
   int32_t nslots;
@@ -127,7 +129,7 @@ struct OpInfo {
   uint8_t group[TRIDENT_MAX_TENSORS];  // in-place group id (0: none)
 };
 
-constexpr int kMaxOp = TRIDENT_OP_PAGED_ATTN;  // ops without slots are not assigned
+constexpr int kMaxOp = TRIDENT_OP_PAGED_ATTN8;  // ops without slots are not assigned
 OpInfo g_ops[kMaxOp + 1];
 
 // slot index constants of the chains
@@ -195,6 +197,24 @@ struct OpInit {
     set(TRIDENT_OP_PAGED_ATTN, 4, false, false,
         {{K_HEADS_Q, false, 0}, {K_PAGED, false, 0}, {K_PAGED, false, 0}, {K_TABLE, false, 0}, {K_CU, false, 0},
          {K_REQ, false, 0}, {K_WORK, true, 0}, {K_HEADS_Q, true, 0}, {K_LSE, true, 0}});
+    const std::initializer_list<std::tuple<Kind, bool, int>> rope_paged8 = {
+        {K_HEADS_Q, false, 1}, {K_HEADS_KV, false, 0}, {K_HEADS_KV, false, 0}, {K_POS, false, 0}, {K_POS, false, 0},
+        {K_FREQ, false, 0}, {K_HEADS_Q, true, 1}, {K_PAGED8, true, 0}, {K_PAGED8, true, 0}, {K_SCALE, true, 0},
+        {K_SCALE, true, 0}};
+    for (int op : {TRIDENT_OP_ROPE_PAGED_KV8, TRIDENT_OP_ROPE_PAGED_KV8_INTERLEAVED, TRIDENT_OP_QKNORM_ROPE_PAGED_KV8,
+                   TRIDENT_OP_QKNORM_ROPE_PAGED_KV8_INTERLEAVED}) {
+      set(op, 6, false, false, rope_paged8);
+      if (op < TRIDENT_OP_QKNORM_ROPE_PAGED_KV8) continue;
+      g_ops[op].nslots = 13;
+      g_ops[op].kind[11] = g_ops[op].kind[12] = K_GAMMA_D;
+    }
+    set(TRIDENT_OP_PAGED_READ8, 4, false, false,
+        {{K_PAGED8, false, 0}, {K_PAGED8, false, 0}, {K_SCALE, false, 0}, {K_SCALE, false, 0}, {K_TABLE, false, 0},
+         {K_CU, false, 0}, {K_REQ, false, 0}, {K_HEADS_KV, true, 0}, {K_HEADS_KV, true, 0}});
+    set(TRIDENT_OP_PAGED_ATTN8, 5, false, false,
+        {{K_HEADS_Q, false, 0}, {K_PAGED8, false, 0}, {K_PAGED8, false, 0}, {K_SCALE, false, 0}, {K_SCALE, false, 0},
+         {K_TABLE, false, 0}, {K_CU, false, 0}, {K_REQ, false, 0}, {K_WORK, true, 0}, {K_HEADS_Q, true, 0},
+         {K_LSE, true, 0}});
   }
 } g_op_init;
 
@@ -202,13 +222,17 @@ inline bool is_paged_op(int32_t op) { return op >= TRIDENT_OP_PAGE_MAP; }
 inline bool is_rope_paged(int32_t op) {
   return op >= TRIDENT_OP_ROPE_PAGED_KV && op <= TRIDENT_OP_QKNORM_ROPE_PAGED_KV_INTERLEAVED;
 }
+inline bool is_rope_paged8(int32_t op) {
+  return op >= TRIDENT_OP_ROPE_PAGED_KV8 && op <= TRIDENT_OP_QKNORM_ROPE_PAGED_KV8_INTERLEAVED;
+}
+inline bool is_paged8_op(int32_t op) { return op >= TRIDENT_OP_ROPE_PAGED_KV8; }
 
 inline int elem_size(int32_t dt) {
   switch (dt) {
     case TRIDENT_BF16: case TRIDENT_FP16: return 2;
     case TRIDENT_FP32: case TRIDENT_I32: return 4;
     case TRIDENT_I64: return 8;
-    case TRIDENT_U8: return 1;
+    case TRIDENT_U8: case TRIDENT_E4M3: case TRIDENT_E8M0: return 1;
     default: return 0;
   }
 }
@@ -235,9 +259,12 @@ inline Rows rows_of(const trident_tensor& t, Kind k) {
     return {sh[0] * sh[1], sh[2], st[1], inner && st[0] == sh[1] * st[1]};
   }
   if (k == K_TABLE) return {sh[0], sh[1], st[0], sh[1] <= 1 || st[1] == 1};
-  if (k == K_PAGED) {  // a row per page, from its first element to its last
-    if (sh[0] == 0 || sh[1] == 0 || sh[2] == 0 || sh[3] == 0) return {0, 0, 0, true};
-    const int64_t w = 1 + (sh[1] - 1) * st[1] + (sh[2] - 1) * st[2] + (sh[3] - 1) * st[3];
+  if (k == K_PAGED || k == K_PAGED8 || k == K_SCALE) {  // a row per page, from its first element to its last
+    int64_t w = 1;
+    for (int d = 0; d < t.ndim; ++d) {
+      if (sh[d] == 0) return {0, 0, 0, true};
+      if (d > 0) w += (sh[d] - 1) * st[d];
+    }
     if (sh[0] == 1 || st[0] >= w) return {sh[0], w, st[0], true};
     return {1, w + (sh[0] - 1) * st[0], 0, true};  // pages inside each other's span: one extent
   }
@@ -288,13 +315,13 @@ inline int32_t check_tensor(const trident_tensor& x, int i, int es) {
   return TRIDENT_OK;
 }
 
-// Does every element of a paged cache have bytes of its own? Dimensions by stride, each past the
-// span of those before it.
+// Does every element of a paged cache (packed rows) or of its scales (a byte each) have bytes of its own?
+// Dimensions by stride, each past the span of those before it.
 inline bool paged_layout_ok(const trident_tensor& x) {
-  if (x.shape[3] > 1 && x.stride[3] != 1) return false;
+  if (x.ndim == 4 && x.shape[3] > 1 && x.stride[3] != 1) return false;
   int d[3] = {0, 1, 2};
   std::sort(d, d + 3, [&](int a, int b) { return x.stride[a] < x.stride[b]; });
-  int64_t span = x.shape[3];
+  int64_t span = x.ndim == 4 ? x.shape[3] : 1;
   for (int k : d) {
     if (x.shape[k] <= 1) continue;
     if (x.stride[k] < span) return false;
@@ -310,9 +337,10 @@ int32_t analyze_paged(const trident_args* a, const OpInfo& oi, Sig* s) {
   if (op == TRIDENT_OP_PAGE_MAP) {
     if (!(a->scalar >= 1.0 && a->scalar <= 65536.0 && a->scalar == std::floor(a->scalar)))
       return fail(TRIDENT_ERR_INVALID, "scalar (the page size) must be a whole number in [1, 65536]");
-  } else if (!(a->scalar > 0.0 && std::isfinite((float)a->scalar) && (float)a->scalar > 0.0f)) {
+  } else if (op != TRIDENT_OP_PAGED_READ8 &&
+             !(a->scalar > 0.0 && std::isfinite((float)a->scalar) && (float)a->scalar > 0.0f)) {
     return fail(TRIDENT_ERR_INVALID, "scalar (%s) must be positive and finite",
-                op == TRIDENT_OP_PAGED_ATTN ? "the scale of the scores" : "the magnitude of cos and sin");
+                op == TRIDENT_OP_PAGED_ATTN || op == TRIDENT_OP_PAGED_ATTN8 ? "the scale of the scores" : "the magnitude of cos and sin");
   }
   s->device = t[0].device;
   s->act_dtype = -1;
@@ -329,7 +357,8 @@ int32_t analyze_paged(const trident_args* a, const OpInfo& oi, Sig* s) {
     bool whole = false;  // i32, read one element at a time
     switch (k) {
       case K_HEADS_Q: case K_HEADS_KV: want = 3; break;
-      case K_PAGED: want = 4; break;
+      case K_PAGED: case K_PAGED8: want = 4; break;
+      case K_SCALE: want = 3; break;
       case K_TABLE: want = 2; whole = true; break;
       case K_FREQ: case K_LSE: want = 2; break;
       case K_GAMMA_D: case K_WORK: break;
@@ -340,9 +369,9 @@ int32_t analyze_paged(const trident_args* a, const OpInfo& oi, Sig* s) {
       if (s->act_dtype == -1) s->act_dtype = x.dtype;
       else if (s->act_dtype != x.dtype) s->act_dtype = kMixed;
     } else {
-      s->aux_dtype_ok &= x.dtype == (whole ? TRIDENT_I32 : TRIDENT_FP32);
+      s->aux_dtype_ok &= x.dtype == (whole ? TRIDENT_I32 : k == K_PAGED8 ? TRIDENT_E4M3 : k == K_SCALE ? TRIDENT_E8M0 : TRIDENT_FP32);
     }
-    if (!whole && s->aligned16) {
+    if (!whole && k != K_SCALE && s->aligned16) {
       if (reinterpret_cast<uintptr_t>(x.data) % 16 != 0) s->aligned16 = false;
       if (k != K_FREQ && k != K_LSE)  // dense where they match
         for (int d = 0; d + 1 < x.ndim; ++d)
@@ -358,9 +387,31 @@ int32_t analyze_paged(const trident_args* a, const OpInfo& oi, Sig* s) {
   s->T = s->lead[0] = t[0].shape[0];
   int64_t B = s->T, M = 0, Hq = 0, Hkv = 0, D = 0, P = 0, ps = 0;
   bool shapes = true;
+  int64_t blocks = 0;  // scales of a page's head
   if (op == TRIDENT_OP_PAGE_MAP) {
     M = t[4].shape[1];
     shapes &= t[7].shape[0] == t[8].shape[0];
+  } else if (is_paged8_op(op)) {
+    const int q = op == TRIDENT_OP_PAGED_READ8 ? 7 : 0, c = op == TRIDENT_OP_PAGED_READ8 ? 0 : op == TRIDENT_OP_PAGED_ATTN8 ? 1 : 7;
+    s->T = s->lead[0] = t[q].shape[0];
+    Hq = t[q].shape[1];
+    D = t[q].shape[2];
+    P = t[c].shape[0]; Hkv = t[c].shape[1]; ps = t[c].shape[2];
+    blocks = t[c + 2].shape[2];
+    const int64_t rows = blocks > 0 && ps % blocks == 0 ? ps / blocks : -1;
+    shapes &= P >= 1;
+    int f = 0;
+    if (op != TRIDENT_OP_PAGED_READ8) s->fixed[f++] = Hq;
+    s->fixed[f++] = Hkv;
+    s->fixed[f++] = D;
+    if (is_rope_paged8(op)) {
+      s->fixed[f++] = 2 * t[5].shape[0];
+    } else {
+      B = t[c + 4].shape[0];
+      M = t[c + 4].shape[1];
+    }
+    s->fixed[f++] = ps;
+    s->fixed[f++] = rows;
   } else {
     const trident_tensor& c = t[op == TRIDENT_OP_PAGED_ATTN ? 1 : 7];
     Hq = t[0].shape[1];
@@ -385,7 +436,8 @@ int32_t analyze_paged(const trident_args* a, const OpInfo& oi, Sig* s) {
     switch (k) {
       case K_HEADS_Q: shapes &= shape_is(x, {s->T, Hq, D}); row = true; break;
       case K_HEADS_KV: shapes &= shape_is(x, {s->T, Hkv, D}); row = true; break;
-      case K_PAGED: shapes &= shape_is(x, {P, Hkv, ps, D}); dense = paged_layout_ok(x); break;
+      case K_PAGED: case K_PAGED8: shapes &= shape_is(x, {P, Hkv, ps, D}); dense = paged_layout_ok(x); break;
+      case K_SCALE: shapes &= shape_is(x, {P, Hkv, blocks}); dense = paged_layout_ok(x); break;
       case K_TABLE: shapes &= shape_is(x, {B, M}); row = true; break;
       case K_POS: shapes &= shape_is(x, {s->T}); break;
       case K_REQ: shapes &= shape_is(x, {B}); break;
@@ -703,13 +755,13 @@ bool same_desc(const trident_tensor& x, const trident_tensor& y) {
 // smaller ones (paged_layout_ok), so at most two e_k leave a rest within their span.
 bool paged_share(const trident_tensor& x, const trident_tensor& y) {
   int d[4] = {0, 1, 2, 3};
-  std::sort(d, d + 4, [&](int a, int b) { return x.stride[a] > x.stride[b]; });
+  std::sort(d, d + x.ndim, [&](int a, int b) { return x.stride[a] > x.stride[b]; });
   int64_t n[4], s[4], span[5] = {0, 0, 0, 0, 0};  // span[i]: what dimensions i .. reach
   int m = 0;
-  for (int k : d)
-    if (x.shape[k] > 1) {
-      n[m] = x.shape[k];
-      s[m++] = x.stride[k];
+  for (int k = 0; k < x.ndim; ++k)
+    if (x.shape[d[k]] > 1) {
+      n[m] = x.shape[d[k]];
+      s[m++] = x.stride[d[k]];
     }
   for (int i = m - 1; i >= 0; --i) span[i] = span[i + 1] + (n[i] - 1) * s[i];
   int64_t rest[16], next[16];
@@ -728,10 +780,11 @@ bool paged_share(const trident_tensor& x, const trident_tensor& y) {
   return count > 0 && std::find(rest, rest + count, 0) != rest + count;
 }
 bool same_paged(const trident_tensor& x, const trident_tensor& y) {
-  for (int d = 0; d < 4; ++d)
+  for (int d = 0; d < x.ndim; ++d)
     if (x.shape[d] != y.shape[d] || x.stride[d] != y.stride[d]) return false;
   return x.dtype == y.dtype;
 }
+inline bool is_pool(Kind k) { return k == K_PAGED || k == K_PAGED8 || k == K_SCALE; }
 
 // Launch precondition (checked after a hit, before the launch): no output shares a byte
 // with another slot unless the two are the same tensor in one of the op's in-place groups.
@@ -766,7 +819,7 @@ int32_t check_overlap(const trident_args* a, const OpInfo& oi) {
       if (!oi.out[i] && !oi.out[j]) continue;  // inputs may share bytes
       if (!rows_overlap(base[i], nr[i], w[i], rs[i], base[j], nr[j], w[j], rs[j])) continue;
       if (oi.group[i] != 0 && oi.group[i] == oi.group[j] && same_desc(a->t[i], a->t[j])) continue;
-      if (oi.kind[i] == K_PAGED && oi.kind[j] == K_PAGED && same_paged(a->t[i], a->t[j]) && !paged_share(a->t[i], a->t[j])) continue;
+      if (is_pool(oi.kind[i]) && oi.kind[i] == oi.kind[j] && same_paged(a->t[i], a->t[j]) && !paged_share(a->t[i], a->t[j])) continue;
       const int o = oi.out[i] ? i : j;
       return fail(TRIDENT_ERR_INVALID, "output tensor %d overlaps tensor %d", o, o == i ? j : i);
     }
@@ -980,6 +1033,7 @@ inline FastDiv fast_divisor(int64_t d) {
 }
 
 inline PagedCache paged_cache(const trident_tensor& t) { return {t.data, t.stride[0], t.stride[1], t.stride[2]}; }
+inline PagedScale paged_scale(const trident_tensor& t) { return {(uint8_t*)t.data, t.stride[0], t.stride[1], t.stride[2]}; }
 
 void pack_page_map(const trident_args* a, const Sig& s, uint32_t* err, PageMapParams* p) {
   const trident_tensor* t = a->t;
@@ -995,14 +1049,15 @@ void pack_page_map(const trident_args* a, const Sig& s, uint32_t* err, PageMapPa
 
 void pack_rope_paged(const trident_args* a, uint32_t* err, RopePagedParams* p) {
   const trident_tensor* t = a->t;
-  const bool qk = a->op >= TRIDENT_OP_QKNORM_ROPE_PAGED_KV;
+  const bool kv8 = is_rope_paged8(a->op), qk = a->op >= (kv8 ? TRIDENT_OP_QKNORM_ROPE_PAGED_KV8 : TRIDENT_OP_QKNORM_ROPE_PAGED_KV);
+  const int g = kv8 ? 11 : 9;
   p->q = t[0].data; p->k = t[1].data; p->v = t[2].data;
   p->pos = (const int32_t*)t[3].data; p->slot = (const int32_t*)t[4].data;
   p->freqs = (const float2*)t[5].data;
   p->q_out = t[6].data;
   p->kc = paged_cache(t[7]); p->vc = paged_cache(t[8]);
-  p->gamma_q = qk ? (const float*)t[9].data : nullptr;
-  p->gamma_k = qk ? (const float*)t[10].data : nullptr;
+  p->gamma_q = qk ? (const float*)t[g].data : nullptr;
+  p->gamma_k = qk ? (const float*)t[g + 1].data : nullptr;
   p->err = err;
   p->T = t[0].shape[0];
   p->slots = t[7].shape[0] * t[7].shape[2];
@@ -1017,15 +1072,45 @@ void pack_rope_paged(const trident_args* a, uint32_t* err, RopePagedParams* p) {
   p->ipt = p->rpi = 0;
 }
 
+void pack_rope_paged8(const trident_args* a, const Sig& s, uint32_t* err, RopePaged8Params* p) {
+  pack_rope_paged(a, err, &p->r);
+  p->ks = paged_scale(a->t[9]);
+  p->vs = paged_scale(a->t[10]);
+  p->block = fast_divisor(s.fixed[5]);
+}
+
+void pack_paged_read8(const trident_args* a, const Sig& s, uint32_t* err, PagedRead8Params* p) {
+  const trident_tensor* t = a->t;
+  p->kc = paged_cache(t[0]); p->vc = paged_cache(t[1]);
+  p->ks = paged_scale(t[2]); p->vs = paged_scale(t[3]);
+  p->table = (const int32_t*)t[4].data; p->cu = (const int32_t*)t[5].data; p->first = (const int32_t*)t[6].data;
+  p->k_out = t[7].data; p->v_out = t[8].data;
+  p->err = err;
+  p->T = s.T; p->B = t[4].shape[0]; p->M = t[4].shape[1]; p->P = t[0].shape[0];
+  p->table_rs = t[4].stride[0]; p->k_rs = t[7].stride[0]; p->v_rs = t[8].stride[0];
+  p->Hkv = (int32_t)s.fixed[0]; p->D = (int32_t)s.fixed[1];
+  p->page = fast_divisor(s.fixed[2]);
+  p->block = fast_divisor(s.fixed[3]);
+}
+
 void pack_paged_attn(const trident_args* a, const Sig& s, uint32_t* err, PagedAttnParams* p) {
   const trident_tensor* t = a->t;
+  const bool kv8 = is_paged8_op(a->op);
+  const int table = kv8 ? 5 : 3;  // slots from the table on: table, cu_q, kv_len, work, out, lse
   p->q = t[0].data;
   p->kc = paged_cache(t[1]); p->vc = paged_cache(t[2]);
-  p->table = (const int32_t*)t[3].data; p->cu = (const int32_t*)t[4].data; p->kv = (const int32_t*)t[5].data;
-  p->out = t[7].data; p->lse = (float*)t[8].data;
+  p->ks = kv8 ? paged_scale(t[3]) : PagedScale{};
+  p->vs = kv8 ? paged_scale(t[4]) : PagedScale{};
+  p->block = fast_divisor(kv8 ? s.fixed[4] : 1);
+  t += table;
+  p->table = (const int32_t*)t[0].data; p->cu = (const int32_t*)t[1].data; p->kv = (const int32_t*)t[2].data;
+  p->out = t[4].data; p->lse = (float*)t[5].data;
   p->err = err;
-  p->T = s.T; p->B = t[3].shape[0]; p->M = t[3].shape[1]; p->P = t[1].shape[0];
-  p->table_rs = t[3].stride[0]; p->q_rs = t[0].stride[0]; p->o_rs = t[7].stride[0];
+  p->B = t[0].shape[0]; p->M = t[0].shape[1];
+  p->table_rs = t[0].stride[0]; p->o_rs = t[4].stride[0];
+  t = a->t;
+  p->T = s.T; p->P = t[1].shape[0];
+  p->q_rs = t[0].stride[0];
   p->Hq = (int32_t)t[0].shape[1]; p->Hkv = (int32_t)t[1].shape[1]; p->G = p->Hq / p->Hkv;
   p->D = (int32_t)t[0].shape[2];
   p->scale = (float)a->scalar;
@@ -1078,6 +1163,24 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
     void* kp[1] = {&p};
     return launch_on(scm, &cfg, fn, kp);
   }
+  if (is_rope_paged8(op)) {
+    RopePaged8Params p;
+    pack_rope_paged8(a, s, scm->d_err, &p);
+    if (s.T * p.r.NH >= kMost || p.r.slots > kMost)
+      return fail(TRIDENT_ERR_INVALID, "paged RoPE call too large for 32-bit counts");
+    cfg.gridDimX = cap_grid((s.T * p.r.NH + kThreads / 32 - 1) / (kThreads / 32));
+    void* kp[1] = {&p};
+    return launch_on(scm, &cfg, v.fn, kp);
+  }
+  if (op == TRIDENT_OP_PAGED_READ8) {
+    PagedRead8Params p;
+    pack_paged_read8(a, s, scm->d_err, &p);
+    if (p.T >= kMost || p.B >= kMost || p.M * (int64_t)p.page.d >= kMost || p.P > kMost)
+      return fail(TRIDENT_ERR_INVALID, "paged read too large for 32-bit counts");
+    cfg.gridDimX = cap_grid((p.T + kThreads / 32 - 1) / (kThreads / 32));
+    void* kp[1] = {&p};
+    return launch_on(scm, &cfg, v.fn, kp);
+  }
   PagedAttnParams p;
   pack_paged_attn(a, s, scm->d_err, &p);
   // the kernels look up to a tile (of 128 keys, by 32 lanes) past a request's last key before they stop at it
@@ -1089,12 +1192,13 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
     cfg.gridDimX = cap_grid((s.T * p.Hq + kThreads / 32 - 1) / (kThreads / 32));
     return launch_on(scm, &cfg, v.fn, kp);
   }
+  const int work_slot = is_paged8_op(op) ? 8 : 6;
   const AttnEntry &rows = v.ke.attn_rows, &tile = v.ke.attn_tile;
   const int64_t rows_slots = attn_slots_floats(rows, scm->sm_count);
   const int64_t tile_slots = attn_slots_floats(tile, scm->sm_count);
-  if (a->t[6].shape[0] < kAttnWords + rows_slots + tile_slots)
+  if (a->t[work_slot].shape[0] < kAttnWords + rows_slots + tile_slots)
     return fail(TRIDENT_ERR_INVALID, "the workspace is smaller than trident_scm_workspace says");
-  float* work = (float*)a->t[6].data;
+  float* work = (float*)a->t[work_slot].data;
   p.counters = reinterpret_cast<uint32_t*>(work);
   p.start = p.counters + 2 * kAttnCounters;
   p.slots = work + kAttnWords;
@@ -1459,7 +1563,7 @@ int32_t validate_desc(const trident_scm* scm, const trident_spec_desc* d, int32_
     return fail(TRIDENT_ERR_INVALID, "activation dtype %d", d->dtype);
   if (d->dtype == TRIDENT_FP32 && (oi.rope || is_paged_op(d->op)))
     return fail(TRIDENT_ERR_INVALID, "RoPE ops, chains and paged attention take bf16 or fp16");
-  if (oi.flattening ? (d->rank != 2 && d->rank != 3) : (d->rank != (map ? 1 : chain ? 2 : 3)))
+  if (oi.flattening ? (d->rank != 2 && d->rank != 3) : (d->rank != (map ? 1 : chain ? 2 : d->op == TRIDENT_OP_PAGED_READ8 ? 4 : 3)))
     return fail(TRIDENT_ERR_INVALID, "rank %d is not valid for op %d", d->rank, d->op);
   if (d->layout < TRIDENT_LAYOUT_CONTIG || d->layout > TRIDENT_LAYOUT_ANY)
     return fail(TRIDENT_ERR_INVALID, "layout %d", d->layout);
@@ -1486,12 +1590,15 @@ int32_t validate_desc(const trident_scm* scm, const trident_spec_desc* d, int32_
     const int64_t D = chain ? d->fixed[3] : d->fixed[2];
     if (D % 2 != 0 || D > 1024) return fail(TRIDENT_ERR_INVALID, "head size D must be even and <= 1024");
   }
-  if (is_rope_paged(d->op)) {
+  if (is_rope_paged(d->op) || is_rope_paged8(d->op)) {
     if (d->fixed[2] > 1024) return fail(TRIDENT_ERR_INVALID, "head size D must be <= 1024");
     if (d->fixed[3] % 2 != 0 || d->fixed[3] > d->fixed[2])
       return fail(TRIDENT_ERR_INVALID, "the rotated part R must be even and <= D");
   }
-  if (d->op == TRIDENT_OP_PAGED_ATTN) {
+  if (d->op == TRIDENT_OP_PAGED_READ8 && d->fixed[1] > 1024) return fail(TRIDENT_ERR_INVALID, "head size D must be <= 1024");
+  if (is_paged8_op(d->op) && d->fixed[oi.nfixed - 2] % d->fixed[oi.nfixed - 1] != 0)
+    return fail(TRIDENT_ERR_INVALID, "the page size must be a multiple of the scales' block");
+  if (d->op == TRIDENT_OP_PAGED_ATTN || d->op == TRIDENT_OP_PAGED_ATTN8) {
     if (d->fixed[0] % d->fixed[1] != 0) return fail(TRIDENT_ERR_INVALID, "Hq must be a multiple of Hkv");
     if (d->fixed[2] > 512) return fail(TRIDENT_ERR_INVALID, "head size D must be <= 512");
   }
@@ -1533,7 +1640,18 @@ int32_t resolve_kernel(const trident_spec_desc& d, KernelEntry* ke) {
                                  d.op >= TRIDENT_OP_QKNORM_ROPE_PAGED_KV,
                                  d.op == TRIDENT_OP_ROPE_PAGED_KV_INTERLEAVED ||
                                      d.op == TRIDENT_OP_QKNORM_ROPE_PAGED_KV_INTERLEAVED, ke, &why);
-      case TRIDENT_OP_PAGED_ATTN: return paged_attn_kernel(d.dtype, var, (int32_t)d.fixed[2], ke, &why);
+      case TRIDENT_OP_ROPE_PAGED_KV8:
+      case TRIDENT_OP_ROPE_PAGED_KV8_INTERLEAVED:
+      case TRIDENT_OP_QKNORM_ROPE_PAGED_KV8:
+      case TRIDENT_OP_QKNORM_ROPE_PAGED_KV8_INTERLEAVED:
+        return rope_paged8_kernel(d.dtype, var, (int32_t)d.fixed[2], (int32_t)d.fixed[3],
+                                  d.op >= TRIDENT_OP_QKNORM_ROPE_PAGED_KV8,
+                                  d.op == TRIDENT_OP_ROPE_PAGED_KV8_INTERLEAVED ||
+                                      d.op == TRIDENT_OP_QKNORM_ROPE_PAGED_KV8_INTERLEAVED, ke, &why);
+      case TRIDENT_OP_PAGED_READ8: return paged_read8_kernel(d.dtype, var, (int32_t)d.fixed[1], ke, &why);
+      case TRIDENT_OP_PAGED_ATTN:
+      case TRIDENT_OP_PAGED_ATTN8:
+        return paged_attn_kernel(d.dtype, var, (int32_t)d.fixed[2], d.op == TRIDENT_OP_PAGED_ATTN8, ke, &why);
       default:
         if (var == TRIDENT_VARIANT_GENERIC) { why = "the layer chain has no generic variant"; return false; }
         return chain_kernel(d.dtype, d.fixed[0], (int32_t)d.fixed[3], d.op == TRIDENT_OP_LAYER_CHAIN_QKNORM, ke, &why);

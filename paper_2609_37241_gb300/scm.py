@@ -15,12 +15,14 @@ LIB_PATH = os.path.join(PKG, "_lib", "libtrident_scm.so")
 OK, MISS_HANDLED, MISS = 0, 1, 2
 ERR_INVALID, ERR_CUDA, ERR_HOOK, ERR_CAPACITY, ERR_STATE = -1, -2, -3, -4, -5
 NOT_RUN = -2
-BF16, FP16, FP32, I32, I64, U8 = 1, 2, 3, 4, 5, 6
+BF16, FP16, FP32, I32, I64, U8, E4M3, E8M0 = 1, 2, 3, 4, 5, 6, 7, 8
 OP_ADD_RMSNORM, OP_ROPE_KV, OP_QKNORM_ROPE_KV, OP_SWIGLU, OP_LAYER_CHAIN, OP_LAYER_CHAIN_QKNORM = 1, 2, 3, 4, 5, 6
 OP_RMSNORM = 7
 OP_SILU, OP_ADD, OP_NEG, OP_MASKED_FILL = 8, 9, 10, 11
 OP_PAGE_MAP, OP_ROPE_PAGED_KV, OP_ROPE_PAGED_KV_INTERLEAVED = 16, 17, 18
 OP_QKNORM_ROPE_PAGED_KV, OP_QKNORM_ROPE_PAGED_KV_INTERLEAVED, OP_PAGED_ATTN = 19, 20, 21
+OP_ROPE_PAGED_KV8, OP_ROPE_PAGED_KV8_INTERLEAVED = 22, 23
+OP_QKNORM_ROPE_PAGED_KV8, OP_QKNORM_ROPE_PAGED_KV8_INTERLEAVED, OP_PAGED_READ8, OP_PAGED_ATTN8 = 24, 25, 26, 27
 LAYOUT_CONTIG, LAYOUT_ROWSTRIDED, LAYOUT_ANY = 0, 1, 2
 VARIANT_AUTO, VARIANT_GENERIC, VARIANT_VECTOR = 0, 1, 2
 OPT_DRY_RUN, OPT_NO_ALIAS_CHECK, OPT_PDL, OPT_TIMING, OPT_FAIL_LAUNCHES = 0x1, 0x2, 0x4, 0x8, 0x10
@@ -322,7 +324,8 @@ def _torch_dtypes():
     if _TORCH_DT is None:
         import torch
         _TORCH_DT = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32,
-                     torch.int32: I32, torch.int64: I64, torch.uint8: U8, torch.bool: U8}
+                     torch.int32: I32, torch.int64: I64, torch.uint8: U8, torch.bool: U8,
+                     torch.float8_e4m3fn: E4M3, torch.float8_e8m0fnu: E8M0}
     return _TORCH_DT
 
 
@@ -369,7 +372,9 @@ def make_args(op, tensors, eps=1e-6, rope_theta=0.0, scalar=0.0):
 
 
 _RANK = {OP_ROPE_KV: 3, OP_QKNORM_ROPE_KV: 3, OP_PAGE_MAP: 1, OP_ROPE_PAGED_KV: 3, OP_ROPE_PAGED_KV_INTERLEAVED: 3,
-         OP_QKNORM_ROPE_PAGED_KV: 3, OP_QKNORM_ROPE_PAGED_KV_INTERLEAVED: 3, OP_PAGED_ATTN: 3}
+         OP_QKNORM_ROPE_PAGED_KV: 3, OP_QKNORM_ROPE_PAGED_KV_INTERLEAVED: 3, OP_PAGED_ATTN: 3,
+         OP_ROPE_PAGED_KV8: 3, OP_ROPE_PAGED_KV8_INTERLEAVED: 3, OP_QKNORM_ROPE_PAGED_KV8: 3,
+         OP_QKNORM_ROPE_PAGED_KV8_INTERLEAVED: 3, OP_PAGED_READ8: 4, OP_PAGED_ATTN8: 3}
 
 
 def make_spec(op, dtype, fixed, tok_lo, tok_hi, rank=None, layout=LAYOUT_CONTIG, align_bytes=16,
@@ -604,7 +609,7 @@ class Scm:
         return trident_scm_select(self.h, args)
 
     def workspace(self, index):
-        """Elements of the fp32 workspace that version `index` needs (PAGED_ATTN's slot 6)."""
+        """Elements of the fp32 workspace that version `index` needs (slot `work` of PAGED_ATTN and PAGED_ATTN8)."""
         st, n = trident_scm_workspace(self.h, index)
         if st != OK:
             raise ScmError(st, "trident_scm_workspace")
