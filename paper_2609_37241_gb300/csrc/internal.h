@@ -216,6 +216,10 @@ struct RopePaged8Params {
   PagedScale ks, vs;
   FastDiv block;  // by the rows of a scale's block
 };
+struct Rope8Grid {
+  int32_t kv_blocks;  // thread blocks that append k and v; those after them rotate q
+  int32_t window;     // tokens of a team's window
+};
 
 // Rows of a cache held in 8 bits, read back in the activation type.
 struct PagedRead8Params {
@@ -414,6 +418,7 @@ int64_t attn_slots_floats(const AttnEntry& e, int32_t sms);
 bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, bool kv8, KernelEntry* out, const char** why);
 bool rope_paged8_kernel(int32_t dtype, int32_t variant, int32_t D, int32_t R, bool qknorm, bool inter,
                         KernelEntry* out, const char** why);
+int rope_paged8_plan(RopePaged8Params* p, Rope8Grid* grid, int32_t* threads, int64_t* blocks, int32_t sms);
 bool paged_read8_kernel(int32_t dtype, int32_t variant, int32_t D, KernelEntry* out, const char** why);
 const void* empty_kernel_entry();  // the latency-floor probe's kernel (does nothing)
 

@@ -147,15 +147,360 @@ __global__ void __launch_bounds__(kThreads) rope_paged8_generic_kernel(const Rop
   }
 }
 
+// ---------------------------------------------------------------- 16-byte aligned rows
+// A head-row by LPG lanes with two vectors of eight elements each (rope_paged.cuh), GW head-rows per warp at a time,
+// PASS times: ROWS rows of one head whose loads are issued together and whose values stay in registers between the
+// largest magnitude and the codes. Teams:
+//   TEAM 1  blocks of at most ROWS rows. A warp looks a window of tokens over and takes whole runs, as many as its
+//           rows hold: 16 decode steps or a block of a prompt cost the same round of loads.
+//   TEAM 4  larger blocks. The thread block's warps share a run, TEAM * ROWS rows at a time; a longer one is read and
+//           rotated twice.
+// Thread blocks [0, kv_blocks) do this, the others rotate q: items of `rpi` heads of a token per warp, as
+// rope_paged.cu.
+constexpr int kRope8Threads = 128;
+
+template <int DT, int LPG, bool INTER, int TEAM>
+struct Append8 {
+  static constexpr int GW = 32 / LPG, PASS = LPG == 4 ? 2 : 4, ROWS = GW * PASS, CAP = TEAM * ROWS;
+  static_assert(TEAM > 1 || CAP <= 16, "a warp's look at its tokens reaches past its rows");
+  struct Smem {
+    float top[4][16];
+    int32_t grown[4][16];
+  };
+  // What a lane holds of a head-row.
+  struct Lane {
+    int l, va, vb;
+    bool on, rot;
+    float4 fq[4];
+  };
+
+  static __device__ __forceinline__ float group_max(float v) {
+#pragma unroll
+    for (int o = LPG / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+  }
+
+  // Rows r(j) < n of the run tokens a + r: their values and, in m[j], their largest magnitudes (0: no such row, or
+  // skipped for its position: live[j] is false).
+  template <class Row>
+  static __device__ __forceinline__ void values(const RopePaged8Params& p8, const Lane& ln, int64_t a, int n, int hh, Row row,
+                                                float (*x)[16], float* m, bool* live) {
+    const RopePagedParams& p = p8.r;
+    const bool is_v = hh >= p.Hq + p.Hkv;
+    uint4 lo[PASS], hi[PASS];
+    int32_t pos[PASS];
+#pragma unroll
+    for (int j = 0; j < PASS; ++j) {
+      const int64_t t = a + min(row(j), n - 1);
+      const char* src = paged_src(p, t, hh);
+      lo[j] = ld16(src + ln.va * 2);
+      hi[j] = ld16(src + ln.vb * 2);
+      pos[j] = p.pos[t];
+    }
+#pragma unroll
+    for (int j = 0; j < PASS; ++j) {
+      const bool good = pos_valid(pos[j]);
+      live[j] = row(j) < n && good;
+      if (row(j) < n && !good && ln.l == 0) atomicOr(p.err, kErrPos);
+      if (is_v) {
+        unpack<DT>(lo[j], x[j]);
+        unpack<DT>(hi[j], x[j] + 8);
+      } else {
+        RopeAngles an;
+        paged_angles(p, good ? pos[j] : 0, ln.fq, &an);
+        if (p.gamma_k)
+          paged_row_math<DT, LPG, true, INTER>(p, lo[j], hi[j], p.gamma_k, an, ln.on, ln.rot, ln.va, ln.vb, x[j], x[j] + 8);
+        else
+          paged_row_math<DT, LPG, false, INTER>(p, lo[j], hi[j], nullptr, an, ln.on, ln.rot, ln.va, ln.vb, x[j], x[j] + 8);
+      }
+      float top = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[j][e]));
+      m[j] = group_max(ln.on && live[j] ? top : 0.f);
+    }
+  }
+
+  static __device__ __forceinline__ void put(const Lane& ln, uint8_t* row, const float* x, int e) {
+    const float f = exp2_int(-e);
+    float y[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = x[i] * f;
+    const uint2 a = make_uint2(codes4(y), codes4(y + 4)), b = make_uint2(codes4(y + 8), codes4(y + 12));
+    if (ln.vb == ln.va + 8) {
+      st16(row + ln.va, make_uint4(a.x, a.y, b.x, b.y));
+    } else {
+      *reinterpret_cast<uint2*>(row + ln.va) = a;
+      *reinterpret_cast<uint2*>(row + ln.vb) = b;
+    }
+  }
+
+  // The block's rows outside [first, first + n) to a scale 2^by larger; `who` of `of` threads.
+  static __device__ __forceinline__ void rescale(const RopePaged8Params& p, const Block8& b, int first, int n, int by, int who, int of) {
+    const int vecs = p.r.D / 16;
+    const float f = exp2_int(-by);
+    for (int i = who; i < (p.block.d - n) * vecs; i += of) {
+      int r = i / vecs;
+      uint8_t* at = b.row0 + (int64_t)(r < first ? r : r + n) * b.row + (i - r * vecs) * 16;
+      const uint4 v = ld16(at);
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+      uint32_t u[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 c = values2(halves2(w[k])), d = values2(halves2_hi(w[k]));
+        u[k] = codes2(c.x * f, c.y * f) | codes2(d.x * f, d.y * f) << 16;
+      }
+      st16(at, make_uint4(u[0], u[1], u[2], u[3]));
+    }
+  }
+
+  // A warp's window [t0, end) of tokens, head-row hh.
+  static __device__ __forceinline__ void window(const RopePaged8Params& p8, Smem& s, const Lane& ln, int64_t t0, int64_t end, int hh) {
+    const RopePagedParams& p = p8.r;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane / LPG;
+    const bool is_v = hh >= p.Hq + p.Hkv;
+    const int h = hh - p.Hq - (is_v ? p.Hkv : 0);
+    int64_t a = t0;
+    while (a < end) {
+      // 32 tokens from a on: which begin a run, which go on with one
+      const bool in = a + lane < p.T;
+      const int32_t slot = in ? p.slot[a + lane] : -1;
+      int32_t before = __shfl_up_sync(0xffffffffu, slot, 1);
+      if (lane == 0) before = a > 0 ? p.slot[a - 1] : -2;
+      const bool valid = slot_valid(p, slot);
+      if (slot >= p.slots && a + lane < end) atomicOr(p.err, kErrSlot);
+      const bool begins = valid && (before != slot - 1 || in_block(p8, slot) == 0 || (a == 0 && lane == 0));
+      const unsigned starts = __ballot_sync(0xffffffffu, begins), on = __ballot_sync(0xffffffffu, valid && !begins);
+      const unsigned mine = end - a < 32 ? starts & ((1u << (end - a)) - 1u) : starts;
+      if (mine == 0) {
+        a += 32;
+        continue;
+      }
+      if (!(mine & 1u)) {
+        a += __ffs(mine) - 1;
+        continue;
+      }
+      // whole runs from a on that fit the rows; none that begins past the window
+      // the last of rows 1 .. CAP that does not go on with a run: no run is longer than a block, which CAP rows hold
+      int n = max(1, 31 - __clz(~on & ((2u << CAP) - 1u)));
+      n = (int)min((int64_t)n, p.T - a);
+      const unsigned past = starts & ~mine;
+      if (past) n = min(n, __ffs(past) - 1);
+      auto row = [&](int j) { return j * GW + g; };
+      // each row's run: its first row and the one past its last; its block, and that block's scale
+      int first[PASS], stop[PASS], old[PASS];
+      int32_t at[PASS];
+      bool has[PASS];
+#pragma unroll
+      for (int j = 0; j < PASS; ++j) {
+        const int r = min(row(j), n - 1);
+        at[j] = __shfl_sync(0xffffffffu, slot, r);
+        has[j] = row(j) < n && ((starts | on) >> r & 1u);
+        const unsigned upto = starts & ((2u << r) - 1u);
+        first[j] = upto ? 31 - __clz(upto) : 0;
+        stop[j] = r + 1 + (__ffs(~(on >> (r + 1))) - 1);
+        old[j] = kScaleLo;
+        if (has[j] && in_block(p8, at[j]) > row(j) - first[j])  // the block was begun by an earlier call
+          old[j] = scale_exp(*block_of(p8, is_v, at[j], h).scale);
+      }
+      float x[PASS][16], m[PASS];
+      bool live[PASS];
+      values(p8, ln, a, n, hh, row, x, m, live);
+#pragma unroll
+      for (int j = 0; j < PASS; ++j)
+        if (ln.l == 0) s.top[w][row(j)] = has[j] ? m[j] : 0.f;
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < PASS; ++j) {
+        float top = 0.f;
+        for (int i = first[j] + ln.l; i < stop[j] && i < CAP; i += LPG) top = fmaxf(top, s.top[w][i]);
+        const int e = max(old[j], scale_for(group_max(top)));
+        const bool lead = has[j] && row(j) == first[j];
+        const int by = lead && in_block(p8, at[j]) > 0 ? e - old[j] : 0;
+        if (ln.l == 0) s.grown[w][row(j)] = by;
+        if (!has[j]) continue;
+        const Block8 blk = block_of(p8, is_v, at[j], h);
+        if (lead && ln.l == 0) *blk.scale = (uint8_t)(e + 127);
+        if (live[j] && ln.on) put(ln, blk.row0 + in_block(p8, at[j]) * blk.row, x[j], e);
+      }
+      __syncwarp();
+      unsigned grown = __ballot_sync(0xffffffffu, lane < n && s.grown[w][min(lane, CAP - 1)] > 0);
+      for (; grown; grown &= grown - 1) {
+        const int r = __ffs(grown) - 1;
+        const int32_t sl = __shfl_sync(0xffffffffu, slot, r);
+        const int len = __ffs(~(on >> (r + 1)));
+        rescale(p8, block_of(p8, is_v, sl, h), in_block(p8, sl), len, s.grown[w][r], lane, 32);
+      }
+      __syncwarp();
+      a += n;
+    }
+  }
+
+  // The same by the whole thread block, a run at a time.
+  static __device__ __forceinline__ void windows_of_team(const RopePaged8Params& p8, Smem& s, const Lane& ln, int64_t t0, int64_t end,
+                                                         int hh) {
+    const RopePagedParams& p = p8.r;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane / LPG;
+    const bool is_v = hh >= p.Hq + p.Hkv;
+    const int h = hh - p.Hq - (is_v ? p.Hkv : 0);
+    for (int64_t base = t0; base < end; base += 32) {
+      // the runs that begin among 32 tokens (every warp looks for itself)
+      const int64_t t = base + lane;
+      const int32_t slot = t < end ? p.slot[t] : -1;
+      if (slot >= p.slots && w == 0) atomicOr(p.err, kErrSlot);
+      unsigned starts = __ballot_sync(0xffffffffu, t < end && run_starts(p8, t, slot));
+      for (; starts; starts &= starts - 1) {
+        const int64_t a = base + __ffs(starts) - 1;
+        const int32_t s0 = __shfl_sync(0xffffffffu, slot, __ffs(starts) - 1);
+        const int at = in_block(p8, s0), most = (int)min((int64_t)(p8.block.d - at), p.T - a);
+        int n = 1;  // the run's tokens
+        while (n < most) {
+          const bool goes = n + lane < most && p.slot[a + n + lane] == s0 + n + lane;
+          const unsigned stop = __ballot_sync(0xffffffffu, !goes);
+          n += stop ? __ffs(stop) - 1 : 32;
+          if (stop) break;
+        }
+        const Block8 blk = block_of(p8, is_v, s0, h);
+        const int old = at > 0 ? scale_exp(*blk.scale) : kScaleLo;
+        float x[PASS][16], m[PASS], top = 0.f;
+        bool live[PASS];
+        int c = 0;
+        auto row = [&](int j) { return c * CAP + (j * TEAM + w) * GW + g; };
+        for (; c * CAP < n; ++c) {
+          values(p8, ln, a, n, hh, row, x, m, live);
+#pragma unroll
+          for (int j = 0; j < PASS; ++j) top = fmaxf(top, m[j]);
+        }
+#pragma unroll
+        for (int o = 16; o >= LPG; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        __syncthreads();  // the words below have been read for the run before
+        if (lane == 0) s.top[0][w] = top;
+        __syncthreads();
+        const int e = max(old, scale_for(fmaxf(fmaxf(s.top[0][0], s.top[0][1]), fmaxf(s.top[0][2], s.top[0][3]))));
+        if (threadIdx.x == 0) *blk.scale = (uint8_t)(e + 127);
+        const bool again = n > CAP;
+        for (c = 0; c * CAP < n; ++c) {
+          if (again) values(p8, ln, a, n, hh, row, x, m, live);
+#pragma unroll
+          for (int j = 0; j < PASS; ++j)
+            if (live[j] && ln.on) put(ln, blk.row0 + (int64_t)(at + row(j)) * blk.row, x[j], e);
+        }
+        if (at > 0 && e > old) rescale(p8, blk, at, n, e - old, threadIdx.x, kRope8Threads);
+      }
+    }
+  }
+};
+
+template <int DT, int LPG, bool INTER, int TEAM, int R>
+__global__ void __launch_bounds__(kRope8Threads, 3) rope_paged8_kernel(const RopePaged8Params p8, const Rope8Grid grid) {
+  using K = Append8<DT, LPG, INTER, TEAM>;
+  __shared__ typename K::Smem smem;
+  pdl_prologue();
+  const RopePagedParams& p = p8.r;
+  const int l = (threadIdx.x & 31) % LPG;
+  typename K::Lane ln;
+  ln.l = l;
+  const int lane = min(l, p.D / 16 - 1);
+  ln.on = l == lane;
+  ln.rot = lane < p.R / 16;
+  lane_vectors<INTER>(p, lane, &ln.va, &ln.vb);
+  if (blockIdx.x < grid.kv_blocks) {
+    const int64_t unit = TEAM > 1 ? blockIdx.x : (int64_t)blockIdx.x * (kRope8Threads / 32) + threadIdx.x / 32;
+    const int64_t win = unit / (2 * p.Hkv), t0 = win * grid.window;
+    if (t0 >= p.T) return;
+    const int hh = p.Hq + (int)(unit - win * (2 * p.Hkv));
+    if (hh < p.Hq + p.Hkv) paged_freqs(p, lane, ln.rot, ln.fq);
+    const int64_t end = min(p.T, t0 + grid.window);
+    if constexpr (TEAM > 1) K::windows_of_team(p8, smem, ln, t0, end, hh);
+    else K::window(p8, smem, ln, t0, end, hh);
+    return;
+  }
+  constexpr int GW = 32 / LPG;
+  const int64_t item = (int64_t)(blockIdx.x - grid.kv_blocks) * (kRope8Threads / 32) + threadIdx.x / 32;
+  if (item >= p.T * p.ipt) return;
+  const uint32_t tok = fast_div((uint32_t)item, p.ipt_magic, p.ipt_shift);
+  const int64_t t = tok;
+  const int first = (int)((uint32_t)item - tok * (uint32_t)p.ipt) * p.rpi, end = min(p.Hq, first + p.rpi);
+  const int hh0 = first + (threadIdx.x & 31) / LPG;
+  uint4 lo[R], hi[R];
+#pragma unroll
+  for (int j = 0; j < R; ++j) {  // groups past the item's end load its last row and drop it
+    const char* src = paged_src(p, t, min(hh0 + j * GW, end - 1));
+    lo[j] = ld16(src + ln.va * 2);
+    hi[j] = ld16(src + ln.vb * 2);
+  }
+  const int32_t pos = p.pos[t];
+  paged_freqs(p, lane, ln.rot, ln.fq);
+  if (!pos_valid(pos)) {
+    if ((threadIdx.x & 31) == 0) atomicOr(p.err, kErrPos);
+    return;
+  }
+  RopeAngles an;
+  paged_angles(p, pos, ln.fq, &an);
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    const int hh = hh0 + j * GW;
+    float x[8], y[8];
+    if (p.gamma_q) paged_row_math<DT, LPG, true, INTER>(p, lo[j], hi[j], p.gamma_q, an, ln.on, ln.rot, ln.va, ln.vb, x, y);
+    else paged_row_math<DT, LPG, false, INTER>(p, lo[j], hi[j], nullptr, an, ln.on, ln.rot, ln.va, ln.vb, x, y);
+    if (ln.on && hh < end) {
+      char* dst = row_ptr(p.q_out, t, p.o_rs, 2) + (int64_t)hh * p.D * 2;
+      st16(dst + ln.va * 2, pack<DT>(x));
+      st16(dst + ln.vb * 2, pack<DT>(y));
+    }
+  }
+}
+
+template <int DT, int LPG, bool INTER>
+void pick_vec(KernelEntry* out) {
+  out->any_fn[0] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 1, 1>;
+  out->any_fn[1] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 1, 3>;
+  out->any_fn[2] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 4, 1>;
+  out->any_fn[3] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 4, 3>;
+}
+
 }  // namespace
+
+// The entry of a vector call; sets q's item split, the grid and its parts.
+int rope_paged8_plan(RopePaged8Params* p8, Rope8Grid* grid, int32_t* threads, int64_t* blocks, int32_t sms) {
+  RopePagedParams* p = &p8->r;
+  const int lpg = p->D <= 64 ? 4 : p->D <= 128 ? 8 : 16, gw = 32 / lpg, rows = gw * (lpg == 4 ? 2 : 4);
+  const bool team = p8->block.d > rows;
+  constexpr int kWarps = kRope8Threads / 32;
+  RopeSplit r = rope_split(p->Hq, gw, 1);
+  if (p->T * r.ipt > 3 * (int64_t)sms) r = rope_split(p->Hq, gw, 3);
+  p->ipt = r.ipt;
+  p->rpi = r.rpi;
+  p->ipt_magic = r.magic;
+  p->ipt_shift = r.shift;
+  grid->window = 16;
+  const int64_t units = (p->T + grid->window - 1) / grid->window * 2 * p->Hkv;
+  const int64_t kv = team ? units : (units + kWarps - 1) / kWarps;
+  grid->kv_blocks = (int32_t)kv;
+  *threads = kRope8Threads;
+  *blocks = kv + (p->T * r.ipt + kWarps - 1) / kWarps;
+  return (team ? 2 : 0) + (r.rpi > gw ? 1 : 0);
+}
 
 bool rope_paged8_kernel(int32_t dtype, int32_t variant, int32_t D, int32_t R, bool qknorm, bool inter,
                         KernelEntry* out, const char** why) {
   if (dtype != DT_BF16 && dtype != DT_FP16) { *why = "RoPE supports bf16 and fp16"; return false; }
   out->kind = KK_ROPE_PAGED8;
   if (variant != 1) {
-    *why = "no vector kernel yet";
-    return false;
+    if (D % 16 != 0 || R % 16 != 0 || D < 32 || D > 256) {
+      *why = "vector paged RoPE supports D in 32 .. 256 and R that are multiples of 16";
+      return false;
+    }
+    out->vec = 8;
+    auto vec = [&](auto dt) {
+      constexpr int DT = decltype(dt)::value;
+      if (D <= 64) inter ? pick_vec<DT, 4, true>(out) : pick_vec<DT, 4, false>(out);
+      else if (D <= 128) inter ? pick_vec<DT, 8, true>(out) : pick_vec<DT, 8, false>(out);
+      else inter ? pick_vec<DT, 16, true>(out) : pick_vec<DT, 16, false>(out);
+    };
+    if (dtype == DT_BF16) vec(std::integral_constant<int, DT_BF16>());
+    else vec(std::integral_constant<int, DT_FP16>());
+    out->fn = out->any_fn[0];
+    return true;
   }
   out->vec = 1;
   auto pick = [&](auto dt) {

@@ -1168,9 +1168,17 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
     pack_rope_paged8(a, s, scm->d_err, &p);
     if (s.T * p.r.NH >= kMost || p.r.slots > kMost)
       return fail(TRIDENT_ERR_INVALID, "paged RoPE call too large for 32-bit counts");
-    cfg.gridDimX = cap_grid((s.T * p.r.NH + kThreads / 32 - 1) / (kThreads / 32));
-    void* kp[1] = {&p};
-    return launch_on(scm, &cfg, v.fn, kp);
+    Rope8Grid grid{};
+    int64_t blocks = (s.T * p.r.NH + kThreads / 32 - 1) / (kThreads / 32);
+    CUfunction fn = v.fn;
+    if (v.ke.vec > 1) {
+      int32_t threads = 0;
+      fn = v.any_fn[rope_paged8_plan(&p, &grid, &threads, &blocks, scm->sm_count)];
+      cfg.blockDimX = (unsigned)threads;
+    }
+    cfg.gridDimX = cap_grid(blocks);
+    void* kp[2] = {&p, &grid};
+    return launch_on(scm, &cfg, fn, kp);
   }
   if (op == TRIDENT_OP_PAGED_READ8) {
     PagedRead8Params p;
@@ -1178,7 +1186,8 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
     if (p.T >= kMost || p.B >= kMost || p.M * (int64_t)p.page.d >= kMost || p.P > kMost)
       return fail(TRIDENT_ERR_INVALID, "paged read too large for 32-bit counts");
     cfg.gridDimX = cap_grid((p.T + kThreads / 32 - 1) / (kThreads / 32));
-    void* kp[1] = {&p};
+    FastDiv vecs = fast_divisor(p.D / 16 > 0 ? p.D / 16 : 1);  // the vector kernel's: 16-byte vectors of a head
+    void* kp[2] = {&p, &vecs};
     return launch_on(scm, &cfg, v.fn, kp);
   }
   PagedAttnParams p;
