@@ -130,15 +130,11 @@ bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, bool kv8, Kern
   if (dtype != DT_BF16 && dtype != DT_FP16) { *why = "paged attention supports bf16 and fp16"; return false; }
   out->kind = KK_PAGED_ATTN;
   if (variant != 1) {
-    if (kv8) {
-      *why = "no vector kernel yet";
-      return false;
-    }
-    if (!attn_rows_entry(dtype, D, &out->attn_rows)) {
+    if (!(kv8 ? attn_rows8_entry(dtype, D, &out->attn_rows) : attn_rows_entry(dtype, D, &out->attn_rows))) {
       *why = "vector paged attention supports D in {64, 128, 256}";
       return false;
     }
-    attn_tile_entry(dtype, D, &out->attn_tile);
+    if (!kv8) attn_tile_entry(dtype, D, &out->attn_tile);
     out->vec = 8;
     out->fn = out->attn_rows.fn;
     return true;

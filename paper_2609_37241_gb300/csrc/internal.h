@@ -399,6 +399,7 @@ bool rope_paged_kernel(int32_t dtype, int32_t variant, int32_t D, int32_t R, boo
 // Which any_fn entry a vector call takes; sets its item split, block size and grid.
 int rope_paged_plan(RopePagedParams* p, int32_t* threads, int64_t* blocks, int32_t sms);
 bool attn_rows_entry(int32_t dtype, int32_t D, AttnEntry* e);
+bool attn_rows8_entry(int32_t dtype, int32_t D, AttnEntry* e);
 bool attn_tile_entry(int32_t dtype, int32_t D, AttnEntry* e);
 // Which attention kernels a call of T rows and B requests takes: the one of few rows, the tile kernel, or
 // both, each for its requests (attn_takes).
