@@ -17,9 +17,9 @@ LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "libtrident_scm.so")
 SOURCES = ["scm.cpp", "tree.cpp", "norm.cu", "rope.cu", "pointwise.cu", "chain.cu",
            "noalloc.cu", "page_map.cu", "rope_paged.cu", "rope_paged8.cu", "paged_read8.cu", "attn.cu",
-           "attn_rows.cu", "attn_rows8.cu", "attn_tile.cu"]
+           "attn_rows.cu", "attn_rows8.cu", "attn_tile.cu", "attn_tile8.cu"]
 HEADERS = ["internal.h", "device_common.cuh", "tree.h", "measure.h", "attn_common.cuh", "attn_count.h",
-           "kv8.cuh", "rope_paged.cuh", "attn_rows.cuh"]
+           "kv8.cuh", "rope_paged.cuh", "attn_rows.cuh", "attn_tile.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-fvisibility=hidden",
          "-I", INC, "-I", CSRC]

@@ -134,7 +134,8 @@ bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, bool kv8, Kern
       *why = "vector paged attention supports D in {64, 128, 256}";
       return false;
     }
-    if (!kv8) attn_tile_entry(dtype, D, &out->attn_tile);
+    if (kv8) attn_tile8_entry(dtype, D, &out->attn_tile);
+    else attn_tile_entry(dtype, D, &out->attn_tile);
     out->vec = 8;
     out->fn = out->attn_rows.fn;
     return true;

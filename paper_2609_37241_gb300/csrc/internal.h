@@ -401,6 +401,7 @@ int rope_paged_plan(RopePagedParams* p, int32_t* threads, int64_t* blocks, int32
 bool attn_rows_entry(int32_t dtype, int32_t D, AttnEntry* e);
 bool attn_rows8_entry(int32_t dtype, int32_t D, AttnEntry* e);
 bool attn_tile_entry(int32_t dtype, int32_t D, AttnEntry* e);
+bool attn_tile8_entry(int32_t dtype, int32_t D, AttnEntry* e);
 // Which attention kernels a call of T rows and B requests takes: the one of few rows, the tile kernel, or
 // both, each for its requests (attn_takes).
 constexpr int64_t kTileJoin = 10;  // tile kernel: what a cut unit costs, in tiles' time (12 us, a tile 1.25)

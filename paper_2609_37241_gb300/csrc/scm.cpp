@@ -1118,16 +1118,28 @@ void pack_paged_attn(const trident_args* a, const Sig& s, uint32_t* err, PagedAt
   p->group = fast_divisor(p->G);
 }
 
-// The tensor map of a paged cache for boxes of 64 elements and a page's rows (at most `keys`).
-bool tile_map(CUtensorMap* m, const trident_tensor& t, int32_t dtype, int32_t keys) {
+// The tensor map of a paged cache for boxes of `inner` elements and a page's rows (at most `keys`).
+bool tile_map(CUtensorMap* m, const trident_tensor& t, int32_t inner, int32_t keys, CUtensorMapSwizzle swizzle) {
+  const cuuint64_t es = (cuuint64_t)elem_size(t.dtype);
   const cuuint64_t dims[4] = {(cuuint64_t)t.shape[3], (cuuint64_t)t.shape[2], (cuuint64_t)t.shape[1], (cuuint64_t)t.shape[0]};
   cuuint64_t strides[3];  // bytes; of a dimension of one, which no coordinate leaves, any valid value
   for (int k = 0; k < 3; ++k)
-    strides[k] = t.shape[2 - k] > 1 ? (cuuint64_t)t.stride[2 - k] * 2 : (cuuint64_t)t.shape[3] * 2;
-  const cuuint32_t box[4] = {64, (cuuint32_t)(t.shape[2] < keys ? t.shape[2] : keys), 1, 1}, step[4] = {1, 1, 1, 1};
-  return g_drv.encode(m, dtype == TRIDENT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
-                      t.data, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+    strides[k] = (cuuint64_t)(t.shape[2 - k] > 1 ? t.stride[2 - k] : t.shape[3]) * es;
+  const cuuint32_t box[4] = {(cuuint32_t)inner, (cuuint32_t)(t.shape[2] < keys ? t.shape[2] : keys), 1, 1}, step[4] = {1, 1, 1, 1};
+  return g_drv.encode(m, t.dtype == TRIDENT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                         : t.dtype == TRIDENT_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8,
+                      4, t.data, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                       CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// k's and v's. 16 bits: both in the products' swizzle. 8 bits: k in it, by parts of at most 128 bytes; v's codes as
+// they lie, whole rows, for they are converted.
+bool tile_maps(CUtensorMap* mk, CUtensorMap* mv, const trident_args* a, int32_t keys) {
+  const trident_tensor &k = a->t[1], &v = a->t[2];
+  if (!is_paged8_op(a->op))
+    return tile_map(mk, k, 64, keys, CU_TENSOR_MAP_SWIZZLE_128B) && tile_map(mv, v, 64, keys, CU_TENSOR_MAP_SWIZZLE_128B);
+  const int32_t D = (int32_t)k.shape[3];
+  return tile_map(mk, k, D < 128 ? D : 128, keys, D < 128 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B) &&
+         tile_map(mv, v, D, keys, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 // Launch of a paged op. Counts that index in 32 bits are bounded here; bytes are indexed in 64.
@@ -1216,7 +1228,7 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
   const AttnPlan pl = attn_plan(tile, s.T, p.B, p.G, p.D, p.page.d, p.M * p.page.d);
   p.reread = pl.reread;
   CUtensorMap mk, mv;  // before the first launch: a call that fails has not begun
-  if (pl.tile && (!tile_map(&mk, a->t[1], v.d.dtype, tile.keys) || !tile_map(&mv, a->t[2], v.d.dtype, tile.keys)))
+  if (pl.tile && !tile_maps(&mk, &mv, a, tile.keys))
     return fail(TRIDENT_ERR_CUDA, "cuTensorMapEncodeTiled failed");
   if (pl.rows) {
     p.part = pl.tile ? ATTN_FEW : ATTN_ALL;

@@ -183,6 +183,6 @@ def reference(b, ps, scale):
 def tolerance(ref, wgt, level, dtype, n_keys):
     """|out - ref| bound: the output's rounding; the numerators' rounding to fp16, 2^-11 of each, and below fp16's normal
     numbers half of 2^-24 where the largest is at least 2^7 (2^-32 of the largest, times codes up to 448, n_keys times);
-    the scores' error, below 2^-13 for inputs as these (D products in fp32; q held within 2^-18 of its row's largest
+    the scores' error, below 2^-13 for inputs as these (D products in fp32; q held within 2^-21 of its row's largest
     element), so 2^-12 of the weights."""
     return 1.01 * R.UNIT[dtype] * ref.abs() + (1.05 * 2.0 ** -11 + 2.0 ** -12) * wgt + n_keys * 2.0 ** -32 * 448 * level
