@@ -10,6 +10,8 @@
 //       makes of them those keys' code 2g and code 2g + 1, operands of two products
 //   q   bf16 rows are scaled by a power of two to a largest element in [2^13, 2^14), so that halves hold them exactly
 //       down to 2^-27 of it
+// (m16n8k32 of 8 bits takes k's codes as they are, with q in two 8-bit pieces, but was slower: 64 decode steps 127 us for
+// 103.)
 // The scales 2^ek of k and 2^ev of v enter with the scores: with s the score in units of log 2, t = 2^ek s' + ev, the
 // running maximum m is of t, numerators 2^(t - m) hold v's scale already, and l takes them times 2^-ev. So the
 // numerators, rounded to halves, are the sizes of what each key adds to out: a block of small values that has the
@@ -52,7 +54,7 @@ __device__ __forceinline__ uint32_t top_bits(uint32_t top, uint32_t w) {
   return max(top, max(w & 0x7fffu, (w >> 16) & 0x7fffu));
 }
 // The exponent x for which a row with largest magnitude `bits` is held as q * 2^x.
-__device__ __forceinline__ int q_shift(uint32_t bits) { return 140 - (int)min(max(bits >> 7, 14u), 254u); }
+__device__ __forceinline__ int half_shift(uint32_t bits) { return 140 - (int)min(max(bits >> 7, 14u), 254u); }
 
 template <int DT_, int D_>
 struct Rows8 {
@@ -62,7 +64,7 @@ struct Rows8 {
   struct Extra {
     alignas(128) char q[2][G::QBUF];
     float q_factor[2][16];               // QS: the rows' 2^-x
-    alignas(16) float4 scale[4][2][WARP];  // of a warp's keys: 2^ek, ev, 2^-ev
+    alignas(16) float2 scale[4][G::NS][WARP];  // of a warp's keys: 2^ek, ev
   };
 
   // The table's entry for the lane's row (lane mod WARP) of the keys from j0 on. It is asked for a stage
@@ -72,9 +74,10 @@ struct Rows8 {
     return p.table[u.b * p.table_rs + fast_div(j, p.page.magic, p.page.shift)];
   }
 
-  // Issues the copies of WARP keys from j0 on into a stage, and returns the scales' bytes of the lane's key (k's, then
-  // v's; past the last key that key's); page: what entry() gave for them.
-  static __device__ __forceinline__ uint32_t load(const PagedAttnParams& p, const Unit& u, const char* kb, const char* vb,
+  struct Scales { uint32_t k, v; };
+
+  // Issues the copies of WARP keys from j0 on into a stage; page: what entry() gave for them.
+  static __device__ __forceinline__ void load(const PagedAttnParams& p, const Unit& u, const char* kb, const char* vb,
                                                   int32_t j0, int32_t page, uint32_t stage, bool* bad) {
     const int lane = threadIdx.x & 31;
     constexpr int RPI = 32 / G::CH;     // rows per instruction
@@ -94,6 +97,17 @@ struct Rows8 {
         const int32_t pg = KG == 1 ? page : __shfl_sync(0xffffffffu, page, 16 * h);
         const char* ks = kb + (int64_t)pg * p.kc.page + (int64_t)(at0 + rr) * p.kc.row + c * 16;
         const char* vs = vb + (int64_t)pg * p.vc.page + (int64_t)(at0 + rr) * p.vc.row + c * 16;
+        if (j0 + WARP <= u.limit) {
+#pragma unroll
+          for (int i = 0; i < ITER; ++i) {
+            const uint32_t dst = stage + G::at(16 * h + rr + i * RPI, c);
+            cp16(dst, ks);
+            cp16(dst + G::HALF, vs);
+            ks += kstep;
+            vs += vstep;
+          }
+          continue;
+        }
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
           const int r = 16 * h + rr + i * RPI;
@@ -116,8 +130,20 @@ struct Rows8 {
         cp16(dst + G::HALF, live ? vb + vr + c * 16 : vb, live);
       }
     }
+  }
+
+  // Asks for the scales of the lane's key (past the last key that key's). They come back behind the copies that were
+  // issued before them, so they are asked for before a stage's copies and used behind the wait for the stage before.
+  static __device__ __forceinline__ Scales scales(const PagedAttnParams& p, const Unit& u, int32_t j0, int32_t page) {
+    if (page < 0 || page >= p.P) page = 0;  // load() says so
+    const uint32_t j = (uint32_t)min(j0 + (int32_t)(threadIdx.x & (WARP - 1)), u.limit - 1);
+    const int32_t at = (int32_t)(j - fast_div(j, p.page.magic, p.page.shift) * (uint32_t)p.page.d);
     const int block = (int)fast_div((uint32_t)at, p.block.magic, p.block.shift);
-    return *scale_at(p.ks, page, u.h, block) | (uint32_t)*scale_at(p.vs, page, u.h, block) << 8;
+    return {*scale_at(p.ks, page, u.h, block), *scale_at(p.vs, page, u.h, block)};
+  }
+  static __device__ __forceinline__ void put_scales(float2* to, const Scales& sc) {
+    const int lane = threadIdx.x & 31, ek = scale_exp(sc.k), ev = scale_exp(sc.v);
+    if (WARP == 32 || lane < WARP) to[lane & (WARP - 1)] = make_float2(exp2_int(ek), (float)ev);
   }
 
   // What a warp holds of a fragment between its first loads and its last product.
@@ -128,7 +154,7 @@ struct Rows8 {
     int32_t see[2];         // keys that rows g and g + 8 see
     uint32_t q[G::QREG][4];
     float factor[2];        // rows g and g + 8: score of the held q times this, in units of log 2
-    uint32_t scale[G::NS - 1];  // scales' bytes of the next groups
+    Scales scale[G::NS - 1];  // of the first groups
     int32_t buf;            // QS: which buffer q is in
   };
 
@@ -162,8 +188,8 @@ struct Rows8 {
         if constexpr (DT == DT_BF16) {
           uint32_t top = top_bits(top_bits(top_bits(top_bits(0, v.x), v.y), v.z), v.w);
           top = __reduce_max_sync(0xffffffffu, top);
-          f = exp2_int(q_shift(top));
-          if (lane == 0) s.q_factor[st.buf][row] = c * exp2_int(-q_shift(top));
+          f = exp2_int(half_shift(top));
+          if (lane == 0) s.q_factor[st.buf][row] = c * exp2_int(-half_shift(top));
         }
         // elements 8 lane ..: of a product's 16, each four give their first two to the first eight, the others to the last
         char* at = s.q[st.buf] + row * (D * 2);
@@ -187,8 +213,8 @@ struct Rows8 {
         if constexpr (DT == DT_BF16) {
           top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
           top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          const float f = exp2_int(q_shift(top));
-          st.factor[k] = c * exp2_int(-q_shift(top));
+          const float f = exp2_int(half_shift(top));
+          st.factor[k] = c * exp2_int(-half_shift(top));
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
             st.q[kk][k] = q_halves<DT>(st.q[kk][k], f);
@@ -208,8 +234,12 @@ struct Rows8 {
     for (int i = 0; i < G::NS; ++i) page[i] = i < st.groups ? entry(p, u, st.first + i * KEYS) : 0;
 #pragma unroll
     for (int i = 0; i < G::NS - 1; ++i) {
-      st.scale[i] = 0;
-      if (i < st.groups) st.scale[i] = load(p, u, st.kb, st.vb, st.first + i * KEYS, page[i], ring + i * G::STAGE, bad);
+      st.scale[i] = {127, 127};
+      if (i < st.groups) st.scale[i] = scales(p, u, st.first + i * KEYS, page[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < G::NS - 1; ++i) {
+      if (i < st.groups) load(p, u, st.kb, st.vb, st.first + i * KEYS, page[i], ring + i * G::STAGE, bad);
       cp_commit();
     }
     st.page = page[G::NS - 1];
@@ -234,21 +264,21 @@ struct Rows8 {
       factor[0] = s.q_factor[st.buf & 1][g];
       factor[1] = s.q_factor[st.buf & 1][g + 8];
     }
-    for (int x = 0; x < st.groups; ++x) {
-      {  // of the keys of this step; the step before last has read these words
-        const int ek = scale_exp(st.scale[0] & 255u), ev = scale_exp(st.scale[0] >> 8);
-        if (WARP == 32 || lane < WARP) s.scale[w][x & 1][lane & (WARP - 1)] = make_float4(exp2_int(ek), (float)ev, exp2_int(-ev), 0.f);
-      }
 #pragma unroll
-      for (int i = 0; i + 1 < G::NS - 1; ++i) st.scale[i] = st.scale[i + 1];
+    for (int i = 0; i < G::NS - 1; ++i) put_scales(s.scale[w][i], st.scale[i]);
+    Scales next{127, 127};  // of group x + NS - 2
+    for (int x = 0; x < st.groups; ++x) {
       cp_wait<G::NS - 2>();
-      __syncwarp();  // all lanes' copies and words have landed, and the stage refilled below has been read
+      __syncwarp();  // all lanes' copies and words have landed, and the stage and the words written below have been read
       {
+        if (x > 0) put_scales(s.scale[w][(x + G::NS - 2) % G::NS], next);
+        if (G::NS == 2) __syncwarp();
         const int y = x + G::NS - 1;
         if (y < st.groups) {
           const int32_t page = st.page;
+          next = scales(p, u, st.first + y * KEYS, page);
           if (y + 1 < st.groups) st.page = entry(p, u, st.first + (y + 1) * KEYS);
-          st.scale[G::NS - 2] = load(p, u, st.kb, st.vb, st.first + y * KEYS, page, ring + (y % G::NS) * G::STAGE, bad);
+          load(p, u, st.kb, st.vb, st.first + y * KEYS, page, ring + (y % G::NS) * G::STAGE, bad);
         }
         cp_commit();
       }
@@ -282,14 +312,16 @@ struct Rows8 {
       // scores with the blocks' scales: t, in sc; f: 2^-ev
       float f[2 * KG][2];
 #pragma unroll
-      for (int nt = 0; nt < 2 * KG; ++nt)
+      for (int nt = 0; nt < 2 * KG; ++nt) {
+        const float4 k = *reinterpret_cast<const float4*>(&s.scale[w][x % G::NS][nt * 8 + 2 * t]);
+        f[nt][0] = fast_exp2(-k.y);
+        f[nt][1] = fast_exp2(-k.w);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float4 k = s.scale[w][x & 1][nt * 8 + 2 * t + e];
-          f[nt][e] = k.z;
-#pragma unroll
-          for (int r = 0; r < 2; ++r) sc[nt][2 * r + e] = fmaf(sc[nt][2 * r + e], factor[r] * k.x, k.y);
+        for (int r = 0; r < 2; ++r) {
+          sc[nt][2 * r] = fmaf(sc[nt][2 * r], factor[r] * k.x, k.y);
+          sc[nt][2 * r + 1] = fmaf(sc[nt][2 * r + 1], factor[r] * k.z, k.w);
         }
+      }
       const int32_t j0 = st.first + x * KEYS;
       if (j0 + WARP > min(st.see[0], st.see[1]))  // some key is hidden from a row
 #pragma unroll

@@ -2,11 +2,7 @@
 //
 // Bound: the tensor cores, as in the kernel of 16 bits (attn_tile.cu), whose frame this is. What the codes change:
 //   scores   k's tiles are operands as they are: 8-bit products (kind::f8f6f4) run at twice the 16-bit rate, and q is a
-//            sum of PIECES 8-bit values, each the rounding of what the ones before leave: e4m3 first, then e5m2, whose
-//            range goes on below (the residual of a rounding to 4 bits is at most 8 units of a bf16's last place, which
-//            3 bits hold). A row is scaled by a power of two to a largest element in [2^7, 2^8). Two pieces hold a bf16
-//            element exactly where it is at least 2^-13 of the row's largest, three an fp16 element; a smaller one is
-//            off by 2^-21 of the largest at most. Two passes over k's codes cost what one 16-bit product does; k is never
+//            sum of 8-bit pieces (kv8.cuh). Two passes over k's codes cost what one 16-bit product does; k is never
 //            converted.
 //   out      v's tiles become halves: a warpgroup reads a tile's codes, loaded into the upper half of its ring slot, and
 //            writes the halves over the whole slot, in the swizzle that the products read. 8 + 16 + 32 KB of shared
@@ -31,25 +27,13 @@ __device__ __forceinline__ void mma_ss8(uint32_t d, uint64_t a, uint64_t b, uint
 __host__ __device__ constexpr uint32_t idesc8_of(int M, int N, bool e5m2) {
   return (1u << 4) | ((e5m2 ? 1u : 0u) << 7) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
-// Two values to e5m2, x in the low byte, and back.
-__device__ __forceinline__ uint32_t e5m2x2(float x, float y) {
-  uint16_t w;
-  asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(w) : "f"(y), "f"(x));
-  return w;
-}
-__device__ __forceinline__ float2 e5m2_values(uint32_t two) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
-  return values2(h);
-}
-
 template <int DT_, int D_, int NT_, int KEYS_, int KS_, int VS_>
 struct Tile8Shape {
   static constexpr int DT = DT_, D = D_, NT = NT_, KEYS = KEYS_;
   static constexpr int KS = KS_, VS = VS_;     // ring slots of k and of v
   static constexpr int OTHERS = 256;           // mma, load and idle warps; the converting warpgroup
   static constexpr int OTHER_REGS = NT == 2 ? 56 : 88, SOFT_REGS = NT == 2 ? 200 : 232;
-  static constexpr int PIECES = DT == DT_BF16 ? 2 : 3;
+  static constexpr int PIECES = q_pieces<DT>();
   static constexpr int QP = 128 * D;           // bytes of a piece of a q tile
   static constexpr int KB = KEYS * D;          // ... of a k tile
   static constexpr int VB = KEYS * D * 2;      // ... of a v tile as halves; its codes come to the upper half
@@ -324,32 +308,21 @@ struct Tile8 : TileFrame<Tile8<C>, C> {
         float y[8];
         if (x * 128 + row >= f.rows) v[e] = make_uint4(0, 0, 0, 0);
         unpack<DT>(v[e], y);
-        // the exponent field of the row's largest magnitude: of the bits, so that a NaN counts as the largest
         uint32_t bits = 0;
 #pragma unroll
         for (int k = 0; k < 8; ++k) bits = max(bits, __float_as_uint(y[k]) & 0x7fffffffu);
 #pragma unroll
         for (int o = CH / 2; o > 0; o >>= 1) bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, o));
-        const int shift = 134 - (int)min(max(bits >> 23, 14u), 254u);
-        const float up = bits >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : exp2_int(shift);  // a row that is not finite: all NaN
+        const float up = q_up(bits);
 #pragma unroll
         for (int k = 0; k < 8; ++k) y[k] *= up;
         const int ch = c >> 1;
         char* dst = s.q + x * PIECES * QP + (ch / (CW / 16)) * QPART + row * CW +
                     ((ch % (CW / 16) ^ (CW == 128 ? row & 7 : (row >> 1) & 3)) << 4) + (c & 1) * 8;
 #pragma unroll
-        for (int piece = 0; piece < PIECES; ++piece) {
-          uint32_t u[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            u[k] = piece == 0 ? codes2(y[2 * k], y[2 * k + 1]) : e5m2x2(y[2 * k], y[2 * k + 1]);
-            const float2 held = piece == 0 ? values2(halves2(u[k])) : e5m2_values(u[k]);
-            y[2 * k] -= held.x;
-            y[2 * k + 1] -= held.y;
-          }
-          *reinterpret_cast<uint2*>(dst + piece * QP) = make_uint2(u[0] | u[1] << 16, u[2] | u[3] << 16);
-        }
-        if (c == 0) s.q_factor[x * 128 + row] = exp2_int(-shift);
+        for (int piece = 0; piece < PIECES; ++piece)
+          *reinterpret_cast<uint2*>(dst + piece * QP) = make_uint2(q_piece(y, piece), q_piece(y + 4, piece));
+        if (c == 0) s.q_factor[x * 128 + row] = q_down(bits);
       }
     }
     fence_async();

@@ -52,6 +52,43 @@ __device__ __forceinline__ float code_value(const void* cache, int64_t at) {
   return values2(halves2(reinterpret_cast<const uint8_t*>(cache)[at])).x;
 }
 
+// Two values to e5m2, x in the low byte, and back.
+__device__ __forceinline__ uint32_t e5m2x2(float x, float y) {
+  uint16_t w;
+  asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(w) : "f"(y), "f"(x));
+  return w;
+}
+__device__ __forceinline__ float2 e5m2_values(uint32_t two) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e5m2x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
+  return values2(h);
+}
+
+// A row of q beside codes, in 8-bit products: the row times a power of two that takes its largest element to [2^7, 2^8),
+// as a sum of 8-bit pieces, each the rounding of what the ones before leave: e4m3 first, then e5m2, whose range goes on
+// below (a rounding to 4 bits leaves at most 8 units of a bf16's last place, which 3 bits hold). Two pieces hold a bf16
+// element exactly where it is at least 2^-13 of the row's largest, three an fp16 element; a smaller one is off by 2^-21
+// of the largest at most.
+template <int DT> __host__ __device__ constexpr int q_pieces() { return DT == DT_BF16 ? 2 : 3; }
+// bits: of the largest magnitude as fp32 (a NaN counts as the largest). A row that is not finite becomes all NaN.
+__device__ __forceinline__ int q_shift(uint32_t bits) { return 134 - (int)min(max(bits >> 23, 14u), 254u); }
+__device__ __forceinline__ float q_up(uint32_t bits) {
+  return bits >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : exp2_int(q_shift(bits));
+}
+__device__ __forceinline__ float q_down(uint32_t bits) { return exp2_int(-q_shift(bits)); }
+// The next piece of four elements, which become what it leaves of them.
+__device__ __forceinline__ uint32_t q_piece(float* y, int piece) {
+  uint32_t u[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    u[k] = piece == 0 ? codes2(y[2 * k], y[2 * k + 1]) : e5m2x2(y[2 * k], y[2 * k + 1]);
+    const float2 held = piece == 0 ? values2(halves2(u[k])) : e5m2_values(u[k]);
+    y[2 * k] -= held.x;
+    y[2 * k + 1] -= held.y;
+  }
+  return u[0] | u[1] << 16;
+}
+
 __device__ __forceinline__ uint8_t* scale_at(const PagedScale& s, int64_t page, int h, int block) {
   return s.base + page * s.page + (int64_t)h * s.head + (int64_t)block * s.block;
 }
