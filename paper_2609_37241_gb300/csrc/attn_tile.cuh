@@ -96,6 +96,7 @@ __host__ __device__ constexpr uint32_t idesc_of(int M, int N, bool b_mn) {
 }
 
 #define TC_R8(r, k) "=r"(r[k]), "=r"(r[k + 1]), "=r"(r[k + 2]), "=r"(r[k + 3]), "=r"(r[k + 4]), "=r"(r[k + 5]), "=r"(r[k + 6]), "=r"(r[k + 7])
+#define TC_W8(r, k) "+r"(r[k]), "+r"(r[k + 1]), "+r"(r[k + 2]), "+r"(r[k + 3]), "+r"(r[k + 4]), "+r"(r[k + 5]), "+r"(r[k + 6]), "+r"(r[k + 7])
 #define TC_I8(r, k) "r"(r[k]), "r"(r[k + 1]), "r"(r[k + 2]), "r"(r[k + 3]), "r"(r[k + 4]), "r"(r[k + 5]), "r"(r[k + 6]), "r"(r[k + 7])
 // 32 columns of the warp's 32 lanes: lane i, register k = column k.
 __device__ __forceinline__ void tc_ld32(uint32_t at, uint32_t* r) {
@@ -109,6 +110,11 @@ __device__ __forceinline__ void tc_st32(uint32_t at, const uint32_t* r) {
                :: TC_I8(r, 0), TC_I8(r, 8), TC_I8(r, 16), TC_I8(r, 24), "r"(at) : "memory");
 }
 
+// The wait, as what brings these registers' values.
+__device__ __forceinline__ void tc_wait_ld32(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : TC_W8(r, 0), TC_W8(r, 8), TC_W8(r, 16), TC_W8(r, 24) :: "memory");
+}
 __device__ __forceinline__ void tc_st16(uint32_t at, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
                :: TC_I8(r, 0), TC_I8(r, 8), "r"(at) : "memory");
@@ -546,13 +552,13 @@ struct TileFrame : TileShape<C> {
     typename K::Other other;
     bool ok = true;
     if (warp < MMA_WARP) {
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(C::SOFT_REGS));
+      if constexpr (C::SOFT_REGS > T::LAUNCH_REGS) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(C::SOFT_REGS));
       Soft so;
       fragments<true>(p, s, a, [&](const Frag& f, const Frag* next) {
         ok = soft_fragment(p, s, tmem, f, next, warp / 4, so, ok, slots, counters);
       });
     } else {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(C::OTHER_REGS));
+      if constexpr (C::SOFT_REGS > T::LAUNCH_REGS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(C::OTHER_REGS));
       const bool one = elect_one();
       fragments<false>(p, s, a, [&](const Frag& f, const Frag*) {
         if (f.limit > 0 && ok) ok = K::work(p, mk, mv, s, tmem, f, warp, other, one);
@@ -563,7 +569,7 @@ struct TileFrame : TileShape<C> {
     // the way out: every copy and product of the block has to be done before its memory is given back
     K::leave(p, s, warp, other, ok);
     if (warp >= MMA_WARP && warp < MMA_WARP + NT) {
-      if (elect_one()) tc_commit(smem_at(&s.drain));
+      if (elect_one()) tc_commit(smem_at(&s.drain));  // warps without products of their own commit nothing, at once
       mb_drain(smem_at(&s.drain), 0);
     }
     __syncwarp();

@@ -149,14 +149,18 @@ __global__ void __launch_bounds__(kThreads) rope_paged8_generic_kernel(const Rop
 
 // ---------------------------------------------------------------- 16-byte aligned rows
 // A head-row by LPG lanes with two vectors of eight elements each (rope_paged.cuh), GW head-rows per warp at a time,
-// PASS times: ROWS rows of one head whose loads are issued together and whose values stay in registers between the
-// largest magnitude and the codes. Teams:
+// PASS times: ROWS rows of one head whose loads are issued together and whose values stay in shared memory between the
+// largest magnitude and the codes (in registers they left an SM twelve warps). Teams:
 //   TEAM 1  blocks of at most ROWS rows. A warp looks a window of tokens over and takes whole runs, as many as its
 //           rows hold: 16 decode steps or a block of a prompt cost the same round of loads.
 //   TEAM 4  larger blocks. The thread block's warps share a run, TEAM * ROWS rows at a time; a longer one is read and
 //           rotated twice.
-// Thread blocks [0, kv_blocks) do this, the others rotate q: items of `rpi` heads of a token per warp, as
-// rope_paged.cu.
+// Q: thread blocks past kv_blocks rotate q, items of a head per lane group as rope_paged.cu. Calls of many tokens have q
+// rotated by that file's kernel, in a launch before this one (rope_paged8_plan).
+//
+// Measured on a GB300 (32 + 8 + 8 heads of 128, bf16, blocks of 16): one prompt of 8192 tokens 50 us, of which q's 134 MB
+// take 21; the append is bound by its chain of loads, rotation (a token's sines and cosines once per kv head), maximum
+// and codes.
 constexpr int kRope8Threads = 128;
 
 template <int DT, int LPG, bool INTER, int TEAM>
@@ -164,6 +168,7 @@ struct Append8 {
   static constexpr int GW = 32 / LPG, PASS = LPG == 4 ? 2 : 4, ROWS = GW * PASS, CAP = TEAM * ROWS;
   static_assert(TEAM > 1 || CAP <= 16, "a warp's look at its tokens reaches past its rows");
   struct Smem {
+    float4 x[4][PASS * 4][32];  // the lanes' values between the largest magnitude and the codes, 16 per row
     float top[4][16];
     int32_t grown[4][16];
   };
@@ -180,51 +185,75 @@ struct Append8 {
     return v;
   }
 
-  // Rows r(j) < n of the run tokens a + r: their values and, in m[j], their largest magnitudes (0: no such row, or
-  // skipped for its position: live[j] is false).
-  template <class Row>
-  static __device__ __forceinline__ void values(const RopePaged8Params& p8, const Lane& ln, int64_t a, int n, int hh, Row row,
-                                                float (*x)[16], float* m, bool* live) {
+  // Rows r(j) < n of the run tokens a + r: their values, to the lane's words of s.x, and each row's largest magnitude to
+  // m(j, .) (0: no such row, or skipped for its position). Returns the rows that count, a bit each. All loads are
+  // issued first and wait in the same words; then a row at a time, so that few registers leave the SM many warps.
+  template <class Row, class Most>
+  static __device__ __forceinline__ unsigned values(const RopePaged8Params& p8, Smem& s, const Lane& ln, int64_t a, int n, int hh,
+                                                    Row row, Most most) {
     const RopePagedParams& p = p8.r;
     const bool is_v = hh >= p.Hq + p.Hkv;
-    uint4 lo[PASS], hi[PASS];
+    uint4* mine = reinterpret_cast<uint4*>(&s.x[threadIdx.x >> 5][0][threadIdx.x & 31]);  // word i: mine[32 i]
     int32_t pos[PASS];
+    {
+      uint4 lo[PASS], hi[PASS];
 #pragma unroll
-    for (int j = 0; j < PASS; ++j) {
-      const int64_t t = a + min(row(j), n - 1);
-      const char* src = paged_src(p, t, hh);
-      lo[j] = ld16(src + ln.va * 2);
-      hi[j] = ld16(src + ln.vb * 2);
-      pos[j] = p.pos[t];
+      for (int j = 0; j < PASS; ++j) {
+        const int64_t t = a + min(row(j), n - 1);
+        const char* src = paged_src(p, t, hh);
+        lo[j] = ld16(src + ln.va * 2);
+        hi[j] = ld16(src + ln.vb * 2);
+        pos[j] = p.pos[t];
+      }
+#pragma unroll
+      for (int j = 0; j < PASS; ++j) {
+        mine[128 * j] = lo[j];
+        mine[128 * j + 32] = hi[j];
+      }
     }
+    unsigned live = 0;
 #pragma unroll
     for (int j = 0; j < PASS; ++j) {
-      const bool good = pos_valid(pos[j]);
-      live[j] = row(j) < n && good;
-      if (row(j) < n && !good && ln.l == 0) atomicOr(p.err, kErrPos);
+      if (row(j) >= n) continue;
+      if (pos_valid(pos[j])) live |= 1u << j;
+      else if (ln.l == 0) atomicOr(p.err, kErrPos);
+    }
+#pragma unroll 1
+    for (int j = 0; j < PASS; ++j) {
+      const uint4 lo = mine[128 * j], hi = mine[128 * j + 32];
+      float x[16];
       if (is_v) {
-        unpack<DT>(lo[j], x[j]);
-        unpack<DT>(hi[j], x[j] + 8);
+        unpack<DT>(lo, x);
+        unpack<DT>(hi, x + 8);
       } else {
+        int32_t at = pos[0];
+#pragma unroll
+        for (int k = 1; k < PASS; ++k)
+          if (j == k) at = pos[k];
         RopeAngles an;
-        paged_angles(p, good ? pos[j] : 0, ln.fq, &an);
-        if (p.gamma_k)
-          paged_row_math<DT, LPG, true, INTER>(p, lo[j], hi[j], p.gamma_k, an, ln.on, ln.rot, ln.va, ln.vb, x[j], x[j] + 8);
-        else
-          paged_row_math<DT, LPG, false, INTER>(p, lo[j], hi[j], nullptr, an, ln.on, ln.rot, ln.va, ln.vb, x[j], x[j] + 8);
+        paged_angles(p, live >> j & 1u ? at : 0, ln.fq, &an);
+        if (p.gamma_k) paged_row_math<DT, LPG, true, INTER>(p, lo, hi, p.gamma_k, an, ln.on, ln.rot, ln.va, ln.vb, x, x + 8);
+        else paged_row_math<DT, LPG, false, INTER>(p, lo, hi, nullptr, an, ln.on, ln.rot, ln.va, ln.vb, x, x + 8);
       }
       float top = 0.f;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[j][e]));
-      m[j] = group_max(ln.on && live[j] ? top : 0.f);
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[e]));
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<float4*>(&mine[128 * j + 32 * e]) = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+      most(j, group_max(ln.on && (live >> j & 1u) ? top : 0.f));
     }
+    return live;
   }
 
-  static __device__ __forceinline__ void put(const Lane& ln, uint8_t* row, const float* x, int e) {
+  static __device__ __forceinline__ void put(const Smem& s, const Lane& ln, uint8_t* row, int j, int e) {
     const float f = exp2_int(-e);
     float y[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) y[i] = x[i] * f;
+    for (int i = 0; i < 4; ++i) {
+      const float4 v = s.x[threadIdx.x >> 5][4 * j + i][threadIdx.x & 31];
+      y[4 * i] = v.x * f; y[4 * i + 1] = v.y * f; y[4 * i + 2] = v.z * f; y[4 * i + 3] = v.w * f;
+    }
     const uint2 a = make_uint2(codes4(y), codes4(y + 4)), b = make_uint2(codes4(y + 8), codes4(y + 12));
     if (ln.vb == ln.va + 8) {
       st16(row + ln.va, make_uint4(a.x, a.y, b.x, b.y));
@@ -302,12 +331,9 @@ struct Append8 {
         if (has[j] && in_block(p8, at[j]) > row(j) - first[j])  // the block was begun by an earlier call
           old[j] = scale_exp(*block_of(p8, is_v, at[j], h).scale);
       }
-      float x[PASS][16], m[PASS];
-      bool live[PASS];
-      values(p8, ln, a, n, hh, row, x, m, live);
-#pragma unroll
-      for (int j = 0; j < PASS; ++j)
-        if (ln.l == 0) s.top[w][row(j)] = has[j] ? m[j] : 0.f;
+      const unsigned live = values(p8, s, ln, a, n, hh, row, [&](int j, float top) {
+        if (ln.l == 0) s.top[w][row(j)] = row(j) < n ? top : 0.f;
+      });
       __syncwarp();
 #pragma unroll
       for (int j = 0; j < PASS; ++j) {
@@ -320,7 +346,7 @@ struct Append8 {
         if (!has[j]) continue;
         const Block8 blk = block_of(p8, is_v, at[j], h);
         if (lead && ln.l == 0) *blk.scale = (uint8_t)(e + 127);
-        if (live[j] && ln.on) put(ln, blk.row0 + in_block(p8, at[j]) * blk.row, x[j], e);
+        if ((live >> j & 1u) && ln.on) put(s, ln, blk.row0 + in_block(p8, at[j]) * blk.row, j, e);
       }
       __syncwarp();
       unsigned grown = __ballot_sync(0xffffffffu, lane < n && s.grown[w][min(lane, CAP - 1)] > 0);
@@ -361,14 +387,12 @@ struct Append8 {
         }
         const Block8 blk = block_of(p8, is_v, s0, h);
         const int old = at > 0 ? scale_exp(*blk.scale) : kScaleLo;
-        float x[PASS][16], m[PASS], top = 0.f;
-        bool live[PASS];
+        float top = 0.f;
+        unsigned live = 0;
         int c = 0;
         auto row = [&](int j) { return c * CAP + (j * TEAM + w) * GW + g; };
         for (; c * CAP < n; ++c) {
-          values(p8, ln, a, n, hh, row, x, m, live);
-#pragma unroll
-          for (int j = 0; j < PASS; ++j) top = fmaxf(top, m[j]);
+          live = values(p8, s, ln, a, n, hh, row, [&](int, float m) { top = fmaxf(top, m); });
         }
 #pragma unroll
         for (int o = 16; o >= LPG; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -379,10 +403,10 @@ struct Append8 {
         if (threadIdx.x == 0) *blk.scale = (uint8_t)(e + 127);
         const bool again = n > CAP;
         for (c = 0; c * CAP < n; ++c) {
-          if (again) values(p8, ln, a, n, hh, row, x, m, live);
+          if (again) live = values(p8, s, ln, a, n, hh, row, [](int, float) {});
 #pragma unroll
           for (int j = 0; j < PASS; ++j)
-            if (live[j] && ln.on) put(ln, blk.row0 + (int64_t)(at + row(j)) * blk.row, x[j], e);
+            if ((live >> j & 1u) && ln.on) put(s, ln, blk.row0 + (int64_t)(at + row(j)) * blk.row, j, e);
         }
         if (at > 0 && e > old) rescale(p8, blk, at, n, e - old, threadIdx.x, kRope8Threads);
       }
@@ -390,8 +414,8 @@ struct Append8 {
   }
 };
 
-template <int DT, int LPG, bool INTER, int TEAM, int R>
-__global__ void __launch_bounds__(kRope8Threads, 3) rope_paged8_kernel(const RopePaged8Params p8, const Rope8Grid grid) {
+template <int DT, int LPG, bool INTER, int TEAM, bool Q>
+__global__ void __launch_bounds__(kRope8Threads, 4) rope_paged8_kernel(const RopePaged8Params p8, const Rope8Grid grid) {
   using K = Append8<DT, LPG, INTER, TEAM>;
   __shared__ typename K::Smem smem;
   pdl_prologue();
@@ -414,20 +438,15 @@ __global__ void __launch_bounds__(kRope8Threads, 3) rope_paged8_kernel(const Rop
     else K::window(p8, smem, ln, t0, end, hh);
     return;
   }
-  constexpr int GW = 32 / LPG;
+  if constexpr (!Q) return;
   const int64_t item = (int64_t)(blockIdx.x - grid.kv_blocks) * (kRope8Threads / 32) + threadIdx.x / 32;
   if (item >= p.T * p.ipt) return;
   const uint32_t tok = fast_div((uint32_t)item, p.ipt_magic, p.ipt_shift);
   const int64_t t = tok;
   const int first = (int)((uint32_t)item - tok * (uint32_t)p.ipt) * p.rpi, end = min(p.Hq, first + p.rpi);
-  const int hh0 = first + (threadIdx.x & 31) / LPG;
-  uint4 lo[R], hi[R];
-#pragma unroll
-  for (int j = 0; j < R; ++j) {  // groups past the item's end load its last row and drop it
-    const char* src = paged_src(p, t, min(hh0 + j * GW, end - 1));
-    lo[j] = ld16(src + ln.va * 2);
-    hi[j] = ld16(src + ln.vb * 2);
-  }
+  const int hh = first + (threadIdx.x & 31) / LPG;
+  const char* src = paged_src(p, t, min(hh, end - 1));  // groups past the item's end load its last row and drop it
+  const uint4 lo = ld16(src + ln.va * 2), hi = ld16(src + ln.vb * 2);
   const int32_t pos = p.pos[t];
   paged_freqs(p, lane, ln.rot, ln.fq);
   if (!pos_valid(pos)) {
@@ -436,38 +455,37 @@ __global__ void __launch_bounds__(kRope8Threads, 3) rope_paged8_kernel(const Rop
   }
   RopeAngles an;
   paged_angles(p, pos, ln.fq, &an);
-#pragma unroll
-  for (int j = 0; j < R; ++j) {
-    const int hh = hh0 + j * GW;
-    float x[8], y[8];
-    if (p.gamma_q) paged_row_math<DT, LPG, true, INTER>(p, lo[j], hi[j], p.gamma_q, an, ln.on, ln.rot, ln.va, ln.vb, x, y);
-    else paged_row_math<DT, LPG, false, INTER>(p, lo[j], hi[j], nullptr, an, ln.on, ln.rot, ln.va, ln.vb, x, y);
-    if (ln.on && hh < end) {
-      char* dst = row_ptr(p.q_out, t, p.o_rs, 2) + (int64_t)hh * p.D * 2;
-      st16(dst + ln.va * 2, pack<DT>(x));
-      st16(dst + ln.vb * 2, pack<DT>(y));
-    }
+  float x[8], y[8];
+  if (p.gamma_q) paged_row_math<DT, LPG, true, INTER>(p, lo, hi, p.gamma_q, an, ln.on, ln.rot, ln.va, ln.vb, x, y);
+  else paged_row_math<DT, LPG, false, INTER>(p, lo, hi, nullptr, an, ln.on, ln.rot, ln.va, ln.vb, x, y);
+  if (ln.on && hh < end) {
+    char* dst = row_ptr(p.q_out, t, p.o_rs, 2) + (int64_t)hh * p.D * 2;
+    st16(dst + ln.va * 2, pack<DT>(x));
+    st16(dst + ln.vb * 2, pack<DT>(y));
   }
 }
 
 template <int DT, int LPG, bool INTER>
 void pick_vec(KernelEntry* out) {
-  out->any_fn[0] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 1, 1>;
-  out->any_fn[1] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 1, 3>;
-  out->any_fn[2] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 4, 1>;
-  out->any_fn[3] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 4, 3>;
+  out->any_fn[0] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 1, true>;
+  out->any_fn[1] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 1, false>;
+  out->any_fn[2] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 4, true>;
+  out->any_fn[3] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 4, false>;
 }
 
 }  // namespace
 
-// The entry of a vector call; sets q's item split, the grid and its parts.
-int rope_paged8_plan(RopePaged8Params* p8, Rope8Grid* grid, int32_t* threads, int64_t* blocks, int32_t sms) {
+// The entry of a vector call; sets q's item split, the grid and its parts. *q_apart: q takes a launch of its own, with
+// rope_paged.cu's kernel, from kRope8Apart warps of q per SM on. Measured, one launch / two: 3333 tokens of 32 heads of 128
+// (175 warps) 30.6 / 33.6 us, 8192 tokens (431 warps) 60.4 / 49.8.
+constexpr int64_t kRope8Apart = 256;
+int rope_paged8_plan(RopePaged8Params* p8, Rope8Grid* grid, bool* q_apart, int32_t* threads, int64_t* blocks, int32_t sms) {
   RopePagedParams* p = &p8->r;
   const int lpg = p->D <= 64 ? 4 : p->D <= 128 ? 8 : 16, gw = 32 / lpg, rows = gw * (lpg == 4 ? 2 : 4);
   const bool team = p8->block.d > rows;
   constexpr int kWarps = kRope8Threads / 32;
-  RopeSplit r = rope_split(p->Hq, gw, 1);
-  if (p->T * r.ipt > 3 * (int64_t)sms) r = rope_split(p->Hq, gw, 3);
+  const RopeSplit r = rope_split(p->Hq, gw, 1);
+  *q_apart = p->T * r.ipt > kRope8Apart * sms;
   p->ipt = r.ipt;
   p->rpi = r.rpi;
   p->ipt_magic = r.magic;
@@ -477,8 +495,8 @@ int rope_paged8_plan(RopePaged8Params* p8, Rope8Grid* grid, int32_t* threads, in
   const int64_t kv = team ? units : (units + kWarps - 1) / kWarps;
   grid->kv_blocks = (int32_t)kv;
   *threads = kRope8Threads;
-  *blocks = kv + (p->T * r.ipt + kWarps - 1) / kWarps;
-  return (team ? 2 : 0) + (r.rpi > gw ? 1 : 0);
+  *blocks = kv + (*q_apart ? 0 : (p->T * r.ipt + kWarps - 1) / kWarps);
+  return (team ? 2 : 0) + (*q_apart ? 1 : 0);
 }
 
 bool rope_paged8_kernel(int32_t dtype, int32_t variant, int32_t D, int32_t R, bool qknorm, bool inter,
@@ -491,6 +509,9 @@ bool rope_paged8_kernel(int32_t dtype, int32_t variant, int32_t D, int32_t R, bo
       return false;
     }
     out->vec = 8;
+    KernelEntry q;
+    if (!rope_paged_kernel(dtype, variant, D, R, qknorm, inter, &q, why)) return false;
+    for (int k = 0; k < 4; ++k) out->q_fn[k] = q.any_fn[k];
     auto vec = [&](auto dt) {
       constexpr int DT = decltype(dt)::value;
       if (D <= 64) inter ? pick_vec<DT, 4, true>(out) : pick_vec<DT, 4, false>(out);
