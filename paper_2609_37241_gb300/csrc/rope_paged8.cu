@@ -194,6 +194,7 @@ struct Append8 {
     const RopePagedParams& p = p8.r;
     const bool is_v = hh >= p.Hq + p.Hkv;
     uint4* mine = reinterpret_cast<uint4*>(&s.x[threadIdx.x >> 5][0][threadIdx.x & 31]);  // word i: mine[32 i]
+    const int g = (threadIdx.x & 31) / LPG;
     int32_t pos[PASS];
     {
       uint4 lo[PASS], hi[PASS];
@@ -219,7 +220,7 @@ struct Append8 {
       else if (ln.l == 0) atomicOr(p.err, kErrPos);
     }
 #pragma unroll 1
-    for (int j = 0; j < PASS; ++j) {
+    for (int j = 0; j < PASS && row(j) - g < n; ++j) {
       const uint4 lo = mine[128 * j], hi = mine[128 * j + 32];
       float x[16];
       if (is_v) {
@@ -478,7 +479,7 @@ void pick_vec(KernelEntry* out) {
 // The entry of a vector call; sets q's item split, the grid and its parts. *q_apart: q takes a launch of its own, with
 // rope_paged.cu's kernel, from kRope8Apart warps of q per SM on. Measured, one launch / two: 3333 tokens of 32 heads of 128
 // (175 warps) 30.6 / 33.6 us, 8192 tokens (431 warps) 60.4 / 49.8.
-constexpr int64_t kRope8Apart = 256;
+constexpr int64_t kRope8Apart = 256, kRope8Small = 8;  // kRope8Small: warps per SM
 int rope_paged8_plan(RopePaged8Params* p8, Rope8Grid* grid, bool* q_apart, int32_t* threads, int64_t* blocks, int32_t sms) {
   RopePagedParams* p = &p8->r;
   const int lpg = p->D <= 64 ? 4 : p->D <= 128 ? 8 : 16, gw = 32 / lpg, rows = gw * (lpg == 4 ? 2 : 4);
@@ -490,7 +491,9 @@ int rope_paged8_plan(RopePaged8Params* p8, Rope8Grid* grid, bool* q_apart, int32
   p->rpi = r.rpi;
   p->ipt_magic = r.magic;
   p->ipt_shift = r.shift;
-  grid->window = 16;
+  // Tokens of a team's window: as many as a warp's rows; few tokens, whose runs may all be of one, in smaller windows for
+  // more warps. 64 decode steps of 32 + 8 + 8 heads of 128: see the file's head.
+  grid->window = p->T * 2 * p->Hkv <= 4 * kRope8Small * sms ? 4 : 16;
   const int64_t units = (p->T + grid->window - 1) / grid->window * 2 * p->Hkv;
   const int64_t kv = team ? units : (units + kWarps - 1) / kWarps;
   grid->kv_blocks = (int32_t)kv;
