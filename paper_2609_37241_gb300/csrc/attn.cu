@@ -99,6 +99,12 @@ __global__ void __launch_bounds__(kThreads) attn_generic_kernel(const PagedAttnP
 // 96 rows over 1000 keys 14.6 / 18.5, over 2000 17.8 / 19.8, 256 over 1000 20.7 / 22.8, 400 over 1000
 // 24.7 / 22.9; D 64, 210 over 2000 12.5 / 17.7; so there it is kRereadOne.
 constexpr int64_t kReread = 4000 * 128, kRereadOne = 20000 * 128;
+// Over caches held in 8 bits the kernel of few rows has half the bytes to read again, and the tile kernel has more to do
+// per tile: 32 requests of 32 rows over 8000 keys 175 / 225, of 48 rows over 3000 keys 111 / 120; 16 of 128 over 2000
+// 99 / 45; 8 of 128 over 2000 55 / 44; D 64, 16 of 64 over 3000 54 / 45, 64 of 32 over 6000 183 / 236; D 256, 8 of 32
+// over 4000 64 / 84. One request of 200 rows over 8000 keys 43 / 81, 400 over 4000 43 / 57, 512 over 2000 34 / 49, 800 over
+// 1000 35 / 33; D 64, 400 over 3000 28 / 28. Here the bound is one of keys read again, whatever D.
+constexpr int64_t kReread8 = 9000, kReread8One = 100000;
 
 // The lengths are on the device, so the choice goes by what T, B and the table's width (keys) leave
 // possible where every request has a row: both kernels, unless no request can then pass the bound, or there is
@@ -111,7 +117,7 @@ AttnPlan attn_plan(const AttnEntry& tile, int64_t T, int64_t B, int64_t G, int64
   const bool fits = tile.fn && G <= 128 && ps % 8 == 0 && (tile.keys % ps == 0 || ps % tile.keys == 0);
   const int64_t most = T > B ? T - B + 1 : 1;  // rows of a request, if every one has some
   AttnPlan pl;
-  pl.reread = ((B == 1 ? kRereadOne : kReread) + D - 1) / D;
+  pl.reread = tile.kv8 ? (B == 1 ? kReread8One : kReread8) : ((B == 1 ? kRereadOne : kReread) + D - 1) / D;
   pl.tile = fits && ((most * G + 15) / 16 - 1) * keys >= pl.reread;
   pl.rows = !pl.tile || B > 1;
   return pl;

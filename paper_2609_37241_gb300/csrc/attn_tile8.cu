@@ -494,6 +494,7 @@ struct Tile8 : TileFrame<Tile8<C>, C> {
 template <int DT, int D, int NT, int KEYS, int KS, int VS>
 void pick(AttnEntry* e) {
   attn_tile_pick<Tile8<Tile8Shape<DT, D, NT, KEYS, KS, VS>>>(e);
+  e->kv8 = true;
 }
 
 }  // namespace

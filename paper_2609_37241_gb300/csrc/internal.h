@@ -284,6 +284,7 @@ struct AttnEntry {
   int32_t threads = 0, smem = 0, per_sm = 0;
   int64_t slot_floats = 0;
   int32_t keys = 0, rows = 0;  // tile kernel: keys and rows of a tile
+  bool kv8 = false;            // ... over caches held in 8 bits
 };
 
 // Kernel entry (host stub address) plus its launch shape rule.

@@ -358,6 +358,19 @@ def test_attention_long(S, new, kv, D, ps, bt, dtype):
     check(b, ps, dt, D ** -0.5, out, lse)
 
 
+@pytest.mark.parametrize("kv", [[260, 385], [384, 400], [300, 527], [200, 1025], [416, 1039]])
+@pytest.mark.parametrize("D,ps,bt,G", [(64, 8, 8, 4), (64, 128, 32, 7), (128, 16, 16, 4), (128, 8, 2, 8), (128, 256, 128, 3),
+                                       (256, 64, 16, 4), (256, 16, 1, 2), (256, 128, 64, 4)])
+@pytest.mark.parametrize("dtype", ["BF16", "FP16"])
+def test_attention_tiles(S, kv, D, ps, bt, G, dtype):
+    """Requests of many rows whose keys end at, before and behind a tile's or a 16's border, from the first token on (kv as
+    many as rows: 300 and 260) or with fewer keys than rows (rows that see none), in pages below, of and above a tile."""
+    dt, g = getattr(S, dtype), np.random.default_rng(D + ps + sum(kv))
+    b = Q.batch(g, [260, 300], kv, G, 1, D, ps, bt, dt, tail=1)
+    out, lse = attend(S, b, G, 1, D, ps, bt, dt, D ** -0.5)
+    check(b, ps, dt, D ** -0.5, out, lse)
+
+
 @pytest.mark.parametrize("new", [1, 130])
 @pytest.mark.parametrize("what", ["nan", "inf"])
 def test_attention_row_not_finite(S, new, what):
