@@ -58,7 +58,7 @@ struct Tile8 : TileFrame<Tile8<C>, C> {
   static constexpr int QPART = 128 * CW, KPART = KEYS * CW;
   static constexpr int VHALF = KEYS * 128;           // bytes of 64 columns of halves
   static constexpr int LOAD_WARP = MMA_WARP + NT, CONVERT_WARP = MMA_WARP + 4;
-  static constexpr float kLeast = 0x1p-126f;         // a score's factor at least: masked scores are infinite, and 0 would make them NaN
+  static constexpr float kLeast = 0x1p-94f;          // a row's factor at least: masked scores are infinite, and one that 2^-32 takes to 0 would make them NaN
 
   static __device__ __forceinline__ void init(Smem& s) {
     for (int i = 0; i < KS; ++i) {
@@ -350,20 +350,20 @@ struct Tile8 : TileFrame<Tile8<C>, C> {
       auto pass = [&]() {
         if (turns && (x == 0 || t + 1 < t1)) turn_pass(x);
       };
-      float base = 0.f, sum = 0.f;
+      float base = 0.f;
+      F2 sum = f2_pack(0.f, 0.f);
       // numerators of half the tile's keys, to the columns of its scores; the turn ends inside the second half
       auto half = [&](int h) {
         uint32_t w[KEYS / 4];
 #pragma unroll
         for (int g = 0; g < KEYS / 32; ++g) {
           const int e0 = h * (KEYS / 2) + 16 * g;
-          F2 part[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
+          F2 part = f2_pack(0.f, 0.f);
           F2 mul, add;
           float out = 1.f;
           if (GROUPS) {
             const float4 k = scale[e0];
-            const float ck = fmaxf(c * k.x, kLeast);
-            mul = f2_pack(ck, ck);
+            mul = f2_pack(c * k.x, c * k.x);
             add = f2_pack(k.y - base, k.y - base);
             out = k.z;
           } else {
@@ -378,13 +378,11 @@ struct Tile8 : TileFrame<Tile8<C>, C> {
             f2_unpack(GROUPS ? f2_fma(z, mul, add) : f2_add(z, add), &u, &v);
             u = fast_exp2(u);
             v = fast_exp2(v);
-            if (GROUPS) part[i & 1] = f2_add(part[i & 1], f2_pack(u, v));
-            else part[i & 1] = f2_fma(f2_pack(u, v), f2_pack(scale[e].z, scale[e + 1].z), part[i & 1]);
+            if (GROUPS) part = f2_add(part, f2_pack(u, v));
+            else part = f2_fma(f2_pack(u, v), f2_pack(scale[e].z, scale[e + 1].z), part);
             w[8 * g + i] = ActType<DT_FP16>::pack2(u, v);
           }
-          float s0, s1;
-          f2_unpack(f2_add(part[0], part[1]), &s0, &s1);
-          sum = fmaf(s0 + s1, out, sum);
+          sum = f2_fma(part, f2_pack(out, out), sum);
           if (h == 1 && g == 0) pass();
         }
 #pragma unroll
@@ -394,7 +392,7 @@ struct Tile8 : TileFrame<Tile8<C>, C> {
         mb_arrive(smem_at(h == 0 ? &s.p_half[x] : &s.p_full[x]));
       };
       if (ok) {
-        if (t == t0) c = p.scale * kLog2e * s.q_factor[x * 128 + (threadIdx.x & 127)];  // what load_q wrote, behind s_full
+        if (t == t0) c = fmaxf(p.scale * kLog2e * s.q_factor[x * 128 + (threadIdx.x & 127)], kLeast);  // what load_q wrote, behind s_full
         tc_after();
 #pragma unroll
         for (int i = 0; i < KEYS / 32; ++i) tc_ld32(sc + i * 32, a + i * 32);
@@ -423,7 +421,7 @@ struct Tile8 : TileFrame<Tile8<C>, C> {
           const float z = fmaxf(top[0], top[1]);
           if (GROUPS) {
             const float4 k = scale[16 * g];
-            hi = fmaxf(hi, fmaf(z, fmaxf(c * k.x, kLeast), k.y));
+            hi = fmaxf(hi, fmaf(z, c * k.x, k.y));
           } else {
             hi = fmaxf(hi, z);
           }
@@ -449,7 +447,9 @@ struct Tile8 : TileFrame<Tile8<C>, C> {
         base = m == -INFINITY ? 0.f : m;
         half(0);  // its products start while the second half's numerators are made
         half(1);
-        l += sum;
+        float s0, s1;
+        f2_unpack(sum, &s0, &s1);
+        l += s0 + s1;
       } else {
         pass();
       }
