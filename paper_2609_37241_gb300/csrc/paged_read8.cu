@@ -58,7 +58,8 @@ __global__ void __launch_bounds__(kThreads) paged_read8_generic_kernel(const Pag
 
 // 16-byte aligned rows, D a multiple of 16: one warp per token, 16 codes per lane at a time, four of them in flight.
 // Bound: HBM (a byte read for two written); the search, the page and the scales are short chains of loads that other
-// warps of the SM cover.
+// warps of the SM cover. Measured on a GB300: 24 requests of 1024 to 8192 tokens, 8 heads of 128, fp16 123 us (5.9 TB/s,
+// 0.87 of the copy rate), 500 tokens 3.4 us.
 template <int DT>
 __global__ void __launch_bounds__(kThreads) paged_read8_vec_kernel(const PagedRead8Params p, const FastDiv vecs) {
   pdl_prologue();
