@@ -179,7 +179,7 @@ def attention_call(S, scm, g, new, kv, D, bt, dt, work):
     b = Q.batch(g, new, kv, 8, 2, D, 16, bt, dt)
     args = S.make_args(S.OP_PAGED_ATTN8, [b["q"], b["kc"], b["vc"], b["ks"], b["vs"], b["table"], b["cu"], b["kv"], work, b["out"],
                                           b["lse"]], scalar=D ** -0.5)
-    return b, args
+    return dict(b, work=work), args  # the arguments hold addresses: every tensor is kept
 
 
 def test_a_workspace_for_both_kinds_of_caches(S):
