@@ -281,7 +281,7 @@ typedef enum trident_variant {
 #define TRIDENT_DEVERR_POS 0x1u   /* a RoPE/KV position was outside [0, S) */
 #define TRIDENT_DEVERR_TIMEOUT 0x2u /* a kernel's bounded wait for its own bulk copies ran
                                        out; that block's outputs were not written */
-#define TRIDENT_DEVERR_SLOT 0x4u  /* ROPE_PAGED_KV: a slot was outside the cache */
+#define TRIDENT_DEVERR_SLOT 0x4u  /* paged ROPE ops: a slot was outside the cache */
 #define TRIDENT_DEVERR_PAGES 0x8u /* PAGE_MAP: the call's lengths do not fit (pages, table, rows) */
 #define TRIDENT_DEVERR_TABLE 0x10u /* a page number, cu_q or kv_len out of range */
 
@@ -333,15 +333,18 @@ typedef struct trident_spec_desc {
   int32_t dtype;                    /* activation dtype (PAGE_MAP: TRIDENT_I32)           */
   int32_t rank;                     /* rank of slot 0 (2 or 3 for the norms, SWIGLU and
                                        the pointwise ops,
-                                       3 for ROPE ops and PAGED_ATTN, 2 for the chains,
-                                       1 for PAGE_MAP)                                    */
+                                       3 for ROPE ops and paged attention, 2 for the
+                                       chains, 1 for PAGE_MAP, 4 for PAGED_READ8)         */
   int32_t layout;                   /* trident_layout                                    */
   int64_t fixed[TRIDENT_MAX_FIXED]; /* fixed sizes: ADD_RMSNORM, RMSNORM {H}; SWIGLU {I};
                                        SILU, ADD, NEG, MASKED_FILL {W};
                                        ROPE ops {Hq, Hkv, D, S};
                                        chains {H, Hq, Hkv, D, S, I};
                                        paged ROPE ops {Hq, Hkv, D, R, ps};
-                                       PAGED_ATTN {Hq, Hkv, D, ps}; unused entries 0      */
+                                       PAGED_ATTN {Hq, Hkv, D, ps};
+                                       paged ROPE ops into 8-bit caches {Hq, Hkv, D, R, ps, bt};
+                                       PAGED_READ8 {Hkv, D, ps, bt};
+                                       PAGED_ATTN8 {Hq, Hkv, D, ps, bt}; unused entries 0 */
   int64_t tok_lo, tok_hi;           /* inclusive token-count bucket, 1 <= lo <= hi       */
   int32_t align_bytes;              /* 16: every pointer and every outer stride 16-byte
                                        aligned (i32 tensors excepted: read per element);
@@ -573,7 +576,7 @@ int32_t trident_scm_invoke_tree(trident_scm_t* scm, const trident_node* nodes, i
  * hook). Errors: ERR_INVALID (scm NULL). */
 int32_t trident_scm_set_tree_hook(trident_scm_t* scm, trident_tree_hook hook, void* user);
 
-/* Elements of the workspace (slot `work`) that calls of PAGED_ATTN version `index` need, from
+/* Elements of the workspace (slot `work`) that calls of PAGED_ATTN or PAGED_ATTN8 version `index` need, from
  * the version's sizes and the device's SM count (calls of any length and number of requests fit).
  * What a launch needs is fixed when the specialisation is built (§3.3), and a hit allocates
  * nothing, so the caller holds the workspace.
