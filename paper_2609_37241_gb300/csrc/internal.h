@@ -301,7 +301,6 @@ struct KernelEntry {
   const void* fn_large = nullptr;  // RoPE: the bulk-copy entry (rope_plan chooses)
   const void* any_fn[4] = {};      // RoPE versions of the generic kind: rope_any_kernel (two, or NULL); paged
                                    // RoPE: rope_paged_kernel by rows per lane group
-  const void* q_fn[4] = {};        // paged RoPE into 8-bit caches: rope_paged_kernel, for q alone
   const void* fn_mid = nullptr;    // RoPE: two head-rows per lane group
   const void* fn_blocks = nullptr;  // RoPE, D 64: fn for blocks of 128 or 256 threads
   const void* pw_fn[kPwEntries] = {};  // elementwise, by PointwiseEntry
@@ -422,7 +421,7 @@ int64_t attn_slots_floats(const AttnEntry& e, int32_t sms);
 bool paged_attn_kernel(int32_t dtype, int32_t variant, int32_t D, bool kv8, KernelEntry* out, const char** why);
 bool rope_paged8_kernel(int32_t dtype, int32_t variant, int32_t D, int32_t R, bool qknorm, bool inter,
                         KernelEntry* out, const char** why);
-int rope_paged8_plan(RopePaged8Params* p, Rope8Grid* grid, bool* q_apart, int32_t* threads, int64_t* blocks, int32_t sms);
+int rope_paged8_plan(RopePaged8Params* p, Rope8Grid* grid, int32_t* threads, int64_t* blocks, int32_t sms);
 bool paged_read8_kernel(int32_t dtype, int32_t variant, int32_t D, KernelEntry* out, const char** why);
 const void* empty_kernel_entry();  // the latency-floor probe's kernel (does nothing)
 

@@ -156,13 +156,14 @@ __global__ void __launch_bounds__(kThreads) rope_paged8_generic_kernel(const Rop
 //           rows hold: 16 decode steps or a block of a prompt cost the same round of loads.
 //   TEAM 4  larger blocks. The thread block's warps share a run, TEAM * ROWS rows at a time; a longer one is read and
 //           rotated twice.
-// Q: thread blocks past kv_blocks rotate q, items of a head per lane group as rope_paged.cu. Calls of many tokens have q
-// rotated by that file's kernel, in a launch before this one (rope_paged8_plan).
+// Thread blocks past kv_blocks rotate q, items of R heads per lane group as rope_paged.cu. They come in as the append's
+// blocks end: that waits for its chains, q for the memory.
 //
 // Measured on a GB300 (32 + 8 + 8 heads of 128, bf16, blocks of 16): 64 decode steps with q/k norm 4.5 us (windows of 16
-// tokens, four rows after one another per warp: 7.7), one prompt of 8192 tokens 49 us (0.55 of the copy rate), of which
-// q's 134 MB take 21; the append is bound by its chain of loads, rotation (a token's sines and cosines once per kv head),
-// maximum and codes. 3333 tokens, half of the head, blocks of 32: 32 us.
+// tokens, four rows after one another per warp: 7.7), one prompt of 8192 tokens 44 us (0.62 of the copy rate; q in a launch
+// of its own 49, append blocks spread among q's 45), of which q's 134 MB would take 21 alone; the append is bound by its
+// chain of loads, rotation (a token's sines and cosines once per kv head), maximum and codes. 3333 tokens, half of the
+// head, blocks of 32: 25 us (one head of q per lane group 32, three 26).
 constexpr int kRope8Threads = 128;
 
 template <int DT, int LPG, bool INTER, int TEAM>
@@ -417,7 +418,7 @@ struct Append8 {
   }
 };
 
-template <int DT, int LPG, bool INTER, int TEAM, bool Q>
+template <int DT, int LPG, bool INTER, int TEAM, int R>
 __global__ void __launch_bounds__(kRope8Threads, 4) rope_paged8_kernel(const RopePaged8Params p8, const Rope8Grid grid) {
   using K = Append8<DT, LPG, INTER, TEAM>;
   __shared__ typename K::Smem smem;
@@ -430,7 +431,7 @@ __global__ void __launch_bounds__(kRope8Threads, 4) rope_paged8_kernel(const Rop
   ln.on = l == lane;
   ln.rot = lane < p.R / 16;
   lane_vectors<INTER>(p, lane, &ln.va, &ln.vb);
-  if (blockIdx.x < grid.kv_blocks) {
+  if (blockIdx.x < (unsigned)grid.kv_blocks) {
     const int64_t unit = TEAM > 1 ? blockIdx.x : (int64_t)blockIdx.x * (kRope8Threads / 32) + threadIdx.x / 32;
     const int64_t win = unit / (2 * p.Hkv), t0 = win * grid.window;
     if (t0 >= p.T) return;
@@ -441,15 +442,20 @@ __global__ void __launch_bounds__(kRope8Threads, 4) rope_paged8_kernel(const Rop
     else K::window(p8, smem, ln, t0, end, hh);
     return;
   }
-  if constexpr (!Q) return;
+  constexpr int GW = 32 / LPG;
   const int64_t item = (int64_t)(blockIdx.x - grid.kv_blocks) * (kRope8Threads / 32) + threadIdx.x / 32;
   if (item >= p.T * p.ipt) return;
   const uint32_t tok = fast_div((uint32_t)item, p.ipt_magic, p.ipt_shift);
   const int64_t t = tok;
   const int first = (int)((uint32_t)item - tok * (uint32_t)p.ipt) * p.rpi, end = min(p.Hq, first + p.rpi);
-  const int hh = first + (threadIdx.x & 31) / LPG;
-  const char* src = paged_src(p, t, min(hh, end - 1));  // groups past the item's end load its last row and drop it
-  const uint4 lo = ld16(src + ln.va * 2), hi = ld16(src + ln.vb * 2);
+  const int hh0 = first + (threadIdx.x & 31) / LPG;
+  uint4 lo[R], hi[R];
+#pragma unroll
+  for (int j = 0; j < R; ++j) {  // groups past the item's end load its last row and drop it
+    const char* src = paged_src(p, t, min(hh0 + j * GW, end - 1));
+    lo[j] = ld16(src + ln.va * 2);
+    hi[j] = ld16(src + ln.vb * 2);
+  }
   const int32_t pos = p.pos[t];
   paged_freqs(p, lane, ln.rot, ln.fq);
   if (!pos_valid(pos)) {
@@ -458,37 +464,40 @@ __global__ void __launch_bounds__(kRope8Threads, 4) rope_paged8_kernel(const Rop
   }
   RopeAngles an;
   paged_angles(p, pos, ln.fq, &an);
-  float x[8], y[8];
-  if (p.gamma_q) paged_row_math<DT, LPG, true, INTER>(p, lo, hi, p.gamma_q, an, ln.on, ln.rot, ln.va, ln.vb, x, y);
-  else paged_row_math<DT, LPG, false, INTER>(p, lo, hi, nullptr, an, ln.on, ln.rot, ln.va, ln.vb, x, y);
-  if (ln.on && hh < end) {
-    char* dst = row_ptr(p.q_out, t, p.o_rs, 2) + (int64_t)hh * p.D * 2;
-    st16(dst + ln.va * 2, pack<DT>(x));
-    st16(dst + ln.vb * 2, pack<DT>(y));
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    const int hh = hh0 + j * GW;
+    float x[8], y[8];
+    if (p.gamma_q) paged_row_math<DT, LPG, true, INTER>(p, lo[j], hi[j], p.gamma_q, an, ln.on, ln.rot, ln.va, ln.vb, x, y);
+    else paged_row_math<DT, LPG, false, INTER>(p, lo[j], hi[j], nullptr, an, ln.on, ln.rot, ln.va, ln.vb, x, y);
+    if (ln.on && hh < end) {
+      char* dst = row_ptr(p.q_out, t, p.o_rs, 2) + (int64_t)hh * p.D * 2;
+      st16(dst + ln.va * 2, pack<DT>(x));
+      st16(dst + ln.vb * 2, pack<DT>(y));
+    }
   }
 }
 
 template <int DT, int LPG, bool INTER>
 void pick_vec(KernelEntry* out) {
-  out->any_fn[0] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 1, true>;
-  out->any_fn[1] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 1, false>;
-  out->any_fn[2] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 4, true>;
-  out->any_fn[3] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 4, false>;
+  out->any_fn[0] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 1, 1>;
+  out->any_fn[1] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 1, 4>;
+  out->any_fn[2] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 4, 1>;
+  out->any_fn[3] = (const void*)rope_paged8_kernel<DT, LPG, INTER, 4, 4>;
 }
 
 }  // namespace
 
-// The entry of a vector call; sets q's item split, the grid and its parts. *q_apart: q takes a launch of its own, with
-// rope_paged.cu's kernel, from kRope8Apart warps of q per SM on. Measured, one launch / two: 3333 tokens of 32 heads of 128
-// (175 warps) 30.6 / 33.6 us, 8192 tokens (431 warps) 60.4 / 49.8.
-constexpr int64_t kRope8Apart = 256, kRope8Small = 8;  // kRope8Small: warps per SM
-int rope_paged8_plan(RopePaged8Params* p8, Rope8Grid* grid, bool* q_apart, int32_t* threads, int64_t* blocks, int32_t sms) {
+// The entry of a vector call; sets q's item split (the rule of rope_paged.cu: items of one head per lane group where
+// they do not fill the GPU), the grid and its parts.
+constexpr int64_t kRope8Small = 8;  // warps per SM
+int rope_paged8_plan(RopePaged8Params* p8, Rope8Grid* grid, int32_t* threads, int64_t* blocks, int32_t sms) {
   RopePagedParams* p = &p8->r;
   const int lpg = p->D <= 64 ? 4 : p->D <= 128 ? 8 : 16, gw = 32 / lpg, rows = gw * (lpg == 4 ? 2 : 4);
   const bool team = p8->block.d > rows;
   constexpr int kWarps = kRope8Threads / 32;
-  const RopeSplit r = rope_split(p->Hq, gw, 1);
-  *q_apart = p->T * r.ipt > kRope8Apart * sms;
+  RopeSplit r = rope_split(p->Hq, gw, 1);
+  if (p->T * r.ipt > 3 * (int64_t)sms) r = rope_split(p->Hq, gw, 4);
   p->ipt = r.ipt;
   p->rpi = r.rpi;
   p->ipt_magic = r.magic;
@@ -497,11 +506,11 @@ int rope_paged8_plan(RopePaged8Params* p8, Rope8Grid* grid, bool* q_apart, int32
   // more warps. 64 decode steps of 32 + 8 + 8 heads of 128: see the file's head.
   grid->window = p->T * 2 * p->Hkv <= 4 * kRope8Small * sms ? 4 : 16;
   const int64_t units = (p->T + grid->window - 1) / grid->window * 2 * p->Hkv;
-  const int64_t kv = team ? units : (units + kWarps - 1) / kWarps;
+  const int64_t kv = team ? units : (units + kWarps - 1) / kWarps, q = (p->T * r.ipt + kWarps - 1) / kWarps;
   grid->kv_blocks = (int32_t)kv;
   *threads = kRope8Threads;
-  *blocks = kv + (*q_apart ? 0 : (p->T * r.ipt + kWarps - 1) / kWarps);
-  return (team ? 2 : 0) + (*q_apart ? 1 : 0);
+  *blocks = kv + q;
+  return (team ? 2 : 0) + (r.rpi > gw ? 1 : 0);
 }
 
 bool rope_paged8_kernel(int32_t dtype, int32_t variant, int32_t D, int32_t R, bool qknorm, bool inter,
@@ -514,9 +523,6 @@ bool rope_paged8_kernel(int32_t dtype, int32_t variant, int32_t D, int32_t R, bo
       return false;
     }
     out->vec = 8;
-    KernelEntry q;
-    if (!rope_paged_kernel(dtype, variant, D, R, qknorm, inter, &q, why)) return false;
-    for (int k = 0; k < 4; ++k) out->q_fn[k] = q.any_fn[k];
     auto vec = [&](auto dt) {
       constexpr int DT = decltype(dt)::value;
       if (D <= 64) inter ? pick_vec<DT, 4, true>(out) : pick_vec<DT, 4, false>(out);

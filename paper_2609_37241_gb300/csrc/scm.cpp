@@ -625,7 +625,6 @@ struct Version {
   RopeSplit rope_split[2];      // layer chain: item splits with one and kChainRopeRows rows
   CUfunction pw_fn[kPwEntries];  // elementwise: entries by layout and size (pointwise_plan)
   CUfunction any_fn[4];            // RoPE versions of the generic kind: rope_any_kernel; rope_paged_kernel
-  CUfunction q_fn[4];              // paged RoPE into 8-bit caches: q alone
   CUfunction attn_tile_fn;       // paged attention: the kernel of many rows
   CUfunction nm_fn[kNormEntries];  // norms: entries by layout and size (norm_plan)
   CUfunction step_fn;           // layer chain: several calls per launch (two blocks per token)
@@ -1186,20 +1185,7 @@ int32_t launch_paged(trident_scm* scm, const Version& v, const trident_args* a, 
     CUfunction fn = v.fn;
     if (v.ke.vec > 1) {
       int32_t threads = 0;
-      bool q_apart = false;
-      fn = v.any_fn[rope_paged8_plan(&p, &grid, &q_apart, &threads, &blocks, scm->sm_count)];
-      if (q_apart) {
-        RopePagedParams q = p.r;
-        q.NH = q.Hq;
-        int32_t q_threads = 0;
-        int64_t q_blocks = 0;
-        const CUfunction q_fn = v.q_fn[rope_paged_plan(&q, &q_threads, &q_blocks, scm->sm_count)];
-        cfg.blockDimX = (unsigned)q_threads;
-        cfg.gridDimX = cap_grid(q_blocks);
-        void* kp[1] = {&q};
-        const int32_t st = launch_on(scm, &cfg, q_fn, kp);
-        if (st != TRIDENT_OK) return st;
-      }
+      fn = v.any_fn[rope_paged8_plan(&p, &grid, &threads, &blocks, scm->sm_count)];
       cfg.blockDimX = (unsigned)threads;
     }
     cfg.gridDimX = cap_grid(blocks);
@@ -1860,7 +1846,7 @@ int32_t append_version(trident_scm_t* scm, const trident_spec_desc* desc, int32_
         if (!resolve(v.ke.pw_fn[k], &v.pw_fn[k]))
           return fail(TRIDENT_ERR_CUDA, "cannot resolve the elementwise kernel entries");
       for (int k = 0; k < 4; ++k)
-        if (!resolve(v.ke.any_fn[k], &v.any_fn[k]) || !resolve(v.ke.q_fn[k], &v.q_fn[k]))
+        if (!resolve(v.ke.any_fn[k], &v.any_fn[k]))
           return fail(TRIDENT_ERR_CUDA, "cannot resolve the RoPE kernel entries");
       for (int k = 0; k < kNormEntries; ++k)
         if (!resolve(v.ke.nm_fn[k], &v.nm_fn[k]))
