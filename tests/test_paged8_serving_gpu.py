@@ -299,3 +299,56 @@ def test_through_a_recipe(S):
     want = torch.stack([x[t[r, j // 16], :, j % 16] for r, j in [(0, j) for j in range(15, 20)] + [(1, j) for j in range(6, 9)]])
     assert torch.equal(v.cpu(), want.bfloat16())
     scm.close()
+
+
+@pytest.mark.parametrize("variant", ["VARIANT_AUTO", "VARIANT_GENERIC"])
+@pytest.mark.parametrize("bt", [16, 32])
+def test_pages_past_32_bits(S, variant, bt):
+    """Pages whose first code lies past 2^32 bytes: every op does there what it does with the same pages at the beginning of
+    a pool, bit for bit; and what lies 2^32 bytes before them is left as it was."""
+    Hq, Hkv, D, ps, dt = 8, 2, 128, 32, S.BF16
+    g = np.random.default_rng(11)
+    new, kv = [1, 70, 150], [400, 90, 700]
+    b = Q.batch(g, new, kv, Hq, Hkv, D, ps, bt, dt)
+    P, T = b["kc"].shape[0], sum(new)
+    off = 2 ** 32 // (Hkv * ps * D)
+    names = ("kc", "vc", "ks", "vs")
+    far = {}
+    for n in names:
+        big = torch.zeros(off + P, *b[n].shape[1:], dtype=torch.uint8, device="cuda")
+        big[off:] = b[n].view(torch.uint8)
+        far[n] = big.view(b[n].dtype)
+    table = b["table"] + off * (b["table"] < P).int()
+    act = R.TORCH[dt]
+    q, k, v = (torch.from_numpy(g.standard_normal((T, h, D)) * 3).to(act).cuda() for h in (Hq, Hkv, Hkv))
+    slot, pos = [], []
+    for r, (n, L) in enumerate(zip(new, kv)):
+        pos += range(L - n, L)
+        slot += [int(b["table"][r, j // ps]) * ps + j % ps for j in range(L - n, L)]
+    pos, slot = i32(pos), i32(slot)
+    s = S.Scm()
+    kw = dict(layout=S.LAYOUT_ANY, variant=getattr(S, variant))
+    s.register(S.make_spec(S.OP_ROPE_PAGED_KV8, dt, [Hq, Hkv, D, D, ps, bt], 1, 1 << 20, **kw))
+    a = s.register(S.make_spec(S.OP_PAGED_ATTN8, dt, [Hq, Hkv, D, ps, bt], 1, 1 << 20, **kw))
+    s.register(S.make_spec(S.OP_PAGED_READ8, dt, [Hkv, D, ps, bt], 1, 1 << 20, **kw))
+    work, freqs, st = torch.zeros(s.workspace(a), device="cuda"), S.rope_freqs(1e4, D), torch.cuda.current_stream().cuda_stream
+
+    def serve(c, table, slot):
+        caches = [c[n] for n in names]
+        rot, out = (torch.zeros(T, Hq, D, dtype=act, device="cuda") for _ in range(2))
+        lse = torch.zeros(T, Hq, device="cuda")
+        ko, vo = (torch.zeros(T, Hkv, D, dtype=act, device="cuda") for _ in range(2))
+        for args in (S.make_args(S.OP_ROPE_PAGED_KV8, [q, k, v, pos, slot, freqs, rot, *caches], scalar=1.0),
+                     S.make_args(S.OP_PAGED_ATTN8, [rot, *caches, table, b["cu"], b["kv"], work, out, lse], scalar=D ** -0.5),
+                     S.make_args(S.OP_PAGED_READ8, [*caches, table, b["cu"], b["kv"] - i32(new), ko, vo])):
+            assert s.invoke(args, st)[0] == S.OK, S.trident_scm_last_error()
+        assert S.trident_scm_device_status(s.h, st)[1] == 0
+        return rot, out, lse, ko, vo
+
+    want, got = serve(b, b["table"], slot), serve(far, table, slot + off * ps)
+    for x, y in zip(want, got):
+        assert torch.isfinite(x).all() and torch.equal(x, y)
+    for n in names:
+        assert torch.equal(far[n][off:].view(torch.uint8), b[n].view(torch.uint8))
+        assert not far[n][:P].view(torch.uint8).any()
+    s.close()
