@@ -59,7 +59,6 @@ __device__ __forceinline__ void tma_4d(uint32_t dst, const CUtensorMap* map, int
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
@@ -110,10 +109,13 @@ __device__ __forceinline__ void tc_st32(uint32_t at, const uint32_t* r) {
                :: TC_I8(r, 0), TC_I8(r, 8), TC_I8(r, 16), TC_I8(r, 24), "r"(at) : "memory");
 }
 
-// The wait, as what brings these registers' values.
-__device__ __forceinline__ void tc_wait_ld32(uint32_t* r) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : TC_W8(r, 0), TC_W8(r, 8), TC_W8(r, 16), TC_W8(r, 24) :: "memory");
+// Waits for the loads before it, as what brings the values of these N registers: a use of them depends on the wait, so
+// that no compiler may move it between a load and the wait.
+template <int N>
+__device__ __forceinline__ void tc_wait_ld(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < N; i += 8) asm volatile("" : TC_W8(r, i));
 }
 __device__ __forceinline__ void tc_st16(uint32_t at, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
@@ -266,7 +268,7 @@ struct TileFrame : TileShape<C> {
     for (int i = 0; i < D / 32; ++i) {
       uint32_t o[32];
       tc_ld32(oc + i * 32, o);
-      tc_wait_ld();
+      tc_wait_ld<32>(o);
       if (live && slot) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -333,7 +335,7 @@ struct TileFrame : TileShape<C> {
             uint32_t o[32];
             __syncwarp();
             tc_ld32(oc + c + d, o);
-            tc_wait_ld();
+            tc_wait_ld<32>(o);
 #pragma unroll
             for (int e = 0; e < 32; ++e) v[d + e] = fmaf(w, __uint_as_float(o[e]), v[d + e]);
           }

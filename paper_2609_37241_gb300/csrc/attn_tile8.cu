@@ -404,7 +404,7 @@ struct Tile8 : TileFrame<Tile8<C>, C> {
         tc_after();
 #pragma unroll
         for (int i = 0; i < KEYS / 32; ++i) tc_ld32(sc + i * 32, a + i * 32);
-        tc_wait_ld();
+        tc_wait_ld<KEYS>(a);
         const int32_t left = see - t * KEYS;  // keys of the tile that the row sees
         if (!GROUPS) {
 #pragma unroll
@@ -445,7 +445,7 @@ struct Tile8 : TileFrame<Tile8<C>, C> {
             for (int i = 0; i < D / 32; ++i) {
               uint32_t o[32];
               tc_ld32(oc + i * 32, o);
-              tc_wait_ld();
+              tc_wait_ld<32>(o);
 #pragma unroll
               for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * g);
               tc_st32(oc + i * 32, o);
