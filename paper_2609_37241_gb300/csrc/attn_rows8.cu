@@ -13,10 +13,13 @@
 // (m16n8k32 of 8 bits takes k's codes as they are, with q in two 8-bit pieces, but was slower: 64 decode steps 127 us for
 // 103.)
 // The scales 2^ek of k and 2^ev of v enter with the scores: with s the score in units of log 2, t = 2^ek s' + ev, the
-// running maximum m is of t, numerators 2^(t - m) hold v's scale already, and l takes them times 2^-ev. So the
-// numerators, rounded to halves, are the sizes of what each key adds to out: a block of small values that has the
-// weights and one of large values that has none are both held to 2^-32 of the largest (numerators reach 2^7, and with a
-// maximum that is 2^8 behind 2^15).
+// running maximum m is of t, numerators 2^(t - m) hold v's scale already, and l takes them times 2^-ev. The numerators
+// are halves: the largest is 2^7 at least (with a maximum that is 2^8 behind 2^15), so each is off by 2^-11 of itself down to
+// 2^-21 of the largest and by 2^-32 of the largest below. In bf16 calls too: rounded to bf16, as over a 16-bit cache, every
+// numerator would lose three bits more. What that costs is a floor. A column gets a key's numerator times a code, at most
+// 448, so what it can lose is n keys * 448 * 2^-32 of the largest numerator: of one key 2^-13 of half the smallest step of a
+// code in that numerator's block, which is what the cache itself is off by there. It shows in columns where that block's
+// codes are 0 or cancel: they get what blocks with numerators of 2^-28 of the largest add, and not what those of 2^-40 do.
 //
 // Measured on a GB300 (32 q heads on 8 kv heads of 128 where nothing else is said; of the 6.77 TB/s copy rate): 64
 // requests of 1000 to 8000 keys 101 us (0.88; the copies alone, with no products, 97), 3 of 131071 keys with a scale for
