@@ -141,7 +141,8 @@ static PyObject* fc_invoke_tree(PyObject* self, PyObject* const* args, Py_ssize_
  * (data_ptr, shape, stride, dtype, get_device); nothing is copied. */
 typedef struct {
   PyObject* tensor_type;
-  PyObject* dtypes[9]; /* bfloat16, float16, float32, int32, int64, uint8, bool, float8_e4m3fn, float8_e8m0fnu */
+  PyObject* dtypes[9]; /* bfloat16, float16, float32, int32, int64, uint8, bool; float8_e4m3fn, float8_e8m0fnu
+                          (NULL in a torch without them) */
   int32_t codes[9];
   PyObject *s_data_ptr, *s_shape, *s_stride, *s_dtype, *s_get_device;
   PyObject *m_data_ptr, *m_stride, *m_get_device; /* torch.Tensor's own methods */
@@ -162,6 +163,10 @@ static int torch_names(void) {
     tn.dtypes[k] = PyObject_GetAttrString(torch, names[k]);
     tn.codes[k] = codes[k];
     ok = tn.dtypes[k] != NULL;
+    if (!ok && k >= 7 && PyErr_ExceptionMatches(PyExc_AttributeError)) {
+      PyErr_Clear();
+      ok = 1;
+    }
   }
   Py_DECREF(torch);
   if (!ok) return -1;

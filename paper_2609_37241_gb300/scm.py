@@ -324,8 +324,11 @@ def _torch_dtypes():
     if _TORCH_DT is None:
         import torch
         _TORCH_DT = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32,
-                     torch.int32: I32, torch.int64: I64, torch.uint8: U8, torch.bool: U8,
-                     torch.float8_e4m3fn: E4M3, torch.float8_e8m0fnu: E8M0}
+                     torch.int32: I32, torch.int64: I64, torch.uint8: U8, torch.bool: U8}
+        # those that only the ops over 8-bit caches take: not every torch has them
+        for name, code in (("float8_e4m3fn", E4M3), ("float8_e8m0fnu", E8M0)):
+            if hasattr(torch, name):
+                _TORCH_DT[getattr(torch, name)] = code
     return _TORCH_DT
 
 
