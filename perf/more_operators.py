@@ -351,6 +351,8 @@ def _plain_attn(s):
 
 
 # ---------------------------------------------------------------- the library's calls
+# Kept for the process, whose passes all go to one stream of one device, one after the other. (Calls that may overlap
+# on the GPU need a workspace each.)
 _lib = {}
 
 
@@ -389,7 +391,7 @@ def _bind(s):
             ts += [s["gamma_q"], s["gamma_k"]]
         return scm, S.make_args(op, ts, eps=EPS, scalar=s["magnitude"]), [q_out, *cache]
     scm, index = _version(S, S.OP_PAGED_ATTN8, dt, [hq, hk, d, ps, bt])
-    if ("work", index) not in _lib:  # a workspace per stream, zeros before its first use
+    if ("work", index) not in _lib:  # one for all of the version's calls, zeros before its first use
         _lib["work", index] = torch.zeros(scm.workspace(index), dtype=torch.float32, device="cuda")
     out, lse = new(tuple(s["q"].shape), s["q"].dtype), new((s["q"].shape[0], hq), torch.float32)
     args = S.make_args(S.OP_PAGED_ATTN8, [s["q"], *cache, s["table"], s["cu"], s["kv"], _lib["work", index], out, lse],
