@@ -23,7 +23,8 @@
 //
 // Measured on a GB300 (32 q heads on 8 kv heads of 128 where nothing else is said; of the 6.77 TB/s copy rate): 64
 // requests of 1000 to 8000 keys 101 us (0.88; the copies alone, with no products, 97), 3 of 131071 keys with a scale for
-// each token 139 us (0.86), one request of 1000 keys 8.9 us. 48 requests of about 3 rows, 28 heads on 4 of 64, over 400 to
+// each token 139 us (0.86), one request of 1000 keys 8.9 us. The 64 requests with heads of 256 199 us (0.89; these spill 24 to
+// 32 bytes of registers), of 64 73 us (0.60). 48 requests of about 3 rows, 28 heads on 4 of 64, over 400 to
 // 3000 keys 30 us: a warp's steps of 32 keys are too short for the memory and bound by their dependent instructions;
 // units of 32 rows, which read the keys once, not twice, are longer and fewer, and took 36.
 #include "attn_rows.cuh"

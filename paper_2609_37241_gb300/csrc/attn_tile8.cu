@@ -14,8 +14,11 @@
 // Warps: NT softmax warpgroups, NT warps that issue products, two that load (k, v), four that convert v and look up the
 // scales.
 //
-// Measured on a GB300 (32 q heads on 8 kv heads of 128, graphs of 30 calls): 8192 rows after 8192 keys 1162 us (1419
-// TFLOP/s, 0.82 of cuBLAS' sustained rate; over a 16-bit cache 978), 2048 rows after 6144 keys 203 us (156). Without the
+// Measured on a GB300 (32 q heads on 8 kv heads of 128, graphs of 30 calls, over a 16-bit cache beside it in parentheses):
+// 8192 rows after 8192 keys 1165 us (950) or 1415 TFLOP/s, 0.82 of cuBLAS' sustained rate (back to back for longer, at the
+// power limit, 1196 (1051)), 2048 rows after 6144 keys 203 us (156), with heads of 64 155 (126), of 256 556 (460). Registers
+// (-Xptxas -v): 248 to 330 bytes of spill stores and 368 to 468 of loads for heads of 64 and 128, 196 and 316 for heads of 256
+// (the 16-bit kernel: 140 to 148 and 248 to 280; none); what they cost has not been taken apart. Without the
 // conversions it is 6% shorter, without half of the scores' products 5%: what bounds it is the chain of a tile's scores,
 // softmax and products, in which every access to shared memory waits beside the products' (a wait that has nothing to
 // wait for takes 200 cycles). Built and measured against this one, 8192 rows after 8192 keys: the conversions by two warps

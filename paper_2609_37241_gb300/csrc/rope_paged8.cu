@@ -155,7 +155,8 @@ __global__ void __launch_bounds__(kThreads) rope_paged8_generic_kernel(const Rop
 //   TEAM 1  blocks of at most ROWS rows. A warp looks a window of tokens over and takes whole runs, as many as its
 //           rows hold: 16 decode steps or a block of a prompt cost the same round of loads.
 //   TEAM 4  larger blocks. The thread block's warps share a run, TEAM * ROWS rows at a time; a longer one is read and
-//           rotated twice.
+//           rotated twice. Runs come one after the other, so decode steps, whose runs are of one row, leave three of four
+//           warps without work: measured below.
 // Thread blocks past kv_blocks rotate q, items of R heads per lane group as rope_paged.cu. They come in as the append's
 // blocks end: that waits for its chains, q for the memory.
 //
@@ -164,6 +165,9 @@ __global__ void __launch_bounds__(kThreads) rope_paged8_generic_kernel(const Rop
 // of its own 49, append blocks spread among q's 45), of which q's 134 MB would take 21 alone; the append is bound by its
 // chain of loads, rotation (a token's sines and cosines once per kv head), maximum and codes. 3333 tokens, half of the
 // head, blocks of 32: 25 us (one head of q per lane group 32, three 26).
+// Decode steps by teams, 64 / 512 steps of these heads with q/k norm: blocks of 1 or 16 rows (a warp's) 4.2 to 4.5 / 8.4 to
+// 9.5 us, of 32 or 64 (a thread block's) 9.5 / 35; heads of 256, blocks of 8 5.8 / 16, of 16 and more 9.6 / 36. The team goes
+// by the block's size though a run may be shorter.
 constexpr int kRope8Threads = 128;
 
 template <int DT, int LPG, bool INTER, int TEAM>
@@ -503,7 +507,11 @@ int rope_paged8_plan(RopePaged8Params* p8, Rope8Grid* grid, int32_t* threads, in
   p->ipt_magic = r.magic;
   p->ipt_shift = r.shift;
   // Tokens of a team's window: as many as a warp's rows; few tokens, whose runs may all be of one, in smaller windows for
-  // more warps. 64 decode steps of 32 + 8 + 8 heads of 128: see the file's head.
+  // more warps. 32 + 8 + 8 heads of 128 with q/k norm, windows of 4 / of 16 tokens, us: decode steps in blocks of 16, 64 of
+  // them 4.4 / 7.3, 304 5.4 / 8.6, 512 7.5 / 9.5, 768 9.0 / 9.1, 1024 11.8 / 10.1, in blocks of 64 9.6 / 29.8, 19.6 / 31.7,
+  // 32.6 / 35.1, 45.9 / 58.0, 59.5 / 65.6; a prompt of 304 in blocks of 16 7.5 / 10.6, of 64 7.0 / 7.0, 512 7.9 / 11.1 and
+  // 8.6 / 6.7, 1024 9.4 / 11.3 and 12.8 / 8.7. The line (304 tokens of these heads) is where prompts in large blocks begin to
+  // lose by small windows; steps would gain from them up to about 750.
   grid->window = p->T * 2 * p->Hkv <= 4 * kRope8Small * sms ? 4 : 16;
   const int64_t units = (p->T + grid->window - 1) / grid->window * 2 * p->Hkv;
   const int64_t kv = team ? units : (units + kWarps - 1) / kWarps, q = (p->T * r.ipt + kWarps - 1) / kWarps;
