@@ -214,8 +214,8 @@ typedef enum trident_dtype {
  *   PAGED_ATTN with k and v = code * scale, in all that is said there but for what is rounded. Codes below kv_len must
  *   not be NaN; codes and scales past it may be anything. Key j's numerator for the product with v holds the scale
  *   2^e_j of v's block: softmax_j * 2^e_j, in fp16 for both activation types. It is off by at most 2^-11 of itself down
- *   to 2^-21 of the row's largest numerator, and below that by at most 2^-32 of the largest; so an element of out is off,
- *   beside its own rounding, by at most 2^-11 * sum_j softmax_j |v_j| + 448 * 2^-32 * (keys seen) * max_j(softmax_j * 2^e_j).
+ *   to 2^-21 of the row's largest numerator, and below that by at most 2^-32 of the largest; this takes an
+ *   element of out off by at most 2^-11 * sum_j softmax_j |v_j| + 448 * 2^-32 * (keys seen) * max_j(softmax_j * 2^e_j).
  *   The second term counts where the block with the largest numerator has codes 0 or ones that cancel: there keys whose
  *   numerators are below 2^-32 of the largest may be lost. (Of one key it is 2^-14 of what that block's smallest code,
  *   2^-9, would add.) TRIDENT_VARIANT_GENERIC keeps its numerators in fp32 and has neither term. Where a request has many

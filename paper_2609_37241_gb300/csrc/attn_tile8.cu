@@ -9,8 +9,9 @@
 //            memory traffic per 128 keys of 128 elements (copy in, read, write) beside the products' own 192.
 //   softmax  the scales 2^ek, 2^ev of k and v enter with the scores: t = 2^ek s' + ev in units of log 2, the running
 //            maximum is of t, numerators 2^(t - m) are halves and hold v's scale, the sum takes them times 2^-ev
-//            (attn_rows8.cu has the reasons and what a column can lose by it). Where a scale's block is 16 keys or more, the 16 scores of a group share
-//            the factors: the group's maximum is taken before they are applied. Else each key has its own.
+//            (attn_rows8.cu has the reasons and what a column can lose by it). Where a scale's block is 16 keys or more,
+//            the 16 scores of a group share the factors: the group's maximum is taken before they are applied. Else each
+//            key has its own.
 // Warps: NT softmax warpgroups, NT warps that issue products, two that load (k, v), four that convert v and look up the
 // scales.
 //
